@@ -274,6 +274,106 @@ int cardan_dense_moe_layer_relu2(const cardan_shape* shape, int32_t B, const car
 int cardan_rmsnorm_bf16(int32_t B, int32_t H, const float* y, float eps,
                         cardan_bf16* x_next, hipStream_t stream);
 
+/* ---- training: the feed-forward block and the distillation loss -----------
+ * The second stage of fitting a compressed layer (paper Sec. 3.3): a student
+ * layer in dense bf16 form runs forward and backward over rows of any number,
+ * and its logits are trained against a teacher's kept top logits, Eq. (3).
+ * Conventions as above, except: the workspace of these calls needs no zero
+ * fill, holds nothing between calls, and may serve any call of these two
+ * operators in turn; their kernels are not persistent and do not wait on one
+ * another. */
+
+/* Shape of a feed-forward block: E matrix sets (experts) of hidden size H and
+ * intermediate size I. H % 64 == 0, I % 32 == 0, 1 <= E <= 1024, H * I * 2
+ * below 2^31. */
+typedef struct {
+  int32_t H, I, E;
+  int32_t act; /* CARDAN_FFN_SILU_GLU or CARDAN_FFN_RELU2_UP */
+} cardan_ffn_shape;
+
+enum {
+  CARDAN_FFN_SILU_GLU = 0, /* h = silu(x W_gate) * (x W_up)                  */
+  CARDAN_FFN_RELU2_UP = 1  /* h = max(x W_up, 0)^2; W_gate is not read       */
+};
+
+/* Dense bf16 weights (device pointers), laid out as in cardan_dense_layer. */
+typedef struct {
+  const cardan_bf16* W_gate; /* [E][H][I] */
+  const cardan_bf16* W_up;   /* [E][H][I] */
+  const cardan_bf16* W_down; /* [E][I][H] */
+} cardan_ffn_weights;
+
+/* Workspace bytes of cardan_ffn_forward and cardan_ffn_backward for up to N
+ * rows of this shape (0 is possible). Host-only. */
+int cardan_ffn_workspace_bytes(const cardan_ffn_shape* shape, int32_t N, size_t* out);
+
+/* The experts' computation of paper Sec. 2.1 on dense weights, for rows
+ * grouped by expert: rows offsets[e] <= n < offsets[e + 1] of x [N][H] bf16
+ * go through matrix set e, y[n] = W_down[e]^T h[n] with h[n] as the
+ * activation says, float32 accumulation, y [N][H] bf16. h enters the second
+ * product in bf16.
+ * offsets: [E + 1] int32 on the device, non-decreasing, within [0, N]; NULL
+ * with E == 1 means all rows. Groups may be empty. Rows in no group are not
+ * read, and theirs of y (and of the kept activations) are left as they were.
+ * Offsets outside [0, N] or decreasing are cut to ranges inside the tensors
+ * (memory-safe); the rows concerned are then unspecified.
+ * gate, up: [N][I] float32, hidden: [N][I] bf16: the activations that
+ * cardan_ffn_backward reads. All three NULL: none are kept (gate is always
+ * NULL with CARDAN_FFN_RELU2_UP). N may be 0: nothing is launched. */
+int cardan_ffn_forward(const cardan_ffn_shape* shape, int32_t N, const cardan_bf16* x,
+                       const int32_t* offsets, const cardan_ffn_weights* weights, cardan_bf16* y,
+                       float* gate, float* up, cardan_bf16* hidden, void* ws, size_t ws_bytes,
+                       hipStream_t stream);
+
+/* Gradients of cardan_ffn_forward for the upstream gradient dy [N][H] bf16,
+ * from its inputs and the activations that it kept:
+ *   dh = dy W_down^T;  du = dh silu(g), dg = dh u silu'(g)  (or du = 2 dh max(u, 0))
+ *   dx = dg W_gate^T + du W_up^T;  dW_gate = x^T dg, dW_up = x^T du, dW_down = h^T dy
+ * with float32 accumulation; dg and du enter the products in bf16. dx [N][H]
+ * bf16 or NULL; dW_gate and dW_up ([E][H][I] bf16, both or neither; dW_gate
+ * NULL with CARDAN_FFN_RELU2_UP) or NULL; dW_down [E][I][H] bf16 or NULL: a
+ * NULL output is not computed, one at least is required. Weight gradients are
+ * written whole (zero for a group without rows), not accumulated. */
+int cardan_ffn_backward(const cardan_ffn_shape* shape, int32_t N, const cardan_bf16* dy,
+                        const cardan_bf16* x, const int32_t* offsets,
+                        const cardan_ffn_weights* weights, const float* gate, const float* up,
+                        const cardan_bf16* hidden, cardan_bf16* dx, cardan_bf16* dW_gate,
+                        cardan_bf16* dW_up, cardan_bf16* dW_down, void* ws, size_t ws_bytes,
+                        hipStream_t stream);
+
+enum { CARDAN_LOGITS_BF16 = 0, CARDAN_LOGITS_F32 = 1 };
+
+/* Workspace bytes of cardan_distill_loss for up to N rows (0 is possible).
+ * Host-only. */
+int cardan_distill_workspace_bytes(int32_t N, size_t* out);
+
+/* Distillation loss of paper Sec. 3.3, Eq. (3), per row, with its gradient:
+ * student logits s over V vocabulary entries (row n at logits + n * ld, type
+ * `logits_type`), a teacher's K kept logits t_j at entries i_j
+ * (teacher [N][K] float32, ids [N][K] int32), temperature T:
+ *   kd = T^2 sum_j p_j (log p_j - log q_{i_j}),  p = softmax_j(t / T),
+ *        q = softmax(s / T) over all V entries;
+ *   ce = -log softmax(s)[label].
+ * loss [N][2] float32 receives kd and ce. dlogits (type of the logits, row
+ * stride dld; NULL: not computed) receives the gradient of
+ * sum_n row_weight[n] (kd_n + ce_weight * ce_n), rounded once; it may be the
+ * logits' own memory (dlogits == logits and dld == ld), and must not overlap
+ * them otherwise. row_weight: [N] float32, NULL for ones.
+ * An id outside [0, V) is no entry (the teacher's distribution is over the
+ * others; a row without any has kd = 0); a label outside [0, V) is none (ce =
+ * 0); labels may be NULL. A row with neither gets zero loss and gradient and
+ * its logits are not looked at. An entry named twice counts with both its
+ * probabilities. -inf logits have probability 0; NaN or +inf among a row's
+ * logits give that row NaN. Values between V and the row strides are neither
+ * read nor written.
+ * 0 <= N, 1 <= V <= 2^30, 0 <= K <= 1024 (teacher and ids may be NULL at
+ * K == 0), V <= ld, dld <= 2^40, T > 0 and finite, ce_weight finite. */
+int cardan_distill_loss(int32_t N, int32_t V, int32_t K, int32_t logits_type, const void* logits,
+                        int64_t ld, const float* teacher, const int32_t* ids,
+                        const int32_t* labels, float temperature, float ce_weight,
+                        const float* row_weight, float* loss, void* dlogits, int64_t dld,
+                        void* ws, size_t ws_bytes, hipStream_t stream);
+
 /* Kernel timing for measurement. cardan_profile_begin(n) makes the next n
  * calls launch each kernel with a HIP start/stop event pair recorded by the
  * dispatch itself (hipExtLaunchKernel), on the call's stream, so the pair

@@ -16,7 +16,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libcardan.so")
-SOURCES = ["cardan_kernels.hip", "cardan_api.hip", "cardan_planner.cpp"]
+SOURCES = ["cardan_kernels.hip", "cardan_api.hip", "cardan_planner.cpp",
+           "cardan_ffn.hip", "cardan_distill.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

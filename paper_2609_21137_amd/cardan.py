@@ -47,6 +47,14 @@ class Shape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("H", "I", "E", "top_k", "d", "K", "r")]
 
 
+class FfnShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("H", "I", "E", "act")]
+
+
+class FfnWeightsStruct(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("W_gate", "W_up", "W_down")]
+
+
 class LayerStruct(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in LAYER_FIELDS]
 
@@ -64,6 +72,9 @@ def _load():
     sp = ctypes.POINTER(Shape)
     lp = ctypes.POINTER(LayerStruct)
     dp = ctypes.POINTER(DenseLayerStruct)
+    fp = ctypes.POINTER(FfnShape)
+    wp = ctypes.POINTER(FfnWeightsStruct)
+    i64, f32 = ctypes.c_int64, ctypes.c_float
     sig = {
         "cardan_abi_version": ([], ctypes.c_int),
         "cardan_last_error": ([], ctypes.c_char_p),
@@ -80,6 +91,12 @@ def _load():
         "cardan_dense_moe_layer": ([sp, i32, vp, dp, vp, vp, vp, vp, sz, vp], ctypes.c_int),
         "cardan_dense_moe_layer_relu2": ([sp, i32, vp, dp, vp, vp, vp, vp, sz, vp], ctypes.c_int),
         "cardan_rmsnorm_bf16": ([i32, i32, vp, ctypes.c_float, vp, vp], ctypes.c_int),
+        "cardan_ffn_workspace_bytes": ([fp, i32, ctypes.POINTER(sz)], ctypes.c_int),
+        "cardan_ffn_forward": ([fp, i32, vp, vp, wp, vp, vp, vp, vp, vp, sz, vp], ctypes.c_int),
+        "cardan_ffn_backward": ([fp, i32, vp, vp, vp, wp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp], ctypes.c_int),
+        "cardan_distill_workspace_bytes": ([i32, ctypes.POINTER(sz)], ctypes.c_int),
+        "cardan_distill_loss": ([i32, i32, i32, i32, vp, i64, vp, vp, vp, f32, f32, vp, vp, vp, i64, vp, sz, vp],
+                                ctypes.c_int),
         "cardan_profile_begin": ([i32], ctypes.c_int),
         "cardan_profile_end": ([ctypes.POINTER(ctypes.c_float), ctypes.POINTER(i32)], ctypes.c_int),
     }
@@ -98,6 +115,8 @@ EXPORTED = (
     "cardan_moe_decode_step", "cardan_moe_layer_relu2",
     "cardan_moe_layer_dense_down", "cardan_dense_moe_layer", "cardan_dense_moe_layer_relu2",
     "cardan_rmsnorm_bf16",
+    "cardan_ffn_workspace_bytes", "cardan_ffn_forward", "cardan_ffn_backward",
+    "cardan_distill_workspace_bytes", "cardan_distill_loss",
     "cardan_profile_begin", "cardan_profile_end",
 )
 
@@ -425,6 +444,184 @@ def rmsnorm_bf16(y, eps: float = 1e-6, out=None):
     _check(_lib.cardan_rmsnorm_bf16(B, H, _ptr(y, torch.float32, "y", (B, H)), eps,
                                     _ptr(xn, torch.bfloat16, "x_next", (B, H)), _stream(y.device)))
     return xn
+
+
+# ---------------------------------------------------------------------------
+# training: the feed-forward block and the distillation loss
+# ---------------------------------------------------------------------------
+FFN_ACTS = {"silu_glu": 0, "relu2_up": 1}
+
+
+def _on(dev, *named):
+    """Every tensor of a call must live on its device."""
+    for name, t in named:
+        if isinstance(t, torch.Tensor) and t.device != dev:
+            raise ValueError(f"{name} is on {t.device}, expected {dev}")
+
+
+def ffn_shape(H, I, E=1, act="silu_glu") -> FfnShape:
+    if act not in FFN_ACTS:
+        raise ValueError(f"unknown activation {act!r}")
+    return FfnShape(H, I, E, FFN_ACTS[act])
+
+
+def ffn_workspace_bytes(shape: FfnShape, N: int) -> int:
+    """Bytes of workspace of a forward or backward call over up to N rows (no
+    zero fill needed; nothing is kept in it between calls)."""
+    out = ctypes.c_size_t(0)
+    _check(_lib.cardan_ffn_workspace_bytes(ctypes.byref(shape), N, ctypes.byref(out)))
+    return out.value
+
+
+def _ffn_call(x, W_gate, W_up, W_down, offsets, act, ws):
+    """Shape, weights, offsets and workspace of a call, as the ABI takes them."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+        raise ValueError("x must be a [N, H] tensor")
+    if not isinstance(W_up, torch.Tensor) or W_up.dim() not in (2, 3):
+        raise ValueError("W_up must be a [H, I] or [E, H, I] tensor")
+    N, H = x.shape
+    many = W_up.dim() == 3
+    E, I = (W_up.shape[0] if many else 1), W_up.shape[-1]
+    shape = ffn_shape(H, I, E, act)
+    pre = (E,) if many else ()
+    up_only = act == "relu2_up"
+    if up_only and W_gate is not None:
+        raise ValueError("up-only experts have no W_gate")
+    dev = x.device
+    _on(dev, ("W_gate", W_gate), ("W_up", W_up), ("W_down", W_down), ("offsets", offsets), ("ws", ws))
+    pg = _ptr(W_gate, torch.bfloat16, "W_gate", pre + (H, I), optional=up_only)
+    weights = FfnWeightsStruct(None if pg is None else pg.value,
+                               _ptr(W_up, torch.bfloat16, "W_up", pre + (H, I)).value,
+                               _ptr(W_down, torch.bfloat16, "W_down", pre + (I, H)).value)
+    off = _ptr(offsets, torch.int32, "offsets", (E + 1,), optional=E == 1)
+    if ws is None:
+        ws = torch.empty(ffn_workspace_bytes(shape, N), dtype=torch.uint8, device=dev)
+    return shape, N, weights, off, ws
+
+
+def ffn_forward(x, W_gate, W_up, W_down, offsets=None, act: str = "silu_glu", save: bool = False,
+                ws=None, out=None, saved=None):
+    """Feed-forward block of dense bf16 weights: ``y = h W_down`` with
+    ``h = silu(x W_gate) * (x W_up)``, or ``max(x W_up, 0)^2`` for
+    ``act="relu2_up"`` (``W_gate=None``).
+
+    ``x [N, H]``; weights ``[H, I]`` / ``[I, H]``, or ``[E, H, I]`` /
+    ``[E, I, H]`` with ``offsets`` (int32 ``[E + 1]``): rows
+    ``offsets[e]:offsets[e + 1]`` go through expert e. Returns ``y [N, H]``
+    (bf16; rows in no group are not written), and with ``save=True`` also the
+    activations ``(gate, up, hidden)`` that ``ffn_backward`` reads (float32,
+    float32, bf16, ``[N, I]``; ``gate`` is None for up-only experts).
+    ``out`` and ``saved`` give the tensors to write."""
+    shape, N, weights, off, ws = _ffn_call(x, W_gate, W_up, W_down, offsets, act, ws)
+    H, I, dev = shape.H, shape.I, x.device
+    y = out if out is not None else torch.empty((N, H), dtype=torch.bfloat16, device=dev)
+    g = u = h = None
+    if save or saved is not None:
+        g, u, h = saved if saved is not None else (
+            torch.empty((N, I), dtype=torch.float32, device=dev) if act == "silu_glu" else None,
+            torch.empty((N, I), dtype=torch.float32, device=dev),
+            torch.empty((N, I), dtype=torch.bfloat16, device=dev))
+    _on(dev, ("out", y), ("gate", g), ("up", u), ("hidden", h))
+    keep = u is not None
+    with torch.cuda.device(dev):
+        _check(_lib.cardan_ffn_forward(
+            ctypes.byref(shape), N, _ptr(x, torch.bfloat16, "x", (N, H)), off, ctypes.byref(weights),
+            _ptr(y, torch.bfloat16, "out", (N, H)),
+            _ptr(g, torch.float32, "gate", (N, I), optional=not keep or act != "silu_glu"),
+            _ptr(u, torch.float32, "up", (N, I), optional=not keep),
+            _ptr(h, torch.bfloat16, "hidden", (N, I), optional=not keep),
+            _ptr(ws, torch.uint8, "ws"), ws.numel(), _stream(dev)))
+    return (y, (g, u, h)) if keep else y
+
+
+def ffn_backward(dy, x, W_gate, W_up, W_down, saved, offsets=None, act: str = "silu_glu",
+                 need_dx: bool = True, need_dw: bool = True, ws=None, out=None):
+    """Gradients of ``ffn_forward`` for the upstream gradient ``dy [N, H]``
+    (bf16), from the activations ``saved`` by it. Returns ``(dx, dW_gate,
+    dW_up, dW_down)`` in bf16, laid out as their inputs (rows in no group of
+    dx are not written; weight gradients of a group without rows are zero);
+    None where not asked for. ``out`` gives the four tensors to write."""
+    shape, N, weights, off, ws = _ffn_call(x, W_gate, W_up, W_down, offsets, act, ws)
+    H, I, dev = shape.H, shape.I, x.device
+    gated = act == "silu_glu"
+    if out is not None:
+        dx, dWg, dWu, dWd = out
+    else:
+        dx = torch.empty_like(x) if need_dx else None
+        dWg = torch.empty_like(W_gate) if need_dw and gated else None
+        dWu, dWd = (torch.empty_like(W_up), torch.empty_like(W_down)) if need_dw else (None, None)
+    g, u, h = saved
+    _on(dev, ("dy", dy), ("gate", g), ("up", u), ("hidden", h), ("dx", dx), ("dW_gate", dWg), ("dW_up", dWu),
+        ("dW_down", dWd))
+    bf = torch.bfloat16
+    with torch.cuda.device(dev):
+        _check(_lib.cardan_ffn_backward(
+            ctypes.byref(shape), N, _ptr(dy, bf, "dy", (N, H)), _ptr(x, bf, "x", (N, H)), off,
+            ctypes.byref(weights), _ptr(g, torch.float32, "gate", (N, I), optional=not gated),
+            _ptr(u, torch.float32, "up", (N, I)), _ptr(h, bf, "hidden", (N, I)),
+            _ptr(dx, bf, "dx", (N, H), optional=True),
+            _ptr(dWg, bf, "dW_gate", W_gate.shape if gated else None, optional=True),
+            _ptr(dWu, bf, "dW_up", W_up.shape, optional=True), _ptr(dWd, bf, "dW_down", W_down.shape, optional=True),
+            _ptr(ws, torch.uint8, "ws"), ws.numel(), _stream(dev)))
+    return dx, dWg, dWu, dWd
+
+
+def _rows_ptr(t, dtype, name, shape):
+    """A [N, V] tensor whose rows are contiguous, as (pointer, row stride)."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if t.dtype != dtype or t.device.type != "cuda" or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be a GPU tensor of {dtype} and shape {tuple(shape)}, "
+                         f"got {t.dtype}, {tuple(t.shape)} on {t.device}")
+    N, V = t.shape
+    if V > 1 and t.stride(1) != 1:
+        raise ValueError(f"the rows of {name} must be contiguous")
+    ld = t.stride(0) if N > 1 else V
+    if ld < V:
+        raise ValueError(f"the rows of {name} overlap")
+    return ctypes.c_void_p(t.data_ptr()), ld
+
+
+def distill_loss(logits, teacher, ids, labels=None, temperature: float = 1.0, ce_weight: float = 0.0,
+                 row_weight=None, grad: bool = True, out=None, dlogits=None, ws=None):
+    """Distillation loss of student ``logits [N, V]`` (bf16 or float32, rows
+    may be padded) against a teacher's kept logits ``teacher [N, K]`` (float32)
+    at the vocabulary entries ``ids [N, K]`` (int32), and its gradient.
+
+    Returns ``(loss [N, 2], dlogits)``: per row ``kd = T^2 KL(softmax(teacher
+    / T) || softmax(logits / T))`` over the teacher's entries and the cross
+    entropy of ``labels`` (int32, [N]); ``dlogits`` is the gradient of
+    ``sum_n row_weight[n] (kd_n + ce_weight ce_n)`` in the logits' type and
+    with rows padded as theirs, or None with ``grad=False``. ``dlogits=logits`` overwrites the
+    logits. Ids and labels outside ``[0, V)`` mark absent entries and labels."""
+    if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or logits.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("logits must be a [N, V] tensor of bfloat16 or float32")
+    N, V = logits.shape
+    dev = logits.device
+    if not isinstance(ids, torch.Tensor) or ids.dim() != 2:
+        raise ValueError("ids must be a [N, K] tensor")
+    K = ids.shape[1]
+    lp, ld = _rows_ptr(logits, logits.dtype, "logits", (N, V))
+    loss = out if out is not None else torch.empty((N, 2), dtype=torch.float32, device=dev)
+    if dlogits is None and grad:
+        # rows as far apart as the logits' (their alignment), where that is padding
+        dlogits = torch.empty((N, ld if ld <= 2 * V else V), dtype=logits.dtype, device=dev)[:, :V]
+    _on(dev, ("teacher", teacher), ("ids", ids), ("labels", labels), ("row_weight", row_weight), ("out", loss),
+        ("dlogits", dlogits), ("ws", ws))
+    gp, dld = _rows_ptr(dlogits, logits.dtype, "dlogits", (N, V)) if dlogits is not None else (None, 0)
+    if ws is None:
+        need = ctypes.c_size_t(0)
+        _check(_lib.cardan_distill_workspace_bytes(N, ctypes.byref(need)))
+        ws = torch.empty(need.value, dtype=torch.uint8, device=dev)
+    with torch.cuda.device(dev):
+        _check(_lib.cardan_distill_loss(
+            N, V, K, 1 if logits.dtype == torch.float32 else 0, lp, ld,
+            _ptr(teacher, torch.float32, "teacher", (N, K)), _ptr(ids, torch.int32, "ids", (N, K)),
+            _ptr(labels, torch.int32, "labels", (N,), optional=True), temperature, ce_weight,
+            _ptr(row_weight, torch.float32, "row_weight", (N,), optional=True),
+            _ptr(loss, torch.float32, "out", (N, 2)), gp, dld, _ptr(ws, torch.uint8, "ws"), ws.numel(),
+            _stream(dev)))
+    return loss, dlogits
 
 
 def profile_begin(max_calls: int):

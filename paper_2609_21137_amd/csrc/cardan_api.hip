@@ -13,6 +13,7 @@
 #include <vector>
 
 #include "../../include/cardan.h"
+#include "cardan_ffn.h"
 #include "cardan_plan.h"
 
 namespace cardan {
@@ -23,6 +24,11 @@ hipError_t launch_expert(const Plan&, const Args&, const Chain&, int, size_t, hi
 hipError_t launch_route_reset(const Plan&, const Args&, hipStream_t);
 hipError_t launch_zero(void* p, size_t bytes, hipStream_t);
 hipError_t launch_rmsnorm(hipStream_t, int, int, const float*, float, uint16_t*, hipEvent_t, hipEvent_t);
+// The training kernels' launchers are weak: a build of the host code without
+// them (the sanitizer tests') links, and reports a HIP error if one is reached.
+__attribute__((weak)) hipError_t launch_ffn_forward(const FfnArgs&, hipStream_t);
+__attribute__((weak)) hipError_t launch_ffn_backward(const FfnArgs&, hipStream_t);
+__attribute__((weak)) hipError_t launch_distill(const DistillArgs&, hipStream_t);
 }  // namespace cardan
 
 using namespace cardan;
@@ -703,6 +709,187 @@ int cardan_rmsnorm_bf16(int32_t B, int32_t H, const float* y, float eps, cardan_
   tm.done();
   prof_next_call();
   return CARDAN_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+int check_ffn(const cardan_ffn_shape* s, int32_t N) {
+  if (!s) return fail(CARDAN_ERR_NULL_PTR, "shape is NULL");
+  if (s->H <= 0 || s->I <= 0 || s->E <= 0) return fail(CARDAN_ERR_BAD_SHAPE, "H, I and E must be positive");
+  if (N < 0) return fail(CARDAN_ERR_BAD_SHAPE, "N=%d is negative", N);
+  if (s->act != CARDAN_FFN_SILU_GLU && s->act != CARDAN_FFN_RELU2_UP)
+    return fail(CARDAN_ERR_UNSUPPORTED, "activation %d is not known", s->act);
+  if (s->H % 64) return fail(CARDAN_ERR_UNSUPPORTED, "H=%d must be a multiple of 64", s->H);
+  if (s->I % 32) return fail(CARDAN_ERR_UNSUPPORTED, "I=%d must be a multiple of 32", s->I);
+  if (s->E > kMaxE) return fail(CARDAN_ERR_UNSUPPORTED, "E=%d exceeds %d", s->E, kMaxE);
+  if ((size_t)s->H * s->I * 2 >= 0x80000000ull)
+    return fail(CARDAN_ERR_UNSUPPORTED, "matrix of H=%d x I=%d exceeds 2 GiB", s->H, s->I);
+  return CARDAN_OK;
+}
+
+// What forward and backward calls share: shape, weights, offsets, workspace.
+int check_ffn_call(const cardan_ffn_shape* s, int32_t N, const int32_t* offsets, const cardan_ffn_weights* w,
+                   const void* ws, size_t ws_bytes, FfnArgs* A) {
+  int rc = check_ffn(s, N);
+  if (rc) return rc;
+  if (!w) return fail(CARDAN_ERR_NULL_PTR, "weights is NULL");
+  const bool gated = s->act == CARDAN_FFN_SILU_GLU;
+  if (gated) REQ(w->W_gate, "W_gate");
+  REQ(w->W_up, "W_up");
+  REQ(w->W_down, "W_down");
+  if (s->E > 1 && !offsets) return fail(CARDAN_ERR_NULL_PTR, "offsets is NULL with E=%d", s->E);
+  if (reinterpret_cast<uintptr_t>(offsets) & 3u) return fail(CARDAN_ERR_ALIGN, "offsets is not 4-byte aligned");
+  size_t need = 0;
+  if ((rc = cardan_ffn_workspace_bytes(s, N, &need))) return rc;
+  if (need > 0 && (rc = check_ws(need, ws, ws_bytes))) return rc;
+  memset(A, 0, sizeof *A);
+  A->N = N;
+  A->E = s->E;
+  A->H = s->H;
+  A->I = s->I;
+  A->relu2 = !gated;
+  A->off = offsets;
+  A->Wg = gated ? w->W_gate : nullptr;
+  A->Wu = w->W_up;
+  A->Wd = w->W_down;
+  return CARDAN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int cardan_ffn_workspace_bytes(const cardan_ffn_shape* shape, int32_t N, size_t* out) {
+  g_err[0] = 0;
+  int rc = check_ffn(shape, N);
+  if (rc) return rc;
+  if (!out) return fail(CARDAN_ERR_NULL_PTR, "out is NULL");
+  // dg and du of the backward pass; a forward pass that keeps nothing has h there
+  *out = 2 * align256((size_t)N * shape->I * 2);
+  return CARDAN_OK;
+}
+
+int cardan_ffn_forward(const cardan_ffn_shape* shape, int32_t N, const cardan_bf16* x, const int32_t* offsets,
+                       const cardan_ffn_weights* weights, cardan_bf16* y, float* gate, float* up,
+                       cardan_bf16* hidden, void* ws, size_t ws_bytes, hipStream_t stream) {
+  g_err[0] = 0;
+  FfnArgs A;
+  int rc = check_ffn_call(shape, N, offsets, weights, ws, ws_bytes, &A);
+  if (rc) return rc;
+  if (N == 0) return CARDAN_OK;
+  REQ(x, "x");
+  REQ(y, "y");
+  if (gate || up || hidden) {
+    if (!A.relu2) REQ(gate, "gate");
+    if (A.relu2 && gate) return fail(CARDAN_ERR_BAD_SHAPE, "up-only experts keep no gate projection");
+    REQ(up, "up");
+    REQ(hidden, "hidden");
+  }
+  A.x = x;
+  A.y = y;
+  A.g = gate;
+  A.u = up;
+  A.h = hidden ? hidden : static_cast<uint16_t*>(ws);
+  const hipError_t e = launch_ffn_forward ? launch_ffn_forward(A, stream) : hipErrorInvalidDeviceFunction;
+  return e == hipSuccess ? CARDAN_OK : hip_fail(e, "ffn forward launch");
+}
+
+int cardan_ffn_backward(const cardan_ffn_shape* shape, int32_t N, const cardan_bf16* dy, const cardan_bf16* x,
+                        const int32_t* offsets, const cardan_ffn_weights* weights, const float* gate,
+                        const float* up, const cardan_bf16* hidden, cardan_bf16* dx, cardan_bf16* dW_gate,
+                        cardan_bf16* dW_up, cardan_bf16* dW_down, void* ws, size_t ws_bytes, hipStream_t stream) {
+  g_err[0] = 0;
+  FfnArgs A;
+  int rc = check_ffn_call(shape, N, offsets, weights, ws, ws_bytes, &A);
+  if (rc) return rc;
+  if (A.relu2 && (gate || dW_gate))
+    return fail(CARDAN_ERR_BAD_SHAPE, "up-only experts have no gate projection (gate, dW_gate)");
+  if (N > 0) {
+    REQ(dy, "dy");
+    REQ(x, "x");
+    if (!A.relu2) REQ(gate, "gate");
+    REQ(up, "up");
+    REQ(hidden, "hidden");
+  }
+  if (!dx && !dW_gate && !dW_up && !dW_down && N > 0) return fail(CARDAN_ERR_NULL_PTR, "no gradient is asked for");
+  if (!A.relu2 && (!dW_gate) != (!dW_up))
+    return fail(CARDAN_ERR_NULL_PTR, "dW_gate and dW_up are computed together: both or neither");
+  if (misaligned(dx) || misaligned(dW_gate) || misaligned(dW_up) || misaligned(dW_down))
+    return fail(CARDAN_ERR_ALIGN, "a gradient is not 16-byte aligned");
+  A.x = x;
+  A.dy = dy;
+  A.g = const_cast<float*>(gate);
+  A.u = const_cast<float*>(up);
+  A.h = const_cast<uint16_t*>(hidden);
+  A.dg = static_cast<uint16_t*>(ws);
+  A.du = reinterpret_cast<uint16_t*>(static_cast<uint8_t*>(ws) + align256((size_t)N * shape->I * 2));
+  A.dx = dx;
+  A.dWg = dW_gate;
+  A.dWu = dW_up;
+  A.dWd = dW_down;
+  const hipError_t e = launch_ffn_backward ? launch_ffn_backward(A, stream) : hipErrorInvalidDeviceFunction;
+  return e == hipSuccess ? CARDAN_OK : hip_fail(e, "ffn backward launch");
+}
+
+int cardan_distill_workspace_bytes(int32_t N, size_t* out) {
+  g_err[0] = 0;
+  if (N < 0) return fail(CARDAN_ERR_BAD_SHAPE, "N=%d is negative", N);
+  if (!out) return fail(CARDAN_ERR_NULL_PTR, "out is NULL");
+  *out = 0;
+  return CARDAN_OK;
+}
+
+int cardan_distill_loss(int32_t N, int32_t V, int32_t K, int32_t logits_type, const void* logits, int64_t ld,
+                        const float* teacher, const int32_t* ids, const int32_t* labels, float temperature,
+                        float ce_weight, const float* row_weight, float* loss, void* dlogits, int64_t dld,
+                        void* ws, size_t ws_bytes, hipStream_t stream) {
+  g_err[0] = 0;
+  if (N < 0 || V < 1 || V > (1 << 30)) return fail(CARDAN_ERR_BAD_SHAPE, "N=%d, V=%d outside the valid range", N, V);
+  if (K < 0 || K > 1024) return fail(CARDAN_ERR_UNSUPPORTED, "K=%d outside [0, 1024]", K);
+  if (logits_type != CARDAN_LOGITS_BF16 && logits_type != CARDAN_LOGITS_F32)
+    return fail(CARDAN_ERR_UNSUPPORTED, "logits type %d is not known", logits_type);
+  const int64_t most = (int64_t)1 << 40;
+  if (ld < V || ld > most || (dlogits && (dld < V || dld > most)))
+    return fail(CARDAN_ERR_BAD_SHAPE, "row strides %lld, %lld are below V=%d or too large", (long long)ld,
+                (long long)dld, V);
+  if (!(temperature > 0.0f) || !isfinite(temperature) || !isfinite(1.0f / temperature) || !isfinite(ce_weight))
+    return fail(CARDAN_ERR_BAD_SHAPE, "temperature must be finite and > 0, ce_weight finite");
+  size_t need = 0;
+  int rc = cardan_distill_workspace_bytes(N, &need);
+  if (rc) return rc;
+  if (need > 0 && (rc = check_ws(need, ws, ws_bytes))) return rc;
+  if (N == 0) return CARDAN_OK;
+  REQ(logits, "logits");
+  REQ(loss, "loss");
+  if (K > 0) {
+    REQ(teacher, "teacher");
+    REQ(ids, "ids");
+  }
+  if (misaligned(dlogits)) return fail(CARDAN_ERR_ALIGN, "dlogits is not 16-byte aligned");
+  if (dlogits == logits && dld != ld) return fail(CARDAN_ERR_BAD_SHAPE, "dlogits in place of the logits needs dld == ld");
+  if ((reinterpret_cast<uintptr_t>(labels) | reinterpret_cast<uintptr_t>(row_weight)) & 3u)
+    return fail(CARDAN_ERR_ALIGN, "labels or row_weight is not 4-byte aligned");
+  DistillArgs A;
+  memset(&A, 0, sizeof A);
+  A.N = N;
+  A.V = V;
+  A.K = K;
+  A.f32 = logits_type == CARDAN_LOGITS_F32;
+  A.ld = ld;
+  A.dld = dld;
+  A.logits = logits;
+  A.teacher = teacher;
+  A.ids = ids;
+  A.labels = labels;
+  A.weight = row_weight;
+  A.temperature = temperature;
+  A.ce_weight = ce_weight;
+  A.loss = loss;
+  A.dlogits = dlogits;
+  const hipError_t e = launch_distill ? launch_distill(A, stream) : hipErrorInvalidDeviceFunction;
+  return e == hipSuccess ? CARDAN_OK : hip_fail(e, "distillation launch");
 }
 
 int cardan_profile_begin(int32_t max_calls) {
