@@ -754,6 +754,12 @@ int check_ffn_call(const cardan_ffn_shape* s, int32_t N, const int32_t* offsets,
   A->Wg = gated ? w->W_gate : nullptr;
   A->Wu = w->W_up;
   A->Wd = w->W_down;
+  // workspace: dg (or h), du, partial sums
+  const size_t half = align256((size_t)N * s->I * 2);
+  uint8_t* base = static_cast<uint8_t*>(const_cast<void*>(ws));
+  A->dg = reinterpret_cast<uint16_t*>(base);
+  A->du = reinterpret_cast<uint16_t*>(base + half);
+  A->part = reinterpret_cast<float*>(base + 2 * half);
   return CARDAN_OK;
 }
 
@@ -766,8 +772,10 @@ int cardan_ffn_workspace_bytes(const cardan_ffn_shape* shape, int32_t N, size_t*
   int rc = check_ffn(shape, N);
   if (rc) return rc;
   if (!out) return fail(CARDAN_ERR_NULL_PTR, "out is NULL");
-  // dg and du of the backward pass; a forward pass that keeps nothing has h there
-  *out = 2 * align256((size_t)N * shape->I * 2);
+  // dg and du of the backward pass (a forward pass that keeps nothing has h
+  // there), and the partial sums of split products
+  *out = 2 * align256((size_t)N * shape->I * 2) +
+         align256(ffn_partial_bytes(N, shape->H, shape->I, shape->act == CARDAN_FFN_SILU_GLU));
   return CARDAN_OK;
 }
 
@@ -791,7 +799,7 @@ int cardan_ffn_forward(const cardan_ffn_shape* shape, int32_t N, const cardan_bf
   A.y = y;
   A.g = gate;
   A.u = up;
-  A.h = hidden ? hidden : static_cast<uint16_t*>(ws);
+  A.h = hidden ? hidden : A.dg;
   const hipError_t e = launch_ffn_forward ? launch_ffn_forward(A, stream) : hipErrorInvalidDeviceFunction;
   return e == hipSuccess ? CARDAN_OK : hip_fail(e, "ffn forward launch");
 }
@@ -823,8 +831,6 @@ int cardan_ffn_backward(const cardan_ffn_shape* shape, int32_t N, const cardan_b
   A.g = const_cast<float*>(gate);
   A.u = const_cast<float*>(up);
   A.h = const_cast<uint16_t*>(hidden);
-  A.dg = static_cast<uint16_t*>(ws);
-  A.du = reinterpret_cast<uint16_t*>(static_cast<uint8_t*>(ws) + align256((size_t)N * shape->I * 2));
   A.dx = dx;
   A.dWg = dW_gate;
   A.dWu = dW_up;

@@ -7,6 +7,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "cardan_ffn_plan.h"
+
 namespace cardan {
 
 // One call of the feed-forward block. Rows n of group e are off[e] <= n <
@@ -22,6 +24,7 @@ struct FfnArgs {
   uint16_t *dg, *du;             // [N][I] gradients of the projections (workspace)
   uint16_t *y, *dx;              // [N][H]
   uint16_t *dWg, *dWu, *dWd;     // as the weights
+  float* part;                   // partial sums of split products (ffn_partial_bytes)
 };
 
 // One call of the distillation loss over the rows of [N][ld] logits.

@@ -8,6 +8,8 @@
 // Every product runs on v_mfma_f32_16x16x32_bf16 with float32 accumulators.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "cardan_ffn.h"
 
 namespace cardan {
@@ -16,24 +18,34 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef __amdgpu_buffer_rsrc_t rsrc_t;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 #define LDS __attribute__((address_space(3)))
 
 constexpr uint32_t kOob = 0x80000000u;     // an offset past every resource
+constexpr size_t kLdsBytes = 160 * 1024;   // of a CU
 constexpr uint32_t kSpan = 0x7fffff00u;    // largest resource
 
-// The products of the block. "rows" are the rows of a group (tokens).
-enum Kind {
-  K_UP = 0,    // [rows, H] x [H, I] (gate and up): activation -> h, and g, u where kept
-  K_DOWN = 1,  // [rows, I] x [I, H] -> y
-  K_DH = 2,    // [rows, H] x Wd^T -> dh, turned into dg, du
-  K_DX = 3,    // dg Wg^T + du Wu^T -> dx
-  K_DW = 4     // x^T dg, x^T du, h^T dy: the sum runs over the group's rows
+struct TileGrid {
+  int32_t col_tiles;  // tiles along the output's columns
+  int32_t row_tiles;  // along its rows (weight gradients; others count their groups' rows)
+  int32_t split;      // parts of the sum
 };
 
-__device__ __forceinline__ rsrc_t make_rsrc(const void* base, int64_t bytes) {
+__device__ __forceinline__ u32x4 make_rsrc(const void* base, int64_t bytes) {
   const uint32_t n = bytes <= 0 ? 0u : bytes > (int64_t)kSpan ? kSpan : (uint32_t)bytes;
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0, (int)n, 0x00020000);
+  const uint64_t b = reinterpret_cast<uintptr_t>(base);
+  return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)b),
+               (uint32_t)__builtin_amdgcn_readfirstlane((int)(b >> 32)) & 0xffffu,
+               (uint32_t)__builtin_amdgcn_readfirstlane((int)n), 0x00020000u};
+}
+
+// 64 lanes x 16 bytes from the resource at `voff` to 1024 bytes of LDS at
+// `lds`. Written as asm because the compiler, which cannot tell the stages of
+// LDS apart, waits for every such load before the next transposing read; the
+// wait that is needed is wait_loads(). It has no output register. (M0 holds
+// the LDS address and must be a wait state old.)
+__device__ __forceinline__ void load_to_lds(u32x4 rs, uint32_t lds, uint32_t voff) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(rs));
 }
 
 // float32 -> bf16, nearest even (NaN stays NaN)
@@ -59,38 +71,64 @@ __device__ __forceinline__ void group_rows(const FfnArgs& A, int e, int& lo, int
   hi = clampi(A.off[e + 1], lo, A.N);
 }
 
-// Group and first row of row tile t, tiles of BM rows counted group by group.
-template <int BM>
-__device__ __forceinline__ bool locate(const FfnArgs& A, int t, int& e, int& row, int& end) {
+// The groups' row tiles, counted group by group: cum[e] tiles up to and with
+// group e, and each group's rows. Built in LDS by the first wave; returns the
+// number of tiles.
+__device__ __forceinline__ int count_tiles(const FfnArgs& A, int BM, int* cum) {
+  if (!A.off) return (A.N + BM - 1) / BM;
+  if (threadIdx.x < 64) {
+    const int lane = threadIdx.x;
+    int before = 0, past = 0;
+    for (int e0 = 0; e0 < A.E; e0 += 64) {
+      int lo = 0, hi = 0;
+      if (e0 + lane < A.E) group_rows(A, e0 + lane, lo, hi);
+      // a group begins where those before it have ended, whatever the offsets
+      int top = hi;
+      for (int s = 1; s < 64; s <<= 1) {
+        const int v = __shfl_up(top, s);
+        top = lane >= s && v > top ? v : top;
+      }
+      const int ended = __shfl_up(top, 1);
+      if (lane > 0 && ended > lo) lo = ended;
+      if (past > lo) lo = past;
+      if (lo > hi) hi = lo;
+      past = max(past, __builtin_amdgcn_readlane(top, 63));
+      int c = (hi - lo + BM - 1) / BM;
+      for (int s = 1; s < 64; s <<= 1) {
+        const int v = __shfl_up(c, s);
+        c += lane >= s ? v : 0;
+      }
+      c += before;
+      if (e0 + lane < A.E) {
+        cum[e0 + lane] = c;
+        cum[A.E + 2 * (e0 + lane)] = lo;
+        cum[A.E + 2 * (e0 + lane) + 1] = hi;
+      }
+      before = __builtin_amdgcn_readlane(c, 63);
+    }
+  }
+  __syncthreads();
+  return __builtin_amdgcn_readfirstlane(cum[A.E - 1]);
+}
+
+// Group, first row and end of rows of row tile t (0 <= t < count_tiles()).
+__device__ __forceinline__ void locate(const FfnArgs& A, int BM, const int* cum, int t, int& e, int& row, int& end) {
   if (!A.off) {
     e = 0;
     row = t * BM;
     end = A.N;
-    return row < A.N;
+    return;
   }
   const int lane = threadIdx.x & 63;
-  int before = 0;
-  for (int e0 = 0; e0 < A.E; e0 += 64) {
-    int lo = 0, hi = 0;
-    if (e0 + lane < A.E) group_rows(A, e0 + lane, lo, hi);
-    const int tiles = (hi - lo + BM - 1) / BM;
-    int cum = tiles;
-    for (int s = 1; s < 64; s <<= 1) {
-      const int v = __shfl_up(cum, s);
-      cum += lane >= s ? v : 0;
-    }
-    const unsigned long long past = __ballot(before + cum > t);
-    if (past) {
-      const int src = __ffsll((long long)past) - 1;
-      e = e0 + src;
-      const int first = __builtin_amdgcn_readlane(lo, src);
-      end = __builtin_amdgcn_readlane(hi, src);
-      row = first + (t - before - (__builtin_amdgcn_readlane(cum, src) - __builtin_amdgcn_readlane(tiles, src))) * BM;
-      return true;
-    }
-    before += __builtin_amdgcn_readlane(cum, 63);
+  for (int e0 = 0;; e0 += 64) {
+    const unsigned long long past = __ballot(e0 + lane < A.E && cum[e0 + lane] > t);
+    if (past == 0 && e0 + 64 < A.E) continue;
+    e = e0 + (past ? __ffsll((long long)past) - 1 : 0);
+    break;
   }
-  return false;
+  const int before = e ? __builtin_amdgcn_readfirstlane(cum[e - 1]) : 0;
+  row = __builtin_amdgcn_readfirstlane(cum[A.E + 2 * e]) + (t - before) * BM;
+  end = __builtin_amdgcn_readfirstlane(cum[A.E + 2 * e + 1]);
 }
 
 // One operand of a tile product: R rows (of the output's row or column axis)
@@ -102,13 +140,19 @@ __device__ __forceinline__ bool locate(const FfnArgs& A, int t, int& e, int& row
 // of row r at place c ^ (r & 7): the 16 rows of an operand read land in
 // different banks.
 // TR = true: memory has the sum down its columns. LDS [64][R], 32-byte pair p
-// of row k at place p ^ (k & 7): a transposing read takes four rows of a pair.
+// of row k at place p ^ swz(k). A transposing read takes one pair of four rows
+// in each 16 lanes, and 32 lanes are served at a time: rows k..k+3 and
+// k+8..k+11, which the places spread over the 64 banks.
 template <int R, bool TR, int NW>
 struct Operand {
   static constexpr int kLoads = R / 8 / NW;     // loads of one wave per stage
   static constexpr int kRow = TR ? R * 2 : 128;  // bytes of an LDS row
   static constexpr int kPairs = TR ? (R / 16 < 8 ? R / 16 : 8) : 1;
   static_assert(R % (8 * NW) == 0, "whole loads");
+
+  static __device__ __forceinline__ int swz(int k) {
+    return kPairs == 8 ? (k & 3) | (k >> 1 & 4) : kPairs == 4 ? (k >> 1 & 1) | (k >> 2 & 2) : k >> 3 & 1;
+  }
 
   uint32_t voff[kLoads];
   bool tail;  // this lane's chunk lies past the last step's end (TR = false)
@@ -121,7 +165,7 @@ struct Operand {
 #pragma unroll
       for (int j = 0; j < kLoads; ++j) {
         const int kk = (j * NW + wave) * per + k;
-        const int src = (((c >> 1) ^ (kk & (kPairs - 1))) << 1) | (c & 1);
+        const int src = (((c >> 1) ^ swz(kk)) << 1) | (c & 1);
         voff[j] = (uint32_t)(kk * ld * 2 + src * 16);
       }
       tail = false;
@@ -133,20 +177,19 @@ struct Operand {
     }
   }
 
-  __device__ __forceinline__ void issue(rsrc_t rs, char* lds, int wave, bool last) const {
+  __device__ __forceinline__ void issue(u32x4 rs, uint32_t lds, int wave, bool last) const {
     const uint32_t drop = last && tail ? kOob : 0u;
 #pragma unroll
     for (int j = 0; j < kLoads; ++j)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (LDS void*)(lds + (j * NW + wave) * 1024), 16,
-                                               (int)(voff[j] | drop), 0, 0, 0);
+      load_to_lds(rs, lds + (j * NW + wave) * 1024, voff[j] | drop);
   }
 
   // byte of the first operand read of the 16-row block that starts at row r0
   static __device__ __forceinline__ int base(int r0) {
     const int l = threadIdx.x & 63;
     if constexpr (TR) {
-      const int a = (l & 15) >> 2, k = (l >> 4) * 8 + a;
-      return k * kRow + ((r0 >> 4) ^ (a & (kPairs - 1))) * 32 + (l & 3) * 8;
+      const int k = (l >> 4) * 8 + ((l & 15) >> 2);
+      return k * kRow + ((r0 >> 4) ^ swz(k)) * 32 + (l & 3) * 8;
     } else {
       return (r0 + (l & 15)) * 128 + ((l >> 4) ^ (l & 7)) * 16;
     }
@@ -155,9 +198,8 @@ struct Operand {
   static __device__ __forceinline__ bf16x8 read(const char* lds, int b, int f, int kk) {
     if constexpr (TR) {
       const int at = (b ^ (f << 5)) + kk * 32 * kRow;
-      const int at4 = (kPairs > 4 ? at ^ 128 : at) + 4 * kRow;
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS s16x4*)(lds + at));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS s16x4*)(lds + at4));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS s16x4*)(lds + at + 4 * kRow));
       return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
       return *(const bf16x8*)(lds + ((b ^ (kk << 6)) + f * 2048));
@@ -168,256 +210,457 @@ struct Operand {
 // s(g) = 1 / (1 + e^-g); e^-g overflows to infinity for g < -88 and gives 0
 __device__ __forceinline__ float sigmoid(float g) { return 1.0f / (1.0f + __expf(-g)); }
 
-// Output tile [BM x BN] of one product. WM x WN waves; a wave holds
+// Waits until at most N loads of this wave are in flight and all of its LDS
+// reads have returned, then for the workgroup's other waves.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(N < 64, "vmcnt");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x0070);  // vmcnt(N), lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// Scheduling order of a block: READS LDS reads spread evenly over PRODS products.
+template <int I, int READS, int PRODS>
+__device__ __forceinline__ void weave() {
+  if constexpr (I < READS) {
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x008, PRODS * (I + 1) / READS - PRODS * I / READS, 0);
+    weave<I + 1, READS, PRODS>();
+  }
+}
+
+// Activation of four projections; g is not used by up-only experts.
+template <bool RELU2>
+__device__ __forceinline__ f32x4 activate(f32x4 g, f32x4 u) {
+  f32x4 h;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    if constexpr (RELU2) {
+      const float p = fmaxf(u[q], 0.f);
+      h[q] = p * p;
+    } else {
+      h[q] = g[q] * sigmoid(g[q]) * u[q];
+    }
+  }
+  return h;
+}
+
+// Gradients of four projections from that of h.
+template <bool RELU2>
+__device__ __forceinline__ void activate_grad(f32x4 dh, f32x4 g, f32x4 u, f32x4& dg, f32x4& du) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    if constexpr (RELU2) {
+      du[q] = dh[q] * 2.f * fmaxf(u[q], 0.f);
+    } else {
+      const float s = sigmoid(g[q]);
+      dg[q] = dh[q] * u[q] * s * (1.f + g[q] * (1.f - s));
+      du[q] = dh[q] * g[q] * s;
+    }
+  }
+}
+
+// Stores the bf16 values of two neighbouring 16x16 blocks, four of a lane in
+// each, as 16 bytes a lane: the odd 16-lane groups' part of the first block
+// changes places with the even groups' part of the second, which leaves every
+// lane eight consecutive columns of one block. p: the lane's row at the first
+// block's first column.
+__device__ __forceinline__ void store_pair(uint16_t* p, uint2 a, uint2 b) {
+  const int grp = (threadIdx.x & 63) >> 4;
+  const auto x = __builtin_amdgcn_permlane16_swap(a.x, b.x, false, false);
+  const auto y = __builtin_amdgcn_permlane16_swap(a.y, b.y, false, false);
+  *(uint4*)(p + (grp & 1) * 16 + (grp >> 1) * 8) = make_uint4(x[0], y[0], x[1], y[1]);
+}
+
+// Output tiles [BM x BN] of one product. WM x WN waves; a wave holds
 // (BM / WM) x (BN / WN) outputs as 16x16 blocks whose columns are the output's
 // rows, so a lane has four consecutive columns of one row.
-template <int KIND, bool RELU2, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN, 2) void k_ffn(const FfnArgs A) {
+//
+// Workgroups take units (part of the sum, tile) in turn. Loads run NS steps of
+// 64 ahead of the products, through the end of a unit into the next one, so
+// only a workgroup's first unit waits for memory and an epilogue's stores and
+// reads overlap the next unit's loads. A unit that is one of several parts
+// writes its float32 partial output, which k_ffn_join adds in order.
+template <int KIND, bool RELU2, int BM, int BN, int WM, int WN, int NS>
+__global__ __launch_bounds__(64 * WM * WN, 2) void k_ffn(const FfnArgs A, const TileGrid G) {
   constexpr int NW = WM * WN;
-  constexpr bool kAT = KIND == K_DW, kBT = KIND == K_UP || KIND == K_DOWN || KIND == K_DW;
+  constexpr bool kDW = KIND == K_DWI || KIND == K_DWD;
+  constexpr bool kAT = kDW, kBT = kDW || KIND == K_UP || KIND == K_DOWN;
   constexpr bool kDual = KIND == K_UP && !RELU2;  // gate and up columns side by side in the tile
   constexpr int kPh = KIND == K_DX && !RELU2 ? 2 : 1;
+  constexpr int kMats = KIND == K_DWI && !RELU2 ? 2 : 1;  // dWg, dWu
   constexpr int BC = kDual ? BN / 2 : BN;         // output columns of a tile
   constexpr int MF = BM / WM / 16, NF = BN / WN / 16;
   constexpr int kStage = (BM + BN) * 128;
   typedef Operand<BM, kAT, NW> OpA;
   typedef Operand<BC, kBT, NW> OpB;
   extern __shared__ __align__(1024) char smem[];
+  int* cum = reinterpret_cast<int*>(smem + NS * kStage);
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int wm = wave / WN, wn = wave % WN;
   const int H = A.H, I = A.I;
+  const int nout = KIND == K_UP || KIND == K_DH || KIND == K_DWI ? I : H;
+  const int mout = KIND == K_DWI ? H : I;             // rows of a weight gradient
+  const int ksum = KIND == K_UP || KIND == K_DH ? H : I;  // (row products)
+  const int lda = kDW ? mout : ksum, ldb = kBT ? nout : ksum;
+  const int64_t astep = kAT ? (int64_t)64 * lda * 2 : 128, bstep = kBT ? (int64_t)64 * ldb * 2 : 128;
 
-  // workgroups go round robin over the 8 XCDs: give each XCD a run of tiles
-  const int total = gridDim.x;
-  int id = blockIdx.x;
-  {
-    const int per = total >> 3, whole = per << 3;
-    if (id < whole) id = (id & 7) * per + (id >> 3);
-  }
+  // units of this workgroup: workgroups go round robin over the 8 XCDs; an XCD
+  // takes runs of neighbouring tiles, which share operands in its L2
+  const int tm = kDW ? G.row_tiles * kMats * A.E : count_tiles(A, BM, cum);
+  const int tiles = tm * G.col_tiles, units = tiles * G.split;
+  const int per = gridDim.x >> 3;
+  const int stride = gridDim.x, first = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
 
-  int e, row = 0, end = 0, n0, m0 = 0;
-  const uint16_t *a0, *a1 = nullptr, *b0, *b1 = nullptr;
-  uint16_t* out = nullptr;
-  int lda, ldb, nout, ksum, mout = 0;
-  int64_t abytes, bbytes;  // from a0 / b0 to the end of the operand
-  if constexpr (KIND == K_DW) {
-    // tiles of dWg, dWu ([H][I]) and dWd ([I][H]) of one group after another
-    const int th = (H + BM - 1) / BM, ti = (I + BN - 1) / BN;
-    const int ti2 = (I + BM - 1) / BM, th2 = (H + BN - 1) / BN;
-    const int n_in = A.dWu ? th * ti * (RELU2 ? 1 : 2) : 0, n_dn = A.dWd ? ti2 * th2 : 0;
-    e = id / (n_in + n_dn);
-    int t = id - e * (n_in + n_dn);
-    int lo, hi;
-    group_rows(A, e, lo, hi);
-    lo = __builtin_amdgcn_readfirstlane(lo);
-    hi = __builtin_amdgcn_readfirstlane(hi);
-    ksum = hi - lo;
-    const bool down = t >= n_in;
-    bool gate = false;
-    if (down) t -= n_in;
-    else if (!RELU2) {
-      gate = t & 1;
-      t >>= 1;
+  struct Unit {  // where a unit's operands are, and its output
+    const char *a, *b, *a1, *b1;
+    int64_t ab, bb;       // bytes from there to the operand's end
+    int k, kend, kt1;     // next step, end, and steps of a phase
+    int e, row, end, n0, mat, part;
+  };
+  auto setup = [&](int u, Unit& U) {
+    U.part = G.split > 1 ? u / tiles : 0;
+    const int id = u - U.part * tiles;
+    if constexpr (kDW) {
+      // tiles of one group's gradients after another; gate and up in turn
+      const int of = G.row_tiles * G.col_tiles * kMats;
+      U.e = id / of;
+      int t = id - U.e * of;
+      U.mat = kMats == 2 ? t & 1 : 1;
+      t /= kMats;
+      int lo, hi;
+      group_rows(A, U.e, lo, hi);
+      lo = __builtin_amdgcn_readfirstlane(lo);
+      hi = __builtin_amdgcn_readfirstlane(hi);
+      const int rows = hi - lo;
+      U.row = t / G.col_tiles * BM;
+      U.n0 = t % G.col_tiles * BN;
+      U.end = mout;
+      U.a = (const char*)((KIND == K_DWD ? A.h : A.x) + (int64_t)lo * lda + U.row);
+      U.b = (const char*)((KIND == K_DWD ? A.dy : U.mat ? A.du : A.dg) + (int64_t)lo * ldb + U.n0);
+      U.ab = ((int64_t)rows * lda - U.row) * 2;
+      U.bb = ((int64_t)rows * ldb - U.n0) * 2;
+      U.kt1 = rows > 0 ? (rows + 63) >> 6 : 1;  // a group without rows: one step of zeros
+      U.k = 0;
+      U.kend = U.kt1;
+    } else {
+      // 8 row tiles by all column tiles at a time
+      const int band = id / (8 * G.col_tiles), in = id - band * 8 * G.col_tiles;
+      const int rows8 = tm - band * 8 < 8 ? tm - band * 8 : 8;
+      U.n0 = in / rows8 * BC;
+      locate(A, BM, cum, band * 8 + in % rows8, U.e, U.row, U.end);
+      U.ab = (int64_t)(U.end - U.row) * lda * 2;
+      const int64_t ar = (int64_t)U.row * lda;
+      const int64_t w = (int64_t)U.e * H * I + (kBT ? U.n0 : (int64_t)U.n0 * ldb);
+      U.a = (const char*)((KIND == K_UP ? A.x : KIND == K_DOWN ? A.h : KIND == K_DH ? A.dy : kPh == 2 ? A.dg : A.du) + ar);
+      U.b = (const char*)((KIND == K_UP || KIND == K_DX ? (RELU2 ? A.Wu : A.Wg) : A.Wd) + w);
+      U.bb = kBT ? ((int64_t)ksum * ldb - U.n0) * 2 : (int64_t)(nout - U.n0) * ldb * 2;
+      if constexpr (kPh == 2) U.a1 = (const char*)(A.du + ar);
+      if constexpr (kPh == 2 || kDual) U.b1 = (const char*)(A.Wu + w);
+      U.kt1 = (ksum + 63) >> 6;
+      const int64_t all = (int64_t)U.kt1 * kPh;
+      U.k = (int)(all * U.part / G.split);
+      U.kend = (int)(all * (U.part + 1) / G.split);
     }
-    mout = down ? I : H;
-    nout = down ? H : I;
-    const int tn = down ? th2 : ti;
-    m0 = t / tn * BM;
-    n0 = t % tn * BN;
-    lda = mout;
-    ldb = nout;
-    a0 = (down ? A.h : A.x) + (int64_t)lo * lda + m0;
-    b0 = (down ? A.dy : gate ? A.dg : A.du) + (int64_t)lo * ldb + n0;
-    abytes = ((int64_t)ksum * lda - m0) * 2;
-    bbytes = ((int64_t)ksum * ldb - n0) * 2;
-    out = (down ? A.dWd : gate ? A.dWg : A.dWu) + (int64_t)e * H * I;
-  } else {
-    nout = KIND == K_UP || KIND == K_DH ? I : H;
-    ksum = KIND == K_UP || KIND == K_DH ? H : I;
-    const int tn = (nout + BC - 1) / BC, tm = total / tn;
-    // 8 row tiles by all column tiles at a time: a run of neighbours shares
-    // its operands in the XCD's L2
-    const int band = id / (8 * tn), in = id - band * 8 * tn;
-    const int rows8 = tm - band * 8 < 8 ? tm - band * 8 : 8;
-    const int t = band * 8 + in % rows8;
-    n0 = in / rows8 * BC;
-    if (!locate<BM>(A, t, e, row, end)) return;
-    row = __builtin_amdgcn_readfirstlane(row);
-    lda = ksum;
-    abytes = (int64_t)(end - row) * lda * 2;
-    const int64_t w = (int64_t)e * H * I, ar = (int64_t)row * lda;
-    a0 = (KIND == K_UP ? A.x : KIND == K_DOWN ? A.h : KIND == K_DH ? A.dy : kPh == 2 ? A.dg : A.du) + ar;
-    const uint16_t* wt = KIND == K_UP || KIND == K_DX ? (RELU2 ? A.Wu : A.Wg) : A.Wd;
-    if constexpr (kBT) {  // weights [ksum][nout]
-      ldb = nout;
-      b0 = wt + w + n0;
-      bbytes = ((int64_t)ksum * ldb - n0) * 2;
-    } else {              // weights [nout][ksum]
-      ldb = ksum;
-      b0 = wt + w + (int64_t)n0 * ldb;
-      bbytes = (int64_t)(nout - n0) * ldb * 2;
-    }
-    if constexpr (kDual) b1 = A.Wu + (b0 - A.Wg);
-    if constexpr (kPh == 2) {
-      a1 = A.du + ar;
-      b1 = A.Wu + (b0 - A.Wg);
-    }
-  }
+  };
 
   OpA opa;
   OpB opb;
-  opa.init(wave, lda, ksum);
-  opb.init(wave, ldb, ksum);
-  const int wm = wave / WN, wn = wave % WN;
+  opa.init(wave, lda, kDW ? 0 : ksum);
+  opb.init(wave, ldb, kDW ? 0 : ksum);
   const int abase = OpA::base(wm * (BM / WM));
   const int bbase = OpB::base(wn * (BC / WN));
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS char*)smem;
 
-  f32x4 acc[MF][NF];
-#pragma unroll
-  for (int i = 0; i < MF; ++i)
-#pragma unroll
-    for (int j = 0; j < NF; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-  const int kt1 = (ksum + 63) >> 6, kts = kt1 * kPh;
-  const int64_t astep = kAT ? (int64_t)64 * lda * 2 : 128, bstep = kBT ? (int64_t)64 * ldb * 2 : 128;
-  auto issue = [&](int kt) {
-    char* buf = smem + (kt & 1) * kStage;
-    const int ph = kPh == 2 && kt >= kt1, k = kt - (ph ? kt1 : 0);
-    const bool last = k == kt1 - 1;
+  // the loads: one step of the unit P into a stage, then on to the next step.
+  // Past the last unit empty resources are loaded, so that every wave always
+  // has the same number of loads in flight.
+  int pu = first;
+  Unit P;
+  if (pu < units) setup(pu, P);
+  auto issue = [&](int stage) {
+    const bool some = pu < units;
+    const uint32_t buf = lds0 + stage * kStage;
+    const bool ph = kPh == 2 && P.k >= P.kt1;
+    const int k = P.k - (ph ? P.kt1 : 0);
+    const bool last = k == P.kt1 - 1;
     const int64_t ao = k * astep, bo = k * bstep;
-    opa.issue(make_rsrc((const char*)(ph ? a1 : a0) + ao, abytes - ao), buf, wave, last);
-    opb.issue(make_rsrc((const char*)(ph ? b1 : b0) + bo, bbytes - bo), buf + BM * 128, wave, last);
-    if constexpr (kDual)
-      opb.issue(make_rsrc((const char*)b1 + bo, bbytes - bo), buf + (BM + BC) * 128, wave, last);
+    opa.issue(make_rsrc((ph ? P.a1 : P.a) + ao, some ? P.ab - ao : 0), buf, wave, last);
+    opb.issue(make_rsrc((ph ? P.b1 : P.b) + bo, some ? P.bb - bo : 0), buf + BM * 128, wave, last);
+    if constexpr (kDual) opb.issue(make_rsrc(P.b1 + bo, some ? P.bb - bo : 0), buf + (BM + BC) * 128, wave, last);
+    if (some && ++P.k == P.kend) {
+      pu += stride;
+      if (pu < units) setup(pu, P);
+    }
   };
-  if (kts > 0) issue(0);
-  for (int kt = 0; kt < kts; ++kt) {
-    __syncthreads();  // stage kt has landed, and no wave reads the other stage any more
-    if (kt + 1 < kts) issue(kt + 1);
-    const char* la = smem + (kt & 1) * kStage;
+  constexpr int kLoads = OpA::kLoads + OpB::kLoads * (kDual ? 2 : 1);
+
+  bf16x8 a0f[MF], b0f[NF], a1f[MF], b1f[NF];  // operands of the two halves of a step
+  auto read = [&](int st, int kk, bf16x8(&a)[MF], bf16x8(&b)[NF]) {
+    const char* la = smem + st * kStage;
     const char* lb = la + BM * 128;
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      bf16x8 a[MF], b[NF];
-#pragma unroll
-      for (int j = 0; j < NF; ++j) {
-        if constexpr (kDual)
-          b[j] = OpB::read(lb + (j < NF / 2 ? 0 : BC * 128), bbase, j % (NF / 2), kk);
-        else
-          b[j] = OpB::read(lb, bbase, j, kk);
-      }
-#pragma unroll
-      for (int i = 0; i < MF; ++i) a[i] = OpA::read(la, abase, i, kk);
-#pragma unroll
-      for (int i = 0; i < MF; ++i)
-#pragma unroll
-        for (int j = 0; j < NF; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], a[i], acc[i][j], 0, 0, 0);
+    for (int j = 0; j < NF; ++j) {
+      if constexpr (kDual)
+        b[j] = OpB::read(lb + (j < NF / 2 ? 0 : BC * 128), bbase, j % (NF / 2), kk);
+      else
+        b[j] = OpB::read(lb, bbase, j, kk);
     }
-  }
-
-  // epilogue: lane -> output row (lane & 15) of a block, columns (lane >> 4) * 4 + 0..3
-  const int rmax = KIND == K_DW ? mout : end;
-  const int r0 = (KIND == K_DW ? m0 : row) + wm * (BM / WM) + (lane & 15);
-  const int c0 = n0 + wn * (BC / WN) + (lane >> 4) * 4;
 #pragma unroll
-  for (int i = 0; i < MF; ++i) {
-    const int r = r0 + i * 16;
-    if (r >= rmax) continue;
-    const int64_t rb = (int64_t)r * nout;
-    if constexpr (KIND == K_UP) {
-      constexpr int NC = kDual ? NF / 2 : NF;
+    for (int i = 0; i < MF; ++i) a[i] = OpA::read(la, abase, i, kk);
+  };
+  f32x4 acc[MF][NF];
+  auto multiply = [&](bf16x8(&a)[MF], bf16x8(&b)[NF]) {
+#pragma unroll
+    for (int i = 0; i < MF; ++i)
+#pragma unroll
+      for (int j = 0; j < NF; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], a[i], acc[i][j], 0, 0, 0);
+  };
+  // order of a half: operand reads of the next half between the products
+  constexpr int kReads = MF * (kAT ? 2 : 1) + NF * (kBT ? 2 : 1), kProds = MF * NF;
+
+  // lane -> output row (lane & 15) of a block, columns (lane >> 4) * 4 + 0..3
+  auto epilogue = [&](const Unit& C, int wrow, int wcol) {
+    constexpr int NC = kDual ? NF / 2 : NF;  // 16-column blocks of the output
+    const int r0 = wrow + (lane & 15), q4 = (lane >> 4) * 4;
+    if (!kDW && G.split > 1) {
+      const int64_t plane = (int64_t)A.N * nout;
+      float* part = A.part + C.part * plane * (kDual ? 2 : 1);
+#pragma unroll
+      for (int i = 0; i < MF; ++i) {
+        const int r = r0 + i * 16;
+        if (r >= C.end) continue;
+        float* p = part + (int64_t)r * nout + q4;
+#pragma unroll
+        for (int j = 0; j < NC; ++j) {
+          const int c = wcol + j * 16;
+          if (c >= nout) continue;
+          *(f32x4*)(p + c) = acc[i][j];
+          if constexpr (kDual) *(f32x4*)(p + c + plane) = acc[i][j + NC];
+        }
+      }
+      return;
+    }
+    // the projections that a gradient block needs are read one block row ahead
+    constexpr int kIn = KIND == K_DH ? NC : 1, kGu = KIND == K_DH ? (RELU2 ? 1 : 2) : 1;
+    f32x4 in[2][kIn][kGu];
+    auto fetch = [&](int i) {
+      if constexpr (KIND == K_DH) {
+        const int r = r0 + i * 16 < C.end ? r0 + i * 16 : C.end - 1;
+        const int64_t rb = (int64_t)r * nout + q4;
+#pragma unroll
+        for (int j = 0; j < NC; ++j) {
+          const int c = wcol + j * 16 < nout ? wcol + j * 16 : wcol;
+          in[i & 1][j][0] = *(const f32x4*)(A.u + rb + c);
+          if constexpr (!RELU2) in[i & 1][j][1] = *(const f32x4*)(A.g + rb + c);
+        }
+      }
+    };
+    uint16_t* o0 = KIND == K_UP ? A.h : KIND == K_DH ? A.du : KIND == K_DOWN ? A.y : KIND == K_DX ? A.dx
+                 : (KIND == K_DWD ? A.dWd : C.mat ? A.dWu : A.dWg) + (int64_t)C.e * H * I;
+    fetch(0);
+#pragma unroll
+    for (int i = 0; i < MF; ++i) {
+      if (i + 1 < MF) fetch(i + 1);
+      const int r = r0 + i * 16;
+      if (r >= C.end) continue;
+      const int64_t rb = (int64_t)r * nout;
+      uint2 v0[NC], v1[NC];
 #pragma unroll
       for (int j = 0; j < NC; ++j) {
-        const int c = c0 + j * 16;
-        if (c >= nout) continue;
-        f32x4 h;
-        const f32x4 u = acc[i][kDual ? j + NC : j];
-        if constexpr (RELU2) {
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const float p = fmaxf(u[q], 0.f);
-            h[q] = p * p;
+        const int c = wcol + j * 16;
+        if constexpr (KIND == K_UP) {
+          const f32x4 g = acc[i][j], u = acc[i][kDual ? j + NC : j];
+          if (c < nout) {
+            if constexpr (!RELU2)
+              if (A.g) *(f32x4*)(A.g + rb + c + q4) = g;
+            if (A.u) *(f32x4*)(A.u + rb + c + q4) = u;
           }
+          v0[j] = pack4(activate<RELU2>(g, u));
+        } else if constexpr (KIND == K_DH) {
+          f32x4 dg, du;
+          activate_grad<RELU2>(acc[i][j], in[i & 1][j][kGu - 1], in[i & 1][j][0], dg, du);
+          v0[j] = pack4(du);
+          if constexpr (!RELU2) v1[j] = pack4(dg);
         } else {
-          const f32x4 g = acc[i][j];
-#pragma unroll
-          for (int q = 0; q < 4; ++q) h[q] = g[q] * sigmoid(g[q]) * u[q];
-          if (A.g) *(f32x4*)(A.g + rb + c) = g;
+          v0[j] = pack4(acc[i][j]);
         }
-        if (A.u) *(f32x4*)(A.u + rb + c) = u;
-        *(uint2*)(A.h + rb + c) = pack4(h);
       }
-    } else if constexpr (KIND == K_DH) {
+      if constexpr (NC % 2 == 0) {
 #pragma unroll
-      for (int j = 0; j < NF; ++j) {
-        const int c = c0 + j * 16;
-        if (c >= nout) continue;
-        const f32x4 dh = acc[i][j], u = *(const f32x4*)(A.u + rb + c);
-        f32x4 du;
-        if constexpr (RELU2) {
-#pragma unroll
-          for (int q = 0; q < 4; ++q) du[q] = dh[q] * 2.f * fmaxf(u[q], 0.f);
-        } else {
-          const f32x4 g = *(const f32x4*)(A.g + rb + c);
-          f32x4 dg;
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const float s = sigmoid(g[q]);
-            dg[q] = dh[q] * u[q] * s * (1.f + g[q] * (1.f - s));
-            du[q] = dh[q] * g[q] * s;
-          }
-          *(uint2*)(A.dg + rb + c) = pack4(dg);
+        for (int j = 0; j < NC; j += 2) {
+          const int c = wcol + j * 16;
+          if (c >= nout) continue;
+          store_pair(o0 + rb + c, v0[j], v0[j + 1]);
+          if constexpr (KIND == K_DH && !RELU2) store_pair(A.dg + rb + c, v1[j], v1[j + 1]);
         }
-        *(uint2*)(A.du + rb + c) = pack4(du);
-      }
-    } else {
-      uint16_t* o = KIND == K_DW ? out : KIND == K_DOWN ? A.y : A.dx;
+      } else {
 #pragma unroll
-      for (int j = 0; j < NF; ++j) {
-        const int c = c0 + j * 16;
-        if (c < nout) *(uint2*)(o + rb + c) = pack4(acc[i][j]);
+        for (int j = 0; j < NC; ++j) {
+          const int c = wcol + j * 16;
+          if (c >= nout) continue;
+          *(uint2*)(o0 + rb + c + q4) = v0[j];
+          if constexpr (KIND == K_DH && !RELU2) *(uint2*)(A.dg + rb + c + q4) = v1[j];
+        }
       }
     }
+  };
+
+  if (first >= units) return;
+#pragma unroll
+  for (int s = 0; s < NS; ++s) issue(s);
+  wait_loads<(NS - 1) * kLoads>();
+  read(0, 0, a0f, b0f);
+  int stage = 0;
+  for (int u = first; u < units; u += stride) {
+    Unit C;
+    setup(u, C);
+#pragma unroll
+    for (int i = 0; i < MF; ++i)
+#pragma unroll
+      for (int j = 0; j < NF; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int wrow = C.row + wm * (BM / WM), wcol = C.n0 + wn * (BC / WN);
+    if (wrow < C.end && wcol < nout) {
+      for (int kt = C.k; kt < C.kend; ++kt) {
+        read(stage, 1, a1f, b1f);
+        multiply(a0f, b0f);
+        weave<0, kReads, kProds>();
+        // the next step has landed, and this step's stage has been read by every wave
+        wait_loads<(NS - 2) * kLoads>();
+        issue(stage);
+        stage = stage == NS - 1 ? 0 : stage + 1;
+        read(stage, 0, a0f, b0f);
+        multiply(a1f, b1f);
+        weave<0, kReads, kProds>();
+      }
+    } else {  // a wave whose outputs lie past the end only loads
+      for (int kt = C.k; kt < C.kend; ++kt) {
+        wait_loads<(NS - 2) * kLoads>();
+        issue(stage);
+        stage = stage == NS - 1 ? 0 : stage + 1;
+      }
+      read(stage, 0, a0f, b0f);
+      continue;
+    }
+
+    epilogue(C, wrow, wcol);
+    read(stage, 0, a0f, b0f);
+  }
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): no load to LDS outlives the workgroup
+}
+
+// Sum of the parts of a split product, in order, and its epilogue.
+template <int KIND, bool RELU2>
+__global__ __launch_bounds__(256) void k_ffn_join(const FfnArgs A, int split) {
+  constexpr bool kDual = KIND == K_UP && !RELU2;
+  const int nout = KIND == K_UP || KIND == K_DH ? A.I : A.H;
+  int lo = 0, hi = A.N, t;
+  if (A.off) {  // rows in no group have no sums
+    group_rows(A, 0, lo, t);
+    group_rows(A, A.E - 1, t, hi);
+  }
+  const int64_t plane = (int64_t)A.N * nout;
+  const int64_t at = (int64_t)lo * nout + ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (at >= (int64_t)hi * nout) return;
+  const float* p = A.part + at;
+  f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
+  for (int s = 0; s < split; ++s) {
+    a += *(const f32x4*)p;
+    if constexpr (kDual) b += *(const f32x4*)(p + plane);
+    p += plane * (kDual ? 2 : 1);
+  }
+  if constexpr (KIND == K_UP) {
+    if constexpr (!RELU2)
+      if (A.g) *(f32x4*)(A.g + at) = a;
+    const f32x4 u = kDual ? b : a;
+    if (A.u) *(f32x4*)(A.u + at) = u;
+    *(uint2*)(A.h + at) = pack4(activate<RELU2>(a, u));
+  } else if constexpr (KIND == K_DH) {
+    f32x4 dg, du;
+    activate_grad<RELU2>(a, RELU2 ? a : *(const f32x4*)(A.g + at), *(const f32x4*)(A.u + at), dg, du);
+    if constexpr (!RELU2) *(uint2*)(A.dg + at) = pack4(dg);
+    *(uint2*)(A.du + at) = pack4(du);
+  } else {
+    *(uint2*)((KIND == K_DOWN ? A.y : A.dx) + at) = pack4(a);
   }
 }
 
-template <int KIND, bool RELU2, int BM, int BN, int WM, int WN>
-hipError_t run(const FfnArgs& A, hipStream_t s) {
-  constexpr bool kDual = KIND == K_UP && !RELU2;
+template <int KIND, bool RELU2, int BM, int BN, int WM, int WN, int NS>
+hipError_t run(const FfnArgs& A, int split, int cus, hipStream_t s) {
+  constexpr bool kDual = KIND == K_UP && !RELU2, kDW = KIND == K_DWI || KIND == K_DWD;
   constexpr int BC = kDual ? BN / 2 : BN;
-  constexpr size_t lds = (size_t)2 * (BM + BN) * 128;
-  int64_t grid;
-  if (KIND == K_DW) {
-    const int64_t th = (A.H + BM - 1) / BM, ti = (A.I + BN - 1) / BN, ti2 = (A.I + BM - 1) / BM, th2 = (A.H + BN - 1) / BN;
-    grid = A.E * ((A.dWu ? th * ti * (RELU2 ? 1 : 2) : 0) + (A.dWd ? ti2 * th2 : 0));
-  } else {
-    const int nout = KIND == K_UP || KIND == K_DH ? A.I : A.H;
-    const int64_t tm = A.off ? A.N / BM + (A.E < A.N ? A.E : A.N) : (A.N + BM - 1) / BM;
-    grid = tm * ((nout + BC - 1) / BC);
+  const int nout = KIND == K_UP || KIND == K_DH || KIND == K_DWI ? A.I : A.H;
+  const int mout = KIND == K_DWI ? A.H : A.I;
+  TileGrid G;
+  G.col_tiles = (nout + BC - 1) / BC;
+  G.row_tiles = kDW ? (mout + BM - 1) / BM : 0;
+  G.split = split;
+  // at most this many tiles (groups end inside tiles); the kernel counts them
+  const int64_t rows = kDW ? (int64_t)G.row_tiles * A.E * (KIND == K_DWI && !RELU2 ? 2 : 1)
+                           : A.off ? A.N / BM + (A.E < A.N ? A.E : A.N) : (A.N + BM - 1) / BM;
+  const int64_t units = rows * G.col_tiles * G.split;
+  if (units == 0) return hipSuccess;
+  if (units > 0x40000000) return hipErrorInvalidValue;
+  const size_t lds = (size_t)NS * (BM + BN) * 128 + (A.off && !kDW ? (size_t)A.E * 12 : 0);
+  const int fit = (int)(kLdsBytes / lds), wave_fit = 8 / (WM * WN);  // workgroups a CU holds at once
+  const int64_t most = (int64_t)cus * (fit < wave_fit ? fit : wave_fit);
+  const int64_t per = (std::min(units, most) + 7) / 8;
+  k_ffn<KIND, RELU2, BM, BN, WM, WN, NS><<<dim3((unsigned)(8 * per)), dim3(64 * WM * WN), lds, s>>>(A, G);
+  hipError_t e = hipGetLastError();
+  if (G.split == 1 || e != hipSuccess) return e;
+  if constexpr (!kDW) {
+    const int64_t vecs = (int64_t)A.N * nout / 4;
+    k_ffn_join<KIND, RELU2><<<dim3((unsigned)((vecs + 255) / 256)), dim3(256), 0, s>>>(A, split);
+    e = hipGetLastError();
   }
-  if (grid == 0) return hipSuccess;
-  if (grid > 0x7fffffff) return hipErrorInvalidValue;
-  k_ffn<KIND, RELU2, BM, BN, WM, WN><<<dim3((unsigned)grid), dim3(64 * WM * WN), lds, s>>>(A);
-  return hipGetLastError();
+  return e;
+}
+
+template <int KIND, bool RELU2>
+hipError_t run_kind(const FfnArgs& A, int cus, hipStream_t s) {
+  const FfnChoice c = choose_ffn(ffn_product((FfnKind)KIND, A.N, A.E, A.H, A.I, !RELU2), cus);
+  switch (c.tile) {
+    case 0: return run<KIND, RELU2, 256, 256, 2, 4, 2>(A, c.split, cus, s);
+    case 1: return run<KIND, RELU2, 128, 256, 2, 4, 3>(A, c.split, cus, s);
+    case 2: return run<KIND, RELU2, 64, 256, 1, 8, 3>(A, c.split, cus, s);
+    case 3: return run<KIND, RELU2, 128, 128, 2, 2, 2>(A, c.split, cus, s);
+    case 4: return run<KIND, RELU2, 64, 128, 1, 4, 3>(A, c.split, cus, s);
+    default: return run<KIND, RELU2, 32, 128, 1, 4, 4>(A, c.split, cus, s);
+  }
 }
 
 template <int KIND>
-hipError_t run_kind(const FfnArgs& A, hipStream_t s) {
-  return A.relu2 ? run<KIND, true, 256, 256, 2, 4>(A, s) : run<KIND, false, 256, 256, 2, 4>(A, s);
+hipError_t run_act(const FfnArgs& A, int cus, hipStream_t s) {
+  return A.relu2 ? run_kind<KIND, true>(A, cus, s) : run_kind<KIND, false>(A, cus, s);
+}
+
+hipError_t device_cus(int* cus) {
+  int dev = 0;
+  const hipError_t e = hipGetDevice(&dev);
+  return e != hipSuccess ? e : hipDeviceGetAttribute(cus, hipDeviceAttributeMultiprocessorCount, dev);
 }
 
 }  // namespace
 
 hipError_t launch_ffn_forward(const FfnArgs& A, hipStream_t s) {
-  hipError_t e = run_kind<K_UP>(A, s);
-  return e != hipSuccess ? e : run_kind<K_DOWN>(A, s);
+  int cus = 0;
+  hipError_t e = device_cus(&cus);
+  if (e == hipSuccess) e = run_act<K_UP>(A, cus, s);
+  if (e == hipSuccess) e = run_act<K_DOWN>(A, cus, s);
+  return e;
 }
 
 hipError_t launch_ffn_backward(const FfnArgs& A, hipStream_t s) {
-  hipError_t e = run_kind<K_DH>(A, s);
-  if (e == hipSuccess && A.dx) e = run_kind<K_DX>(A, s);
-  if (e == hipSuccess && (A.dWu || A.dWd)) e = run_kind<K_DW>(A, s);
+  int cus = 0;
+  hipError_t e = device_cus(&cus);
+  if (e == hipSuccess && A.N > 0 && (A.dx || A.dWu)) e = run_act<K_DH>(A, cus, s);
+  if (e == hipSuccess && A.N > 0 && A.dx) e = run_act<K_DX>(A, cus, s);
+  if (e == hipSuccess && A.dWu) e = run_act<K_DWI>(A, cus, s);
+  if (e == hipSuccess && A.dWd) e = run_act<K_DWD>(A, cus, s);
   return e;
 }
 

@@ -1,0 +1,121 @@
+// Launch planning of the feed-forward block (host only): the tile of a product
+// and the number of parts that its sum is split into.
+#ifndef CARDAN_FFN_PLAN_H
+#define CARDAN_FFN_PLAN_H
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+namespace cardan {
+
+// The products of the block. "rows" are the rows of a group (tokens).
+enum FfnKind {
+  K_UP = 0,    // [rows, H] x [H, I] (gate and up): activation -> h, and g, u where kept
+  K_DOWN = 1,  // [rows, I] x [I, H] -> y
+  K_DH = 2,    // [rows, H] x Wd^T -> dh, turned into dg, du
+  K_DX = 3,    // dg Wg^T + du Wu^T -> dx
+  K_DWI = 4,   // x^T dg and x^T du: the sum runs over the group's rows
+  K_DWD = 5    // h^T dy, likewise
+};
+
+// A product of few tiles is split over its sum into at most kMaxSplit parts,
+// whose float32 partial outputs take at most this many bytes for N rows or
+// fewer (the widest output is the 2 I projections or H).
+constexpr int kMaxSplit = 32;
+constexpr size_t kPartialMax = (size_t)64 << 20;
+inline size_t ffn_partial_bytes(int32_t N, int32_t H, int32_t I, bool gated) {
+  const size_t wide = (size_t)(gated ? 2 : 1) * I;
+  const size_t all = (size_t)kMaxSplit * N * ((size_t)H > wide ? (size_t)H : wide) * 4;
+  return all < kPartialMax ? all : kPartialMax;
+}
+
+// Tiles (output rows x columns), the workgroups that a CU holds of them, and
+// the time of one step of 64 of the sum, measured with every CU busy
+// (8192 x 4096 x 11008 and 1000 x 4096 x 11008, operands in L2).
+struct FfnTile {
+  int bm, bn, per_cu;
+  double step_us;
+};
+constexpr FfnTile kFfnTiles[] = {{256, 256, 1, 1.70}, {128, 256, 1, 1.03}, {64, 256, 1, 0.66},
+                                 {128, 128, 2, 1.06}, {64, 128, 2, 0.83},  {32, 128, 2, 0.63}};
+constexpr int kFfnTileCount = sizeof kFfnTiles / sizeof kFfnTiles[0];
+constexpr double kUnitUs = 3.8;         // a unit's setup and epilogue ...
+constexpr double kUnitAreaUs = 4.0;     // ... plus this for 256 x 256 outputs
+constexpr double kJoinUs = 3.5;         // a joining kernel
+constexpr double kStreamBytesUs = 4.5e6;  // bytes per us that weights stream at
+
+// One product: `rows` output rows in `groups` groups (weight gradients: the
+// rows of one gradient, times `mats` matrices), `cols` columns, a sum of
+// `steps` steps, `weight_bytes` read or written once whatever the tile.
+struct FfnProduct {
+  int64_t rows, groups, mats;
+  int cols;
+  bool dual;      // two products side by side in a tile (gate and up)
+  bool grad;      // a weight gradient: every group has `rows` rows of its own
+  int64_t steps;
+  int max_split;  // parts that the workspace holds
+  double weight_bytes;
+};
+
+inline FfnProduct ffn_product(FfnKind kind, int32_t N, int32_t E, int32_t H, int32_t I, bool gated) {
+  const bool grad = kind == K_DWI || kind == K_DWD;
+  const bool over_h = kind == K_UP || kind == K_DH;  // the sum runs over H
+  const int64_t active = std::max(1, std::min(E, N));
+  FfnProduct p;
+  p.dual = kind == K_UP && gated;
+  p.grad = grad;
+  p.cols = over_h || kind == K_DWI ? I : H;
+  p.groups = grad ? E : active;
+  p.rows = kind == K_DWI ? H : kind == K_DWD ? I : N;
+  p.mats = kind == K_DWI && gated ? 2 : 1;
+  p.steps = grad ? (N / active + 63) / 64 : ((over_h ? H : I) + 63) / 64 * (kind == K_DX && gated ? 2 : 1);
+  p.weight_bytes = (double)p.groups * H * I * 2 * (p.dual || p.mats == 2 || (kind == K_DX && gated) ? 2 : 1);
+  // every part has a step, and its partial outputs a place in the workspace
+  const size_t plane = std::max((size_t)N * p.cols * 4 * (p.dual ? 2 : 1), (size_t)1);
+  const int64_t room = (int64_t)(ffn_partial_bytes(N, H, I, gated) / plane);
+  p.max_split = grad ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(room, p.steps), kMaxSplit));
+  return p;
+}
+
+struct FfnChoice {
+  int tile, split;
+};
+
+// The tile and split of least estimated time: rounds of units over the chip's
+// slots, each as long as its steps, against the time that the weights take to
+// stream; a split adds its joining kernel and the partial sums' bytes.
+// Groups end inside tiles: half a tile of each is counted as lost.
+inline FfnChoice choose_ffn(const FfnProduct& p, int cus) {
+  FfnChoice best = {0, 1};
+  double best_us = 1e30;
+  for (int t = 0; t < kFfnTileCount; ++t) {
+    const FfnTile& T = kFfnTiles[t];
+    const int bc = p.dual ? T.bn / 2 : T.bn;
+    const double cols = (double)((p.cols + bc - 1) / bc);
+    const double own = (double)((p.rows + T.bm - 1) / T.bm);
+    const double rows = p.grad ? own * p.groups * p.mats
+                               : p.groups == 1 ? own
+                                               : std::max((double)std::min(p.groups, p.rows), (double)p.rows / T.bm + 0.5 * p.groups);
+    const double unit_us = kUnitUs + kUnitAreaUs * T.bm * T.bn / 65536.0;
+    const double stream_us = p.weight_bytes / kStreamBytesUs;
+    for (int s = 1; s <= p.max_split; s = s < 4 ? s + 1 : s * 2) {
+      const double slots = (double)cus * T.per_cu;
+      const double units = rows * cols * s;
+      const double rounds = units <= slots ? 1.0 : (double)(int64_t)((units + slots - 1) / slots);
+      const double work = rounds * (T.step_us * (double)((p.steps + s - 1) / s) + unit_us);
+      const double join = s == 1 ? 0.0 : kJoinUs + s * (double)p.rows * p.cols * (p.dual ? 8.0 : 4.0) / 4.0e6;
+      const double us = std::max(work, stream_us) + 0.1 * std::min(work, stream_us) + join;
+      if (us < best_us) {
+        best_us = us;
+        best = {t, s};
+      }
+    }
+  }
+  return best;
+}
+
+}  // namespace cardan
+
+#endif  // CARDAN_FFN_PLAN_H

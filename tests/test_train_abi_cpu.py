@@ -6,9 +6,13 @@ pointers are never dereferenced.
 
 import ctypes
 import os
+import re
+import subprocess
 
 import pytest
 import torch
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 FAKE, ODD = 0x10000, 0x10004
 
@@ -150,3 +154,34 @@ def test_binding_refuses(C):
         C.distill_loss(z.double(), t, i)
     with pytest.raises(ValueError):
         C.distill_loss(z, t, i[0])
+
+
+def test_launch_choices(tmp_path):
+    exe = str(tmp_path / "ffn_plan_sweep")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
+                    "-include", "cmath", os.path.join(ROOT, "tests", "host", "ffn_plan_sweep.cpp"), "-o", exe],
+                   check=True, capture_output=True, text=True)
+    res = subprocess.run([exe, "3000"], capture_output=True, text=True)
+    assert res.returncode == 0 and " 0 failures" in res.stdout, res.stdout + res.stderr
+
+
+def test_kernels_do_not_spill(C, tmp_path):
+    """No kernel of any device image in the library keeps vector registers in scratch memory."""
+    llvm = os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "llvm", "bin")
+    fat = str(tmp_path / "fat")
+    if not os.path.exists(f"{llvm}/llvm-objcopy"):
+        pytest.skip("llvm tools not installed")
+    subprocess.run([f"{llvm}/llvm-objcopy", f"--dump-section=.hip_fatbin={fat}", C.LIB_PATH, str(tmp_path / "copy")],
+                   check=True, capture_output=True)
+    data = open(fat, "rb").read()
+    names = []
+    for i, at in enumerate(m.start() for m in re.finditer(b"__CLANG_OFFLOAD_BUNDLE__", data)):
+        part, obj = str(tmp_path / f"part{i}"), str(tmp_path / f"obj{i}")
+        open(part, "wb").write(data[at:])
+        subprocess.run([f"{llvm}/clang-offload-bundler", "--type=o", "--unbundle", f"--input={part}",
+                        f"--output={obj}", "--targets=hipv4-amdgcn-amd-amdhsa--gfx950"], check=True, capture_output=True)
+        notes = subprocess.run([f"{llvm}/llvm-readelf", "--notes", obj], check=True, capture_output=True, text=True).stdout
+        for sym, spill in re.findall(r"\.symbol:\s+(\S+)[\s\S]*?\.vgpr_spill_count:\s+(\d+)", notes):
+            names.append(sym)
+            assert spill == "0", sym
+    assert any("k_ffn" in n for n in names) and any("k_distill" in n for n in names)
