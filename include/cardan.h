@@ -278,10 +278,11 @@ int cardan_rmsnorm_bf16(int32_t B, int32_t H, const float* y, float eps,
  * The second stage of fitting a compressed layer (paper Sec. 3.3): a student
  * layer in dense bf16 form runs forward and backward over rows of any number,
  * and its logits are trained against a teacher's kept top logits, Eq. (3).
- * Conventions as above, except: the workspace of these calls needs no zero
- * fill, holds nothing between calls, and may serve any call of these two
- * operators in turn; their kernels are not persistent and do not wait on one
- * another. */
+ * Conventions as above, except: the workspace of the feed-forward calls needs
+ * no zero fill and holds nothing between calls (two calls that may overlap in
+ * time, two captured graphs among them, need one each); the loss needs none.
+ * No workgroup of these kernels waits for another one. The stream's device
+ * must be the current one. */
 
 /* Shape of a feed-forward block: E matrix sets (experts) of hidden size H and
  * intermediate size I. H % 64 == 0, I % 32 == 0, 1 <= E <= 1024, H * I * 2
@@ -343,10 +344,6 @@ int cardan_ffn_backward(const cardan_ffn_shape* shape, int32_t N, const cardan_b
 
 enum { CARDAN_LOGITS_BF16 = 0, CARDAN_LOGITS_F32 = 1 };
 
-/* Workspace bytes of cardan_distill_loss for up to N rows (0 is possible).
- * Host-only. */
-int cardan_distill_workspace_bytes(int32_t N, size_t* out);
-
 /* Distillation loss of paper Sec. 3.3, Eq. (3), per row, with its gradient:
  * student logits s over V vocabulary entries (row n at logits + n * ld, type
  * `logits_type`), a teacher's K kept logits t_j at entries i_j
@@ -372,7 +369,7 @@ int cardan_distill_loss(int32_t N, int32_t V, int32_t K, int32_t logits_type, co
                         int64_t ld, const float* teacher, const int32_t* ids,
                         const int32_t* labels, float temperature, float ce_weight,
                         const float* row_weight, float* loss, void* dlogits, int64_t dld,
-                        void* ws, size_t ws_bytes, hipStream_t stream);
+                        hipStream_t stream);
 
 /* Kernel timing for measurement. cardan_profile_begin(n) makes the next n
  * calls launch each kernel with a HIP start/stop event pair recorded by the

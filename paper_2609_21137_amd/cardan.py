@@ -13,6 +13,7 @@ raw bf16 bit pattern the ABI expects).
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 
@@ -94,8 +95,7 @@ def _load():
         "cardan_ffn_workspace_bytes": ([fp, i32, ctypes.POINTER(sz)], ctypes.c_int),
         "cardan_ffn_forward": ([fp, i32, vp, vp, wp, vp, vp, vp, vp, vp, sz, vp], ctypes.c_int),
         "cardan_ffn_backward": ([fp, i32, vp, vp, vp, wp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp], ctypes.c_int),
-        "cardan_distill_workspace_bytes": ([i32, ctypes.POINTER(sz)], ctypes.c_int),
-        "cardan_distill_loss": ([i32, i32, i32, i32, vp, i64, vp, vp, vp, f32, f32, vp, vp, vp, i64, vp, sz, vp],
+        "cardan_distill_loss": ([i32, i32, i32, i32, vp, i64, vp, vp, vp, f32, f32, vp, vp, vp, i64, vp],
                                 ctypes.c_int),
         "cardan_profile_begin": ([i32], ctypes.c_int),
         "cardan_profile_end": ([ctypes.POINTER(ctypes.c_float), ctypes.POINTER(i32)], ctypes.c_int),
@@ -116,7 +116,7 @@ EXPORTED = (
     "cardan_moe_layer_dense_down", "cardan_dense_moe_layer", "cardan_dense_moe_layer_relu2",
     "cardan_rmsnorm_bf16",
     "cardan_ffn_workspace_bytes", "cardan_ffn_forward", "cardan_ffn_backward",
-    "cardan_distill_workspace_bytes", "cardan_distill_loss",
+    "cardan_distill_loss",
     "cardan_profile_begin", "cardan_profile_end",
 )
 
@@ -452,11 +452,35 @@ def rmsnorm_bf16(y, eps: float = 1e-6, out=None):
 FFN_ACTS = {"silu_glu": 0, "relu2_up": 1}
 
 
-def _on(dev, *named):
-    """Every tensor of a call must live on its device."""
-    for name, t in named:
-        if isinstance(t, torch.Tensor) and t.device != dev:
-            raise ValueError(f"{name} is on {t.device}, expected {dev}")
+def _arg(t, dtype, name, shape, dev, optional=False):
+    """``_ptr`` for the calls whose whole time is a few microseconds: one pass
+    over a tensor's properties, with ``_ptr``'s messages where one does not fit,
+    and the tensor must live on the call's device. Returns the address."""
+    if t is None and optional:
+        return None
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.is_contiguous()
+            and t.device == dev and t.is_cuda):
+        return t.data_ptr()
+    _ptr(t, dtype, name, shape)
+    raise ValueError(f"{name} is on {t.device}, expected {dev}")
+
+
+class _Device:
+    """The current stream of a tensor's device, which is made current for the call."""
+    __slots__ = ("index", "was")
+
+    def __init__(self, dev):
+        self.index = dev.index
+
+    def __enter__(self):
+        self.was = torch.cuda.current_device()
+        if self.was != self.index:
+            torch.cuda.set_device(self.index)
+        return torch._C._cuda_getCurrentRawStream(self.index)
+
+    def __exit__(self, *exc):
+        if self.was != self.index:
+            torch.cuda.set_device(self.was)
 
 
 def ffn_shape(H, I, E=1, act="silu_glu") -> FfnShape:
@@ -473,6 +497,11 @@ def ffn_workspace_bytes(shape: FfnShape, N: int) -> int:
     return out.value
 
 
+@functools.lru_cache(maxsize=256)
+def _ffn_bytes(H, I, E, act, N):
+    return ffn_workspace_bytes(ffn_shape(H, I, E, act), N)
+
+
 def _ffn_call(x, W_gate, W_up, W_down, offsets, act, ws):
     """Shape, weights, offsets and workspace of a call, as the ABI takes them."""
     if not isinstance(x, torch.Tensor) or x.dim() != 2:
@@ -480,22 +509,23 @@ def _ffn_call(x, W_gate, W_up, W_down, offsets, act, ws):
     if not isinstance(W_up, torch.Tensor) or W_up.dim() not in (2, 3):
         raise ValueError("W_up must be a [H, I] or [E, H, I] tensor")
     N, H = x.shape
-    many = W_up.dim() == 3
-    E, I = (W_up.shape[0] if many else 1), W_up.shape[-1]
+    up_shape = W_up.shape
+    I = up_shape[-1]
+    many = len(up_shape) == 3
+    E = up_shape[0] if many else 1
     shape = ffn_shape(H, I, E, act)
-    pre = (E,) if many else ()
+    in_shape, out_shape = ((E, H, I), (E, I, H)) if many else ((H, I), (I, H))
     up_only = act == "relu2_up"
     if up_only and W_gate is not None:
         raise ValueError("up-only experts have no W_gate")
-    dev = x.device
-    _on(dev, ("W_gate", W_gate), ("W_up", W_up), ("W_down", W_down), ("offsets", offsets), ("ws", ws))
-    pg = _ptr(W_gate, torch.bfloat16, "W_gate", pre + (H, I), optional=up_only)
-    weights = FfnWeightsStruct(None if pg is None else pg.value,
-                               _ptr(W_up, torch.bfloat16, "W_up", pre + (H, I)).value,
-                               _ptr(W_down, torch.bfloat16, "W_down", pre + (I, H)).value)
-    off = _ptr(offsets, torch.int32, "offsets", (E + 1,), optional=E == 1)
+    dev, bf = x.device, torch.bfloat16
+    weights = FfnWeightsStruct(_arg(W_gate, bf, "W_gate", in_shape, dev, up_only),
+                               _arg(W_up, bf, "W_up", in_shape, dev), _arg(W_down, bf, "W_down", out_shape, dev))
+    off = _arg(offsets, torch.int32, "offsets", (E + 1,), dev, E == 1)
     if ws is None:
-        ws = torch.empty(ffn_workspace_bytes(shape, N), dtype=torch.uint8, device=dev)
+        ws = torch.empty(_ffn_bytes(H, I, E, act, N), dtype=torch.uint8, device=dev)
+    elif ws.dtype is not torch.uint8 or ws.device != dev or not ws.is_contiguous():
+        raise ValueError(f"ws must be a contiguous uint8 tensor on {dev}")
     return shape, N, weights, off, ws
 
 
@@ -514,23 +544,22 @@ def ffn_forward(x, W_gate, W_up, W_down, offsets=None, act: str = "silu_glu", sa
     ``out`` and ``saved`` give the tensors to write."""
     shape, N, weights, off, ws = _ffn_call(x, W_gate, W_up, W_down, offsets, act, ws)
     H, I, dev = shape.H, shape.I, x.device
-    y = out if out is not None else torch.empty((N, H), dtype=torch.bfloat16, device=dev)
+    bf, f32 = torch.bfloat16, torch.float32
+    gated = act == "silu_glu"
+    y = out if out is not None else torch.empty((N, H), dtype=bf, device=dev)
+    keep = save or saved is not None
     g = u = h = None
-    if save or saved is not None:
-        g, u, h = saved if saved is not None else (
-            torch.empty((N, I), dtype=torch.float32, device=dev) if act == "silu_glu" else None,
-            torch.empty((N, I), dtype=torch.float32, device=dev),
-            torch.empty((N, I), dtype=torch.bfloat16, device=dev))
-    _on(dev, ("out", y), ("gate", g), ("up", u), ("hidden", h))
-    keep = u is not None
-    with torch.cuda.device(dev):
-        _check(_lib.cardan_ffn_forward(
-            ctypes.byref(shape), N, _ptr(x, torch.bfloat16, "x", (N, H)), off, ctypes.byref(weights),
-            _ptr(y, torch.bfloat16, "out", (N, H)),
-            _ptr(g, torch.float32, "gate", (N, I), optional=not keep or act != "silu_glu"),
-            _ptr(u, torch.float32, "up", (N, I), optional=not keep),
-            _ptr(h, torch.bfloat16, "hidden", (N, I), optional=not keep),
-            _ptr(ws, torch.uint8, "ws"), ws.numel(), _stream(dev)))
+    if saved is not None:
+        g, u, h = saved
+    elif save:
+        g = torch.empty((N, I), dtype=f32, device=dev) if gated else None
+        u, h = torch.empty((N, I), dtype=f32, device=dev), torch.empty((N, I), dtype=bf, device=dev)
+    xp, yp = _arg(x, bf, "x", (N, H), dev), _arg(y, bf, "out", (N, H), dev)
+    gp, up, hp = (_arg(g, f32, "gate", (N, I), dev, not gated), _arg(u, f32, "up", (N, I), dev),
+                  _arg(h, bf, "hidden", (N, I), dev)) if keep else (None, None, None)
+    with _Device(dev) as stream:
+        _check(_lib.cardan_ffn_forward(ctypes.byref(shape), N, xp, off, ctypes.byref(weights), yp, gp, up, hp,
+                                       ws.data_ptr(), ws.numel(), stream))
     return (y, (g, u, h)) if keep else y
 
 
@@ -543,6 +572,7 @@ def ffn_backward(dy, x, W_gate, W_up, W_down, saved, offsets=None, act: str = "s
     None where not asked for. ``out`` gives the four tensors to write."""
     shape, N, weights, off, ws = _ffn_call(x, W_gate, W_up, W_down, offsets, act, ws)
     H, I, dev = shape.H, shape.I, x.device
+    bf, f32 = torch.bfloat16, torch.float32
     gated = act == "silu_glu"
     if out is not None:
         dx, dWg, dWu, dWd = out
@@ -551,39 +581,35 @@ def ffn_backward(dy, x, W_gate, W_up, W_down, saved, offsets=None, act: str = "s
         dWg = torch.empty_like(W_gate) if need_dw and gated else None
         dWu, dWd = (torch.empty_like(W_up), torch.empty_like(W_down)) if need_dw else (None, None)
     g, u, h = saved
-    _on(dev, ("dy", dy), ("gate", g), ("up", u), ("hidden", h), ("dx", dx), ("dW_gate", dWg), ("dW_up", dWu),
-        ("dW_down", dWd))
-    bf = torch.bfloat16
-    with torch.cuda.device(dev):
-        _check(_lib.cardan_ffn_backward(
-            ctypes.byref(shape), N, _ptr(dy, bf, "dy", (N, H)), _ptr(x, bf, "x", (N, H)), off,
-            ctypes.byref(weights), _ptr(g, torch.float32, "gate", (N, I), optional=not gated),
-            _ptr(u, torch.float32, "up", (N, I)), _ptr(h, bf, "hidden", (N, I)),
-            _ptr(dx, bf, "dx", (N, H), optional=True),
-            _ptr(dWg, bf, "dW_gate", W_gate.shape if gated else None, optional=True),
-            _ptr(dWu, bf, "dW_up", W_up.shape, optional=True), _ptr(dWd, bf, "dW_down", W_down.shape, optional=True),
-            _ptr(ws, torch.uint8, "ws"), ws.numel(), _stream(dev)))
+    args = (_arg(dy, bf, "dy", (N, H), dev), _arg(x, bf, "x", (N, H), dev), off, ctypes.byref(weights),
+            _arg(g, f32, "gate", (N, I), dev, not gated), _arg(u, f32, "up", (N, I), dev),
+            _arg(h, bf, "hidden", (N, I), dev), _arg(dx, bf, "dx", (N, H), dev, True),
+            _arg(dWg, bf, "dW_gate", W_up.shape, dev, True), _arg(dWu, bf, "dW_up", W_up.shape, dev, True),
+            _arg(dWd, bf, "dW_down", W_down.shape, dev, True))
+    with _Device(dev) as stream:
+        _check(_lib.cardan_ffn_backward(ctypes.byref(shape), N, *args, ws.data_ptr(), ws.numel(), stream))
     return dx, dWg, dWu, dWd
 
 
-def _rows_ptr(t, dtype, name, shape):
-    """A [N, V] tensor whose rows are contiguous, as (pointer, row stride)."""
+def _rows_ptr(t, dtype, name, shape, dev):
+    """A [N, V] tensor whose rows are contiguous, as (address, row stride)."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch tensor")
-    if t.dtype != dtype or t.device.type != "cuda" or tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must be a GPU tensor of {dtype} and shape {tuple(shape)}, "
+    if t.dtype is not dtype or not t.is_cuda or t.device != dev or t.shape != shape:
+        raise ValueError(f"{name} must be a tensor of {dtype} and shape {shape} on {dev if dev.type == 'cuda' else 'a GPU'}, "
                          f"got {t.dtype}, {tuple(t.shape)} on {t.device}")
-    N, V = t.shape
-    if V > 1 and t.stride(1) != 1:
+    N, V = shape
+    st = t.stride()
+    if V > 1 and st[1] != 1:
         raise ValueError(f"the rows of {name} must be contiguous")
-    ld = t.stride(0) if N > 1 else V
+    ld = st[0] if N > 1 else V
     if ld < V:
         raise ValueError(f"the rows of {name} overlap")
-    return ctypes.c_void_p(t.data_ptr()), ld
+    return t.data_ptr(), ld
 
 
 def distill_loss(logits, teacher, ids, labels=None, temperature: float = 1.0, ce_weight: float = 0.0,
-                 row_weight=None, grad: bool = True, out=None, dlogits=None, ws=None):
+                 row_weight=None, grad: bool = True, out=None, dlogits=None):
     """Distillation loss of student ``logits [N, V]`` (bf16 or float32, rows
     may be padded) against a teacher's kept logits ``teacher [N, K]`` (float32)
     at the vocabulary entries ``ids [N, K]`` (int32), and its gradient.
@@ -601,26 +627,18 @@ def distill_loss(logits, teacher, ids, labels=None, temperature: float = 1.0, ce
     if not isinstance(ids, torch.Tensor) or ids.dim() != 2:
         raise ValueError("ids must be a [N, K] tensor")
     K = ids.shape[1]
-    lp, ld = _rows_ptr(logits, logits.dtype, "logits", (N, V))
-    loss = out if out is not None else torch.empty((N, 2), dtype=torch.float32, device=dev)
+    dt, f32, i32 = logits.dtype, torch.float32, torch.int32
+    lp, ld = _rows_ptr(logits, dt, "logits", (N, V), dev)
+    loss = out if out is not None else torch.empty((N, 2), dtype=f32, device=dev)
     if dlogits is None and grad:
         # rows as far apart as the logits' (their alignment), where that is padding
-        dlogits = torch.empty((N, ld if ld <= 2 * V else V), dtype=logits.dtype, device=dev)[:, :V]
-    _on(dev, ("teacher", teacher), ("ids", ids), ("labels", labels), ("row_weight", row_weight), ("out", loss),
-        ("dlogits", dlogits), ("ws", ws))
-    gp, dld = _rows_ptr(dlogits, logits.dtype, "dlogits", (N, V)) if dlogits is not None else (None, 0)
-    if ws is None:
-        need = ctypes.c_size_t(0)
-        _check(_lib.cardan_distill_workspace_bytes(N, ctypes.byref(need)))
-        ws = torch.empty(need.value, dtype=torch.uint8, device=dev)
-    with torch.cuda.device(dev):
-        _check(_lib.cardan_distill_loss(
-            N, V, K, 1 if logits.dtype == torch.float32 else 0, lp, ld,
-            _ptr(teacher, torch.float32, "teacher", (N, K)), _ptr(ids, torch.int32, "ids", (N, K)),
-            _ptr(labels, torch.int32, "labels", (N,), optional=True), temperature, ce_weight,
-            _ptr(row_weight, torch.float32, "row_weight", (N,), optional=True),
-            _ptr(loss, torch.float32, "out", (N, 2)), gp, dld, _ptr(ws, torch.uint8, "ws"), ws.numel(),
-            _stream(dev)))
+        dlogits = torch.empty((N, ld if ld <= 2 * V else V), dtype=dt, device=dev)[:, :V]
+    gp, dld = _rows_ptr(dlogits, dt, "dlogits", (N, V), dev) if dlogits is not None else (None, 0)
+    args = (_arg(teacher, f32, "teacher", (N, K), dev), _arg(ids, i32, "ids", (N, K), dev),
+            _arg(labels, i32, "labels", (N,), dev, True), temperature, ce_weight,
+            _arg(row_weight, f32, "row_weight", (N,), dev, True), _arg(loss, f32, "out", (N, 2), dev), gp, dld)
+    with _Device(dev) as stream:
+        _check(_lib.cardan_distill_loss(N, V, K, 1 if dt is f32 else 0, lp, ld, *args, stream))
     return loss, dlogits
 
 

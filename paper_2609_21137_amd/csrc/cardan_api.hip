@@ -839,18 +839,10 @@ int cardan_ffn_backward(const cardan_ffn_shape* shape, int32_t N, const cardan_b
   return e == hipSuccess ? CARDAN_OK : hip_fail(e, "ffn backward launch");
 }
 
-int cardan_distill_workspace_bytes(int32_t N, size_t* out) {
-  g_err[0] = 0;
-  if (N < 0) return fail(CARDAN_ERR_BAD_SHAPE, "N=%d is negative", N);
-  if (!out) return fail(CARDAN_ERR_NULL_PTR, "out is NULL");
-  *out = 0;
-  return CARDAN_OK;
-}
-
 int cardan_distill_loss(int32_t N, int32_t V, int32_t K, int32_t logits_type, const void* logits, int64_t ld,
                         const float* teacher, const int32_t* ids, const int32_t* labels, float temperature,
                         float ce_weight, const float* row_weight, float* loss, void* dlogits, int64_t dld,
-                        void* ws, size_t ws_bytes, hipStream_t stream) {
+                        hipStream_t stream) {
   g_err[0] = 0;
   if (N < 0 || V < 1 || V > (1 << 30)) return fail(CARDAN_ERR_BAD_SHAPE, "N=%d, V=%d outside the valid range", N, V);
   if (K < 0 || K > 1024) return fail(CARDAN_ERR_UNSUPPORTED, "K=%d outside [0, 1024]", K);
@@ -862,10 +854,6 @@ int cardan_distill_loss(int32_t N, int32_t V, int32_t K, int32_t logits_type, co
                 (long long)dld, V);
   if (!(temperature > 0.0f) || !isfinite(temperature) || !isfinite(1.0f / temperature) || !isfinite(ce_weight))
     return fail(CARDAN_ERR_BAD_SHAPE, "temperature must be finite and > 0, ce_weight finite");
-  size_t need = 0;
-  int rc = cardan_distill_workspace_bytes(N, &need);
-  if (rc) return rc;
-  if (need > 0 && (rc = check_ws(need, ws, ws_bytes))) return rc;
   if (N == 0) return CARDAN_OK;
   REQ(logits, "logits");
   REQ(loss, "loss");

@@ -177,11 +177,9 @@ struct Operand {
     }
   }
 
-  __device__ __forceinline__ void issue(u32x4 rs, uint32_t lds, int wave, bool last) const {
-    const uint32_t drop = last && tail ? kOob : 0u;
-#pragma unroll
-    for (int j = 0; j < kLoads; ++j)
-      load_to_lds(rs, lds + (j * NW + wave) * 1024, voff[j] | drop);
+  // load j of this wave; `last`: the step is the sum's last
+  __device__ __forceinline__ void issue(u32x4 rs, uint32_t lds, int wave, bool last, int j) const {
+    load_to_lds(rs, lds + (j * NW + wave) * 1024, voff[j] | (last && tail ? kOob : 0u));
   }
 
   // byte of the first operand read of the 16-row block that starts at row r0
@@ -221,16 +219,6 @@ __device__ __forceinline__ void wait_loads() {
   asm volatile("" ::: "memory");
 }
 
-// Scheduling order of a block: READS LDS reads spread evenly over PRODS products.
-template <int I, int READS, int PRODS>
-__device__ __forceinline__ void weave() {
-  if constexpr (I < READS) {
-    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-    __builtin_amdgcn_sched_group_barrier(0x008, PRODS * (I + 1) / READS - PRODS * I / READS, 0);
-    weave<I + 1, READS, PRODS>();
-  }
-}
-
 // Activation of four projections; g is not used by up-only experts.
 template <bool RELU2>
 __device__ __forceinline__ f32x4 activate(f32x4 g, f32x4 u) {
@@ -262,16 +250,49 @@ __device__ __forceinline__ void activate_grad(f32x4 dh, f32x4 g, f32x4 u, f32x4&
   }
 }
 
-// Stores the bf16 values of two neighbouring 16x16 blocks, four of a lane in
-// each, as 16 bytes a lane: the odd 16-lane groups' part of the first block
-// changes places with the even groups' part of the second, which leaves every
-// lane eight consecutive columns of one block. p: the lane's row at the first
-// block's first column.
-__device__ __forceinline__ void store_pair(uint16_t* p, uint2 a, uint2 b) {
-  const int grp = (threadIdx.x & 63) >> 4;
+// The bf16 values of two neighbouring 16x16 blocks, four of a lane in each, as
+// eight consecutive columns a lane: the odd 16-lane groups' part of the first
+// block changes places with the even groups' part of the second. The lane's
+// columns begin at pair_col().
+__device__ __forceinline__ u32x4 pair_up(uint2 a, uint2 b) {
   const auto x = __builtin_amdgcn_permlane16_swap(a.x, b.x, false, false);
   const auto y = __builtin_amdgcn_permlane16_swap(a.y, b.y, false, false);
-  *(uint4*)(p + (grp & 1) * 16 + (grp >> 1) * 8) = make_uint4(x[0], y[0], x[1], y[1]);
+  return u32x4{x[0], y[0], x[1], y[1]};
+}
+__device__ __forceinline__ int pair_col() {
+  const int grp = (threadIdx.x & 63) >> 4;
+  return (grp & 1) * 16 + (grp >> 1) * 8;
+}
+
+// Two 64-byte pieces of a row, a and b (four lanes' 16 bytes each, in 16
+// rows): lanes 8..15 of a row group's a change places with lanes 0..7's b, so
+// that one store covers whole 128-byte lines of eight rows. Lane (lane & 15)
+// stores `s0` to row (lane & 7), `s1` to row (lane & 7) + 8, at the first
+// piece's columns for lanes 0..7 and the second's for 8..15.
+__device__ __forceinline__ void lines_of(u32x4 a, u32x4 b, u32x4& s0, u32x4& s1) {
+  const bool high = threadIdx.x & 8;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const uint32_t give = high ? a[q] : b[q];
+    const uint32_t got = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)give, 0x128, 0xF, 0xF, false);  // row_ror:8
+    s0[q] = high ? got : a[q];
+    s1[q] = high ? b[q] : got;
+  }
+}
+
+template <bool NT>
+__device__ __forceinline__ void put16(void* p, u32x4 v) {
+  if constexpr (NT) __builtin_nontemporal_store(v, (u32x4*)p);
+  else *(u32x4*)p = v;
+}
+
+// Whole lines of rows r8 and r8 + 8 (those below `end`), pieces a and b.
+template <bool NT>
+__device__ __forceinline__ void put_lines(char* p, int64_t row_bytes, int r8, int end, u32x4 a, u32x4 b) {
+  u32x4 s0, s1;
+  lines_of(a, b, s0, s1);
+  if (r8 < end) put16<NT>(p, s0);
+  if (r8 + 8 < end) put16<NT>(p + 8 * row_bytes, s1);
 }
 
 // Output tiles [BM x BN] of one product. WM x WN waves; a wave holds
@@ -331,10 +352,14 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_ffn(const FfnArgs A, const 
       int t = id - U.e * of;
       U.mat = kMats == 2 ? t & 1 : 1;
       t /= kMats;
-      int lo, hi;
-      group_rows(A, U.e, lo, hi);
-      lo = __builtin_amdgcn_readfirstlane(lo);
-      hi = __builtin_amdgcn_readfirstlane(hi);
+      // (a scalar load: a vector load's wait would be one for the stores of the
+      // unit before, too)
+      int lo = 0, hi = A.N;
+      if (A.off) {
+        const auto* off = (const __attribute__((address_space(4))) int32_t*)A.off;
+        lo = clampi(off[U.e], 0, A.N);
+        hi = clampi(off[U.e + 1], lo, A.N);
+      }
       const int rows = hi - lo;
       U.row = t / G.col_tiles * BM;
       U.n0 = t % G.col_tiles * BN;
@@ -375,53 +400,65 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_ffn(const FfnArgs A, const 
   const int bbase = OpB::base(wn * (BC / WN));
   const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS char*)smem;
 
-  // the loads: one step of the unit P into a stage, then on to the next step.
-  // Past the last unit empty resources are loaded, so that every wave always
-  // has the same number of loads in flight.
+  // The loads: one step of the unit P into a stage. step_ahead() forms the
+  // resources of the next step, fill() issues the wave's load q of it. Past the
+  // last unit empty resources are loaded, so that every wave always has the
+  // same number of loads in flight.
   int pu = first;
   Unit P;
   if (pu < units) setup(pu, P);
-  auto issue = [&](int stage) {
+  constexpr int kLoads = OpA::kLoads + OpB::kLoads * (kDual ? 2 : 1);
+  u32x4 ra, rb, rb1;
+  bool last = false;
+  auto step_ahead = [&]() {
     const bool some = pu < units;
-    const uint32_t buf = lds0 + stage * kStage;
     const bool ph = kPh == 2 && P.k >= P.kt1;
     const int k = P.k - (ph ? P.kt1 : 0);
-    const bool last = k == P.kt1 - 1;
+    last = k == P.kt1 - 1;
     const int64_t ao = k * astep, bo = k * bstep;
-    opa.issue(make_rsrc((ph ? P.a1 : P.a) + ao, some ? P.ab - ao : 0), buf, wave, last);
-    opb.issue(make_rsrc((ph ? P.b1 : P.b) + bo, some ? P.bb - bo : 0), buf + BM * 128, wave, last);
-    if constexpr (kDual) opb.issue(make_rsrc(P.b1 + bo, some ? P.bb - bo : 0), buf + (BM + BC) * 128, wave, last);
+    ra = make_rsrc((ph ? P.a1 : P.a) + ao, some ? P.ab - ao : 0);
+    rb = make_rsrc((ph ? P.b1 : P.b) + bo, some ? P.bb - bo : 0);
+    if constexpr (kDual) rb1 = make_rsrc(P.b1 + bo, some ? P.bb - bo : 0);
     if (some && ++P.k == P.kend) {
       pu += stride;
       if (pu < units) setup(pu, P);
     }
   };
-  constexpr int kLoads = OpA::kLoads + OpB::kLoads * (kDual ? 2 : 1);
+  auto fill = [&](int stage, int q) {
+    const uint32_t buf = lds0 + stage * kStage;
+    if (q < OpA::kLoads) opa.issue(ra, buf, wave, last, q);
+    else if (q < OpA::kLoads + OpB::kLoads) opb.issue(rb, buf + BM * 128, wave, last, q - OpA::kLoads);
+    else opb.issue(rb1, buf + (BM + BC) * 128, wave, last, q - OpA::kLoads - OpB::kLoads);
+  };
 
   bf16x8 a0f[MF], b0f[NF], a1f[MF], b1f[NF];  // operands of the two halves of a step
-  auto read = [&](int st, int kk, bf16x8(&a)[MF], bf16x8(&b)[NF]) {
+  auto read1 = [&](int st, int kk, bf16x8(&a)[MF], bf16x8(&b)[NF], int q) {
     const char* la = smem + st * kStage;
     const char* lb = la + BM * 128;
-#pragma unroll
-    for (int j = 0; j < NF; ++j) {
-      if constexpr (kDual)
-        b[j] = OpB::read(lb + (j < NF / 2 ? 0 : BC * 128), bbase, j % (NF / 2), kk);
-      else
-        b[j] = OpB::read(lb, bbase, j, kk);
-    }
-#pragma unroll
-    for (int i = 0; i < MF; ++i) a[i] = OpA::read(la, abase, i, kk);
+    if (q >= NF) a[q - NF] = OpA::read(la, abase, q - NF, kk);
+    else if constexpr (kDual) b[q] = OpB::read(lb + (q < NF / 2 ? 0 : BC * 128), bbase, q % (NF / 2), kk);
+    else b[q] = OpB::read(lb, bbase, q, kk);
   };
   f32x4 acc[MF][NF];
-  auto multiply = [&](bf16x8(&a)[MF], bf16x8(&b)[NF]) {
+  // Half a step: its products row by row, and between them the operand reads
+  // of the next half (all issued in the first three quarters, so that they have
+  // returned at its end) and, in the second half, the loads of a step ahead.
+  auto half = [&](bf16x8(&a)[MF], bf16x8(&b)[NF], int st, int kk, bf16x8(&an)[MF], bf16x8(&bn)[NF], bool loads, int to) {
+    constexpr int kR = MF + NF, kQ = MF > 2 ? MF - 1 : MF;
 #pragma unroll
-    for (int i = 0; i < MF; ++i)
+    for (int i = 0; i < MF; ++i) {
+      if (loads)
+#pragma unroll
+        for (int q = kLoads * i / MF; q < kLoads * (i + 1) / MF; ++q) fill(to, q);
+      if (i < kQ)
+#pragma unroll
+        for (int q = kR * i / kQ; q < kR * (i + 1) / kQ; ++q) read1(st, kk, an, bn, q);
 #pragma unroll
       for (int j = 0; j < NF; ++j)
         acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], a[i], acc[i][j], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
-  // order of a half: operand reads of the next half between the products
-  constexpr int kReads = MF * (kAT ? 2 : 1) + NF * (kBT ? 2 : 1), kProds = MF * NF;
 
   // lane -> output row (lane & 15) of a block, columns (lane >> 4) * 4 + 0..3
   auto epilogue = [&](const Unit& C, int wrow, int wcol) {
@@ -455,8 +492,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_ffn(const FfnArgs A, const 
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
           const int c = wcol + j * 16 < nout ? wcol + j * 16 : wcol;
-          in[i & 1][j][0] = *(const f32x4*)(A.u + rb + c);
-          if constexpr (!RELU2) in[i & 1][j][1] = *(const f32x4*)(A.g + rb + c);
+          in[i & 1][j][0] = __builtin_nontemporal_load((const f32x4*)(A.u + rb + c));
+          if constexpr (!RELU2) in[i & 1][j][1] = __builtin_nontemporal_load((const f32x4*)(A.g + rb + c));
         }
       }
     };
@@ -466,21 +503,12 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_ffn(const FfnArgs A, const 
 #pragma unroll
     for (int i = 0; i < MF; ++i) {
       if (i + 1 < MF) fetch(i + 1);
-      const int r = r0 + i * 16;
-      if (r >= C.end) continue;
-      const int64_t rb = (int64_t)r * nout;
+      if (wrow + i * 16 >= C.end) break;
       uint2 v0[NC], v1[NC];
 #pragma unroll
       for (int j = 0; j < NC; ++j) {
-        const int c = wcol + j * 16;
         if constexpr (KIND == K_UP) {
-          const f32x4 g = acc[i][j], u = acc[i][kDual ? j + NC : j];
-          if (c < nout) {
-            if constexpr (!RELU2)
-              if (A.g) *(f32x4*)(A.g + rb + c + q4) = g;
-            if (A.u) *(f32x4*)(A.u + rb + c + q4) = u;
-          }
-          v0[j] = pack4(activate<RELU2>(g, u));
+          v0[j] = pack4(activate<RELU2>(acc[i][j], acc[i][kDual ? j + NC : j]));
         } else if constexpr (KIND == K_DH) {
           f32x4 dg, du;
           activate_grad<RELU2>(acc[i][j], in[i & 1][j][kGu - 1], in[i & 1][j][0], dg, du);
@@ -490,19 +518,62 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_ffn(const FfnArgs A, const 
           v0[j] = pack4(acc[i][j]);
         }
       }
-      if constexpr (NC % 2 == 0) {
+      const int r = r0 + i * 16, r8 = wrow + i * 16 + (lane & 7), high = lane >> 3 & 1;
+      const int64_t rb = (int64_t)r * nout, rb8 = (int64_t)r8 * nout;
+      if constexpr (KIND == K_UP && NC % 2 == 0) {  // kept projections: pieces are blocks of 16 float32
+        if (A.u) {
+#pragma unroll
+          for (int j = 0; j < NC; j += 2) {
+            if (wcol + j * 16 >= nout) continue;
+            const int64_t at = rb8 + wcol + j * 16 + high * 16 + q4;
+            if constexpr (!RELU2)
+              put_lines<true>((char*)(A.g + at), (int64_t)nout * 4, r8, C.end, __builtin_bit_cast(u32x4, acc[i][j]), __builtin_bit_cast(u32x4, acc[i][j + 1]));
+            put_lines<true>((char*)(A.u + at), (int64_t)nout * 4, r8, C.end, __builtin_bit_cast(u32x4, acc[i][kDual ? j + NC : j]), __builtin_bit_cast(u32x4, acc[i][kDual ? j + 1 + NC : j + 1]));
+          }
+        }
+      } else if constexpr (KIND == K_UP) {
+        if (r < C.end && A.u && wcol < nout) {
+          static_assert(NC == 1, "blocks come in pairs or alone");
+          if constexpr (!RELU2) *(f32x4*)(A.g + rb + wcol + q4) = acc[i][0];
+          *(f32x4*)(A.u + rb + wcol + q4) = acc[i][kDual ? NC : 0];
+        }
+      }
+      if constexpr (NC % 4 == 0) {  // pieces are pairs of bf16 blocks
+#pragma unroll
+        for (int j = 0; j < NC; j += 4) {
+          const int c = wcol + j * 16;
+          if (c >= nout) continue;
+          if (c + 32 < nout) {
+            const int64_t at = rb8 + c + high * 32 + pair_col();
+            put_lines<kDW>((char*)(o0 + at), (int64_t)nout * 2, r8, C.end, pair_up(v0[j], v0[j + 1]), pair_up(v0[j + 2], v0[j + 3]));
+            if constexpr (KIND == K_DH && !RELU2)
+              put_lines<false>((char*)(A.dg + at), (int64_t)nout * 2, r8, C.end, pair_up(v1[j], v1[j + 1]), pair_up(v1[j + 2], v1[j + 3]));
+          } else {
+            const u32x4 a = pair_up(v0[j], v0[j + 1]);
+            if (r < C.end) put16<false>(o0 + rb + c + pair_col(), a);
+            if constexpr (KIND == K_DH && !RELU2) {
+              const u32x4 b = pair_up(v1[j], v1[j + 1]);
+              if (r < C.end) put16<false>(A.dg + rb + c + pair_col(), b);
+            }
+          }
+        }
+      } else if constexpr (NC % 2 == 0) {
 #pragma unroll
         for (int j = 0; j < NC; j += 2) {
           const int c = wcol + j * 16;
           if (c >= nout) continue;
-          store_pair(o0 + rb + c, v0[j], v0[j + 1]);
-          if constexpr (KIND == K_DH && !RELU2) store_pair(A.dg + rb + c, v1[j], v1[j + 1]);
+          const u32x4 a = pair_up(v0[j], v0[j + 1]);
+          if (r < C.end) put16<false>(o0 + rb + c + pair_col(), a);
+          if constexpr (KIND == K_DH && !RELU2) {
+            const u32x4 b = pair_up(v1[j], v1[j + 1]);
+            if (r < C.end) put16<false>(A.dg + rb + c + pair_col(), b);
+          }
         }
       } else {
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
           const int c = wcol + j * 16;
-          if (c >= nout) continue;
+          if (c >= nout || r >= C.end) continue;
           *(uint2*)(o0 + rb + c + q4) = v0[j];
           if constexpr (KIND == K_DH && !RELU2) *(uint2*)(A.dg + rb + c + q4) = v1[j];
         }
@@ -512,9 +583,28 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_ffn(const FfnArgs A, const 
 
   if (first >= units) return;
 #pragma unroll
-  for (int s = 0; s < NS; ++s) issue(s);
+  for (int st = 0; st < NS; ++st) {
+    step_ahead();
+#pragma unroll
+    for (int q = 0; q < kLoads; ++q) fill(st, q);
+  }
+  step_ahead();
   wait_loads<(NS - 1) * kLoads>();
-  read(0, 0, a0f, b0f);
+  auto read_first = [&](int st) {
+#pragma unroll
+    for (int q = 0; q < MF + NF; ++q) read1(st, 0, a0f, b0f, q);
+  };
+  read_first(0);
+  // Stores of an epilogue whose outputs all lie inside (at least: kept
+  // projections and partial sums are more). Memory operations complete in the
+  // order they were issued, and the loads of a unit's second step are older
+  // than the stores of the unit before: the wait for them need not wait for
+  // those stores.
+  constexpr int kOutBlocks = kDual ? NF / 2 : NF;
+  constexpr int kStores = MF * (kOutBlocks > 1 ? kOutBlocks / 2 : 1) * (KIND == K_DH && !RELU2 ? 2 : 1);
+  constexpr int kBehind = (NS - 2) * kLoads;
+  constexpr int kBehindStores = kBehind + kStores < 63 ? kBehind + kStores : 63;
+  bool stored = false;
   int stage = 0;
   for (int u = first; u < units; u += stride) {
     Unit C;
@@ -526,29 +616,32 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_ffn(const FfnArgs A, const 
     const int wrow = C.row + wm * (BM / WM), wcol = C.n0 + wn * (BC / WN);
     if (wrow < C.end && wcol < nout) {
       for (int kt = C.k; kt < C.kend; ++kt) {
-        read(stage, 1, a1f, b1f);
-        multiply(a0f, b0f);
-        weave<0, kReads, kProds>();
+        half(a0f, b0f, stage, 1, a1f, b1f, false, 0);
         // the next step has landed, and this step's stage has been read by every wave
-        wait_loads<(NS - 2) * kLoads>();
-        issue(stage);
-        stage = stage == NS - 1 ? 0 : stage + 1;
-        read(stage, 0, a0f, b0f);
-        multiply(a1f, b1f);
-        weave<0, kReads, kProds>();
+        if (kDW && stored) wait_loads<kBehindStores>();
+        else wait_loads<kBehind>();
+        stored = false;
+        const int next = stage == NS - 1 ? 0 : stage + 1;
+        half(a1f, b1f, next, 0, a0f, b0f, true, stage);
+        stage = next;
+        step_ahead();
       }
     } else {  // a wave whose outputs lie past the end only loads
+      stored = false;
       for (int kt = C.k; kt < C.kend; ++kt) {
-        wait_loads<(NS - 2) * kLoads>();
-        issue(stage);
+        wait_loads<kBehind>();
+#pragma unroll
+        for (int q = 0; q < kLoads; ++q) fill(stage, q);
         stage = stage == NS - 1 ? 0 : stage + 1;
+        step_ahead();
       }
-      read(stage, 0, a0f, b0f);
+      read_first(stage);
       continue;
     }
 
     epilogue(C, wrow, wcol);
-    read(stage, 0, a0f, b0f);
+    stored = wrow + BM / WM <= C.end && wcol + BC / WN <= nout;
+    read_first(stage);
   }
   __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): no load to LDS outlives the workgroup
 }
@@ -568,10 +661,21 @@ __global__ __launch_bounds__(256) void k_ffn_join(const FfnArgs A, int split) {
   if (at >= (int64_t)hi * nout) return;
   const float* p = A.part + at;
   f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
-  for (int s = 0; s < split; ++s) {
-    a += *(const f32x4*)p;
-    if constexpr (kDual) b += *(const f32x4*)(p + plane);
-    p += plane * (kDual ? 2 : 1);
+  const int64_t step = plane * (kDual ? 2 : 1);
+  for (int s0 = 0; s0 < split; s0 += 8) {  // eight parts' loads at once; a part past the end is read as the last
+    f32x4 pa[8], pb[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float* q = p + step * (s0 + k < split ? s0 + k : split - 1);
+      pa[k] = *(const f32x4*)q;
+      if constexpr (kDual) pb[k] = *(const f32x4*)(q + plane);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (s0 + k >= split) break;
+      a += pa[k];
+      if constexpr (kDual) b += pb[k];
+    }
   }
   if constexpr (KIND == K_UP) {
     if constexpr (!RELU2)
@@ -638,6 +742,175 @@ hipError_t run_act(const FfnArgs& A, int cus, hipStream_t s) {
   return A.relu2 ? run_kind<KIND, true>(A, cus, s) : run_kind<KIND, false>(A, cus, s);
 }
 
+// ---------------------------------------------------------------------------
+// Few rows through one small matrix set: the latency of two launches is most
+// of the time. The weights go from memory to the matrix operands without LDS.
+// A workgroup has 32 output columns (of both projections for gated experts),
+// its NW waves take the sum's steps of 32 in turn. A lane reads two neighbouring
+// columns of eight rows of a step, and byte permutations turn them into two
+// operands of eight sum elements of one column; x comes as 16-byte row pieces.
+// The waves' partial outputs are added in order through LDS.
+// ---------------------------------------------------------------------------
+//
+// Where the groups of columns are fewer than the CUs, gridDim.y workgroups of
+// the first product share a group's sum (PART) and leave their partial
+// projections; each of the second product's workgroups adds them, in order,
+// and forms h in LDS: no launch in between.
+template <int KIND, bool RELU2, int MB, int NW, bool PART>
+__global__ __launch_bounds__(64 * NW, NW / 4) void k_ffn_few(const FfnArgs A, int split) {
+  constexpr bool kDual = KIND == K_UP && !RELU2;
+  constexpr int CW = 2;  // neighbouring columns of a lane
+  constexpr int NM = kDual ? 2 : 1, kCols = 16 * CW, kPad = kCols + CW;
+  constexpr int kAhead = 2;  // steps of a wave whose loads are in flight
+  __shared__ float red[NW][NM][16 * kPad];
+  extern __shared__ __align__(16) uint16_t hidden[];  // [N][I] (second product, PART)
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int n16 = lane & 15, kg = lane >> 4;
+  const int nout = KIND == K_UP ? A.I : A.H, ksum = KIND == K_UP ? A.H : A.I;
+  // neighbouring columns, which may share memory lines, go to one XCD
+  const int groups = (nout + kCols - 1) / kCols, per = (gridDim.x + 7) >> 3;
+  const int grp = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  if (grp >= groups) return;
+  const int c0 = grp * kCols;
+  const int all = ksum >> 5, y = blockIdx.y;
+  const int beg = KIND == K_UP && PART ? all * y / split : 0, steps = KIND == K_UP && PART ? all * (y + 1) / split : all;
+
+  const auto res = [](const void* p, uint32_t n) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, (int)n, 0x00020000);
+  };
+  const uint32_t wbytes = (uint32_t)((size_t)ksum * nout * 2);
+  const auto rw0 = res(KIND == K_UP ? (RELU2 ? A.Wu : A.Wg) : A.Wd, wbytes);
+  const auto rw1 = res(A.Wu, wbytes);
+  const auto rx = res(KIND == K_UP ? A.x : A.h, (uint32_t)((size_t)A.N * ksum * 2));
+  const int col = c0 + n16 * CW;
+  const uint32_t wv = col < nout ? (uint32_t)((kg * 8 * nout + col) * 2) : kOob;
+  uint32_t xv[MB];
+#pragma unroll
+  for (int b = 0; b < MB; ++b) xv[b] = b * 16 + n16 < A.N ? (uint32_t)(((b * 16 + n16) * ksum + kg * 8) * 2) : kOob;
+
+  uint32_t wb[kAhead][NM][8];
+  u32x4 xb[kAhead][MB];
+  auto load = [&](int slot, int st) {
+    if (st >= steps) return;
+    const uint32_t wo = (uint32_t)st * 32u * (uint32_t)nout * 2u;
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+#pragma unroll
+      for (int m = 0; m < NM; ++m)
+        wb[slot][m][r] = __builtin_amdgcn_raw_buffer_load_b32(m ? rw1 : rw0, (wv + (uint32_t)r * nout * 2) | (wv & kOob), wo, 0);
+    if constexpr (!(KIND == K_DOWN && PART)) {
+#pragma unroll
+      for (int b = 0; b < MB; ++b) xb[slot][b] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rx, xv[b], st * 64, 0));
+    }
+  };
+  f32x4 acc[NM][CW][MB];
+#pragma unroll
+  for (int m = 0; m < NM; ++m)
+#pragma unroll
+    for (int c = 0; c < CW; ++c)
+#pragma unroll
+      for (int b = 0; b < MB; ++b) acc[m][c][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int a = 0; a < kAhead; ++a) load(a, beg + wave + a * NW);
+  if constexpr (KIND == K_DOWN && PART) {
+    // h of all rows from the parts of its projections, while the weights are on their way
+    constexpr int P = RELU2 ? 1 : 2;
+    const int plane = A.N * ksum;
+    for (int at = threadIdx.x * 4; at < plane; at += 64 * NW * 4) {
+      f32x4 g = {0.f, 0.f, 0.f, 0.f}, u = g;
+      const float* p = A.part + at;
+#pragma unroll 4
+      for (int k = 0; k < split; ++k) {
+        if constexpr (!RELU2) g += *(const f32x4*)p;
+        u += *(const f32x4*)(p + (P - 1) * plane);
+        p += P * plane;
+      }
+      *(uint2*)(hidden + at) = pack4(activate<RELU2>(g, u));
+    }
+    __syncthreads();
+  }
+  for (int st0 = beg + wave; st0 < steps; st0 += kAhead * NW) {
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+      if (st0 + a * NW >= steps) break;
+      if constexpr (KIND == K_DOWN && PART)  // rows past the last one are the last one's: not stored
+        xb[a][0] = *(const u32x4*)(hidden + (n16 < A.N ? n16 : A.N - 1) * ksum + (st0 + a * NW) * 32 + kg * 8);
+#pragma unroll
+      for (int m = 0; m < NM; ++m)
+#pragma unroll
+        for (int c = 0; c < CW; ++c) {
+          u32x4 w;
+#pragma unroll
+          for (int d = 0; d < 4; ++d)
+            w[d] = __builtin_amdgcn_perm(wb[a][m][2 * d + 1], wb[a][m][2 * d], c ? 0x07060302u : 0x05040100u);
+#pragma unroll
+          for (int b = 0; b < MB; ++b)
+            acc[m][c][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, xb[a][b]), acc[m][c][b], 0, 0, 0);
+        }
+      load(a, st0 + (kAhead + a) * NW);
+    }
+  }
+
+  // lane -> row (lane & 15) of a block of 16, columns kg * 4 CW + i CW + c
+#pragma unroll
+  for (int b = 0; b < MB; ++b) {
+    if (b * 16 >= A.N) break;
+    if (b) __syncthreads();
+#pragma unroll
+    for (int m = 0; m < NM; ++m)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < CW; ++c) red[wave][m][n16 * kPad + kg * 4 * CW + i * CW + c] = acc[m][c][b][i];
+    __syncthreads();
+    for (int o = threadIdx.x; o < 16 * kCols; o += 64 * NW) {
+      const int r = o / kCols, c = o % kCols, row = b * 16 + r;
+      if (row >= A.N || c0 + c >= nout) continue;
+      float s[NM];
+#pragma unroll
+      for (int m = 0; m < NM; ++m) {
+        s[m] = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) s[m] += red[w][m][r * kPad + c];
+      }
+      const int64_t at = (int64_t)row * nout + c0 + c;
+      if constexpr (KIND == K_UP && PART) {
+#pragma unroll
+        for (int m = 0; m < NM; ++m) A.part[(int64_t)(y * NM + m) * A.N * nout + at] = s[m];
+      } else if constexpr (KIND == K_UP) {
+        const f32x4 g = {s[0], 0.f, 0.f, 0.f}, u = {s[NM - 1], 0.f, 0.f, 0.f};
+        A.h[at] = (uint16_t)bf16_bits(activate<RELU2>(g, u)[0]);
+        if (A.u) {
+          if constexpr (!RELU2) A.g[at] = s[0];
+          A.u[at] = s[NM - 1];
+        }
+      } else {
+        A.y[at] = (uint16_t)bf16_bits(s[0]);
+      }
+    }
+  }
+}
+
+template <bool RELU2, int MB, int NW, bool PART>
+hipError_t run_few(const FfnArgs& A, int split, hipStream_t s) {
+  const int up = (A.I + 31) / 32, down = (A.H + 31) / 32;
+  k_ffn_few<K_UP, RELU2, MB, NW, PART><<<dim3((unsigned)((up + 7) / 8 * 8), split), dim3(64 * NW), 0, s>>>(A, split);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  // without parts the activation is in h, and both kinds of experts are alike
+  const size_t hidden = PART ? (size_t)A.N * A.I * 2 : 0;
+  k_ffn_few<K_DOWN, RELU2 && PART, MB, NW, PART><<<dim3((unsigned)((down + 7) / 8 * 8)), dim3(64 * NW), hidden, s>>>(A, split);
+  return hipGetLastError();
+}
+
+template <bool RELU2>
+hipError_t run_few_act(const FfnArgs& A, int cus, hipStream_t s) {
+  const int split = A.u ? 1 : few_split(A.N, A.H, A.I, cus);
+  if (split > 1) return run_few<RELU2, 1, 16, true>(A, split, s);
+  if (A.N <= 16) return run_few<RELU2, 1, 16, false>(A, 1, s);
+  return A.N <= 32 ? run_few<RELU2, 2, 8, false>(A, 1, s) : run_few<RELU2, 4, 8, false>(A, 1, s);
+}
+
 hipError_t device_cus(int* cus) {
   int dev = 0;
   const hipError_t e = hipGetDevice(&dev);
@@ -649,6 +922,10 @@ hipError_t device_cus(int* cus) {
 hipError_t launch_ffn_forward(const FfnArgs& A, hipStream_t s) {
   int cus = 0;
   hipError_t e = device_cus(&cus);
+  if (few_rows(A.N, A.H, A.I, A.off != nullptr)) {
+    if (e == hipSuccess) e = A.relu2 ? run_few_act<true>(A, cus, s) : run_few_act<false>(A, cus, s);
+    return e;
+  }
   if (e == hipSuccess) e = run_act<K_UP>(A, cus, s);
   if (e == hipSuccess) e = run_act<K_DOWN>(A, cus, s);
   return e;

@@ -116,6 +116,24 @@ inline FfnChoice choose_ffn(const FfnProduct& p, int cus) {
   return best;
 }
 
+// Whether a forward pass takes the kernels for few rows: one launch a product,
+// no join, but 3 TB/s of weights against the tiles' 4.8.
+inline bool few_rows(int32_t N, int32_t H, int32_t I, bool grouped) {
+  return !grouped && N <= 64 && (int64_t)H * I * ((N + 15) / 16) <= (6 << 20);
+}
+
+// Workgroups that share a column group's sum in such a pass over at most 16
+// rows: as many as the chip's CUs allow, up to 8, and at least a step for every
+// wave. Each of the second product's workgroups adds the parts of all of h and
+// holds it in LDS. (One row through 2048 x 1408: the two products take 4.7 and
+// 5.6 us with four parts, 9.4 and 5.8 without.)
+inline int few_split(int32_t N, int32_t H, int32_t I, int cus) {
+  if (N > 16 || (int64_t)N * I > 32768) return 1;
+  int s = 1;
+  while (s < 8 && (I + 31) / 32 * (2 * s) <= cus && H / 32 >= 16 * 2 * s) s *= 2;
+  return s;
+}
+
 }  // namespace cardan
 
 #endif  // CARDAN_FFN_PLAN_H

@@ -108,9 +108,8 @@ def test_ffn_backward_refusals(C):
 
 
 def _distill(C, N=2, V=100, K=4, typ=0, logits=FAKE, ld=100, teacher=FAKE, ids=FAKE, labels=None, T=1.0, c=0.0, w=None,
-             loss=FAKE, d=None, dld=0, ws=FAKE, nbytes=1 << 40):
-    return C.lib().cardan_distill_loss(N, V, K, typ, logits, ld, teacher, ids, labels, T, c, w, loss, d, dld, ws,
-                                       nbytes, None)
+             loss=FAKE, d=None, dld=0):
+    return C.lib().cardan_distill_loss(N, V, K, typ, logits, ld, teacher, ids, labels, T, c, w, loss, d, dld, None)
 
 
 def test_distill_refusals(C):
@@ -132,8 +131,6 @@ def test_distill_refusals(C):
     assert _distill(C, d=ODD, dld=100) == -6
     assert _distill(C, labels=FAKE + 2) == -6 and _distill(C, w=FAKE + 1) == -6
     assert _distill(C, N=0, logits=None, loss=None) == 0
-    assert C.lib().cardan_distill_workspace_bytes(-1, ctypes.byref(ctypes.c_size_t())) == -2
-    assert C.lib().cardan_distill_workspace_bytes(1, None) == -1
 
 
 def test_binding_refuses(C):
