@@ -4,13 +4,19 @@ This is the training-free initialisation of the hybrid representation
 (Sec. 3.3): product quantisation of the expert matrices into one shared code
 book per projection and private index maps, then the closed-form whitened
 shared-basis correction of the post-VQ residuals (Appendix A.1, Eq. (4)-(6)),
-optionally with the route-aware expert weights ``w_e``. The paper's
-end-to-end distillation (Eq. (3)) needs a trained model and is not here.
+optionally with the route-aware expert weights ``w_e``. It runs on the host
+in float64 (numpy); the result is a layer dict in the storage formats the
+kernels read (bf16 bit patterns, uint8 codes, keys of ``cardan_layer``), so a
+fitted layer goes through the same library calls as any other.
 
-Everything runs on the host in float64 (numpy); the result is a layer dict
-in the storage formats the kernels read (bf16 bit patterns, uint8 codes,
-keys of ``cardan_layer``), so a fitted layer goes through the same library
-calls as any other.
+The second stage, distillation (Sec. 3.3, Eq. (3)), trains the code books,
+bases and coefficients of such a layer on a GPU (``TrainedLayer``,
+``distill_layer``): the experts run as dense bf16 matrices through the
+library's feed-forward block and its gradients, and the logits behind the
+layer are held against a teacher's kept top logits by its distillation loss.
+Index maps and routing stay as they are. Reading: the paper trains a whole
+model end to end; here the model behind the layer is one matrix to logits, or
+whatever produces the gradient of the layer's output.
 
 Layouts (as the kernels read them):
 
@@ -351,3 +357,185 @@ def fit_layer(dense: dict, router_w, router_bias, X_calib, k: int, d: int, K: in
     rep.factors = factors
     rep.Q = Q
     return layer, rep
+
+
+# --------------------------------------------------------------------------
+# distillation (Sec. 3.3, Eq. (3)), on a GPU
+# --------------------------------------------------------------------------
+FACTORS = ("cb_gate", "cb_up", "cb_down", "U_gate", "U_up", "V_gate", "V_up", "A_down", "B_down")
+
+
+class TrainedLayer:
+    """A compressed layer whose code books and low-rank factors are trained.
+
+    ``layer`` is a layer dict (``fit_layer``, ``synth.make_layer``); its factors
+    become float32 tensors on ``device`` (``factors``, the master copies), its
+    codes and router stay fixed. ``forward`` runs rows of any number and keeps
+    what ``backward`` needs; ``backward`` returns the gradient of every factor.
+    One basis shared by gate and up (``U_up is U_gate``) is one factor,
+    ``U_up``."""
+
+    def __init__(self, layer: dict, k: int, d: int, act: str = "silu_glu", device="cuda"):
+        import torch
+
+        from . import cardan
+        if act not in ACTIVATIONS:
+            raise ValueError(f"unknown activation {act!r}")
+        self.k, self.d, self.act = k, d, act
+        self.gated = act == "silu_glu"
+        self.device = torch.empty(0, device=device).device
+        self.shared = self.gated and layer["U_gate"] is layer["U_up"]
+        skip = () if self.gated else ("cb_gate", "U_gate", "V_gate")
+        self.factors = {n: cardan.bf16_tensor(layer[n], self.device).float() for n in FACTORS
+                        if n not in skip and layer.get(n) is not None and not (n == "U_gate" and self.shared)}
+        self.router_w = cardan.bf16_tensor(layer["router_w"], self.device)
+        bias = layer.get("router_bias")
+        self.router_bias = None if bias is None else torch.as_tensor(bias, device=self.device)
+        # blocks in the order of their code words, for the sums over a word's blocks
+        self.codes, self._order, self._count = {}, {}, {}
+        for p in self._projections() + ["down"]:
+            J = torch.as_tensor(np.ascontiguousarray(layer["codes_" + p])).to(self.device).long()
+            self.codes[p] = J
+            self._order[p] = torch.argsort(J.reshape(-1), stable=True)
+            self._count[p] = torch.bincount(J.reshape(-1), minlength=self.factors["cb_" + p].shape[0])
+        self._kept = None
+
+    def _projections(self):
+        return ["gate", "up"] if self.gated else ["up"]
+
+    def _lowrank(self, p):
+        """The two factors of a projection's low-rank term ([.., n_in, r], [.., r, n_out])."""
+        if p == "down":
+            return "A_down", "B_down"
+        return ("U_up" if self.shared else "U_" + p), "V_" + p
+
+    def dense(self, p):
+        """Expert matrices of projection ``p`` ([E, n_in, n_out] bf16): decoded
+        code words plus the low-rank term, summed in float32."""
+        import torch
+        J = self.codes[p]
+        E, nb, n_out = J.shape
+        W = self.factors["cb_" + p][J].permute(0, 1, 3, 2).reshape(E, nb * self.d, n_out)
+        left, right = self._lowrank(p)
+        if left in self.factors:
+            W = W + torch.matmul(self.factors[left], self.factors[right])
+        return W.to(torch.bfloat16)
+
+    def route(self, x):
+        """Top-k experts (descending logit, ties to the lower index) and their
+        softmax affinities, from float64 logits."""
+        import torch
+        logits = x.double() @ self.router_w.double()
+        if self.router_bias is not None:
+            logits = logits + self.router_bias.double()
+        val, idx = torch.sort(logits, dim=1, descending=True, stable=True)
+        return idx[:, :self.k], torch.softmax(val[:, :self.k], 1).float()
+
+    def forward(self, x):
+        """Layer output [N, H] float32 for rows x [N, H] bf16."""
+        import torch
+
+        from . import cardan
+        N, H = x.shape
+        E = self.codes["up"].shape[0]
+        idx, a = self.route(x)
+        order = torch.argsort(idx.reshape(-1), stable=True)      # rows of an expert together
+        rows, a = order // self.k, a.reshape(-1)[order]
+        offsets = torch.zeros(E + 1, dtype=torch.int32, device=self.device)
+        offsets[1:] = torch.bincount(idx.reshape(-1), minlength=E).cumsum(0)
+        W = {p: self.dense(p) for p in self._projections() + ["down"]}
+        xe = x[rows].contiguous()
+        ye, saved = cardan.ffn_forward(xe, W.get("gate"), W["up"], W["down"], offsets=offsets, act=self.act, save=True)
+        # every row has k outputs: add them in the order of its selections
+        y = torch.empty_like(ye)
+        y[order] = ye
+        part = y.view(N, self.k, H).float() * torch.empty_like(a).index_copy_(0, order, a).view(N, self.k, 1)
+        self._kept = (xe, rows, a, offsets, W, saved)
+        return part.sum(1)
+
+    def backward(self, dy):
+        """Gradients of the factors for the gradient dy [N, H] of the last
+        ``forward``'s output."""
+        import torch
+
+        from . import cardan
+        if self._kept is None:
+            raise RuntimeError("backward needs a forward pass")
+        xe, rows, a, offsets, W, saved = self._kept
+        dye = (dy.float()[rows] * a[:, None]).to(torch.bfloat16)
+        _, dg, du, dd = cardan.ffn_backward(dye, xe, W.get("gate"), W["up"], W["down"], saved, offsets=offsets,
+                                            act=self.act, need_dx=False)
+        grads = {}
+        for p, dW in (("gate", dg), ("up", du), ("down", dd)):
+            if dW is None:
+                continue
+            dW = dW.float()
+            E, n_in, n_out = dW.shape
+            blocks = dW.view(E, n_in // self.d, self.d, n_out).permute(0, 1, 3, 2).reshape(-1, self.d)
+            grads["cb_" + p] = torch.segment_reduce(blocks[self._order[p]], "sum", lengths=self._count[p], axis=0,
+                                                    initial=0)
+            left, right = self._lowrank(p)
+            if left not in self.factors:
+                continue
+            L, R = self.factors[left], self.factors[right]
+            dl = torch.matmul(dW, R.transpose(-1, -2).contiguous())
+            dr = torch.matmul(L.transpose(-1, -2).contiguous(), dW)
+            for name, g in ((left, dl), (right, dr)):
+                if self.factors[name].dim() == 2:                 # shared by the experts
+                    g = g.sum(0)
+                grads[name] = grads[name] + g if name in grads else g
+        return grads
+
+    def layer(self, like: dict) -> dict:
+        """The layer dict ``like`` with these factors, in storage formats."""
+        out = dict(like)
+        for name, t in self.factors.items():
+            out[name] = to_bf16_bits(t.detach().cpu().numpy())
+        if self.shared:
+            out["U_gate"] = out["U_up"]
+        return out
+
+
+def distill_step(student: TrainedLayer, x, head, teacher, ids, labels=None, temperature: float = 1.0,
+                 ce_weight: float = 0.0, row_weight=None):
+    """One forward and backward pass of Eq. (3): the layer's output times
+    ``head`` [H, V] (bf16) against a teacher's kept logits ``teacher`` [N, K]
+    float32 at the entries ``ids`` [N, K] int32. ``row_weight`` [N] defaults to
+    1 / N. Returns ``(loss [N, 2] as of cardan.distill_loss, gradients of the
+    factors)``."""
+    import torch
+
+    from . import cardan
+    N = x.shape[0]
+    if row_weight is None:
+        row_weight = torch.full((N,), 1.0 / max(1, N), device=x.device)
+    y = student.forward(x)
+    logits = y.to(torch.bfloat16) @ head
+    loss, dlogits = cardan.distill_loss(logits, teacher, ids, labels=labels, temperature=temperature,
+                                        ce_weight=ce_weight, row_weight=row_weight, dlogits=logits)
+    dy = dlogits.float() @ head.float().t().contiguous()
+    return loss, student.backward(dy)
+
+
+def distill_layer(layer: dict, X, head, teacher, ids, k: int, d: int, act: str = "silu_glu", labels=None,
+                  temperature: float = 1.0, ce_weight: float = 0.0, steps: int = 100, rows: int = 4096,
+                  lr: float = 1e-4, seed: int = 0, device="cuda"):
+    """Distillation of a fitted layer (Sec. 3.3, Eq. (3)): ``steps`` Adam steps
+    on its code books, bases and coefficients over random batches of ``rows`` of
+    the rows ``X`` [N, H] (bf16) with a teacher's kept logits. Returns ``(layer
+    dict in storage formats, mean loss [steps, 2])``."""
+    import torch
+    student = TrainedLayer(layer, k, d, act, device)
+    params = list(student.factors.values())
+    opt = torch.optim.Adam(params, lr=lr)
+    gen = torch.Generator().manual_seed(seed)
+    N, history = X.shape[0], []
+    for _ in range(steps):
+        at = torch.randperm(N, generator=gen)[:rows].to(X.device)
+        loss, grads = distill_step(student, X[at].contiguous(), head, teacher[at].contiguous(), ids[at].contiguous(),
+                                   None if labels is None else labels[at].contiguous(), temperature, ce_weight)
+        for name, t in student.factors.items():
+            t.grad = grads[name]
+        opt.step()
+        history.append(loss.mean(0))
+    return student.layer(layer), torch.stack(history).cpu().numpy() if history else np.zeros((0, 2))
