@@ -281,12 +281,13 @@ int cardan_rmsnorm_bf16(int32_t B, int32_t H, const float* y, float eps,
  * Conventions as above, except: the workspace of the feed-forward calls needs
  * no zero fill and holds nothing between calls (two calls that may overlap in
  * time, two captured graphs among them, need one each); the loss needs none.
- * No workgroup of these kernels waits for another one. The stream's device
- * must be the current one. */
+ * Outputs must not overlap inputs or one another, except as said. No workgroup
+ * of these kernels waits for another one. The stream's device must be the
+ * current one. */
 
 /* Shape of a feed-forward block: E matrix sets (experts) of hidden size H and
  * intermediate size I. H % 64 == 0, I % 32 == 0, 1 <= E <= 1024, H * I * 2
- * below 2^31. */
+ * below 2^31; calls take 0 <= N <= 2^30 rows. */
 typedef struct {
   int32_t H, I, E;
   int32_t act; /* CARDAN_FFN_SILU_GLU or CARDAN_FFN_RELU2_UP */
@@ -363,8 +364,8 @@ enum { CARDAN_LOGITS_BF16 = 0, CARDAN_LOGITS_F32 = 1 };
  * probabilities. -inf logits have probability 0; NaN or +inf among a row's
  * logits give that row NaN. Values between V and the row strides are neither
  * read nor written.
- * 0 <= N, 1 <= V <= 2^30, 0 <= K <= 1024 (teacher and ids may be NULL at
- * K == 0), V <= ld, dld <= 2^40, T > 0 and finite, ce_weight finite. */
+ * 0 <= N <= 2^30, 1 <= V <= 2^30, 0 <= K <= 1024 (teacher and ids may be NULL
+ * at K == 0), V <= ld, dld <= 2^40, 2^-16 <= T <= 2^16, ce_weight finite. */
 int cardan_distill_loss(int32_t N, int32_t V, int32_t K, int32_t logits_type, const void* logits,
                         int64_t ld, const float* teacher, const int32_t* ids,
                         const int32_t* labels, float temperature, float ce_weight,

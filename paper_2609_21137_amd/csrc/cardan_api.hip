@@ -718,7 +718,7 @@ namespace {
 int check_ffn(const cardan_ffn_shape* s, int32_t N) {
   if (!s) return fail(CARDAN_ERR_NULL_PTR, "shape is NULL");
   if (s->H <= 0 || s->I <= 0 || s->E <= 0) return fail(CARDAN_ERR_BAD_SHAPE, "H, I and E must be positive");
-  if (N < 0) return fail(CARDAN_ERR_BAD_SHAPE, "N=%d is negative", N);
+  if (N < 0 || N > (1 << 30)) return fail(CARDAN_ERR_BAD_SHAPE, "N=%d outside [0, 2^30]", N);
   if (s->act != CARDAN_FFN_SILU_GLU && s->act != CARDAN_FFN_RELU2_UP)
     return fail(CARDAN_ERR_UNSUPPORTED, "activation %d is not known", s->act);
   if (s->H % 64) return fail(CARDAN_ERR_UNSUPPORTED, "H=%d must be a multiple of 64", s->H);
@@ -844,7 +844,7 @@ int cardan_distill_loss(int32_t N, int32_t V, int32_t K, int32_t logits_type, co
                         float ce_weight, const float* row_weight, float* loss, void* dlogits, int64_t dld,
                         hipStream_t stream) {
   g_err[0] = 0;
-  if (N < 0 || V < 1 || V > (1 << 30)) return fail(CARDAN_ERR_BAD_SHAPE, "N=%d, V=%d outside the valid range", N, V);
+  if (N < 0 || N > (1 << 30) || V < 1 || V > (1 << 30)) return fail(CARDAN_ERR_BAD_SHAPE, "N=%d, V=%d outside the valid range", N, V);
   if (K < 0 || K > 1024) return fail(CARDAN_ERR_UNSUPPORTED, "K=%d outside [0, 1024]", K);
   if (logits_type != CARDAN_LOGITS_BF16 && logits_type != CARDAN_LOGITS_F32)
     return fail(CARDAN_ERR_UNSUPPORTED, "logits type %d is not known", logits_type);
@@ -852,8 +852,8 @@ int cardan_distill_loss(int32_t N, int32_t V, int32_t K, int32_t logits_type, co
   if (ld < V || ld > most || (dlogits && (dld < V || dld > most)))
     return fail(CARDAN_ERR_BAD_SHAPE, "row strides %lld, %lld are below V=%d or too large", (long long)ld,
                 (long long)dld, V);
-  if (!(temperature > 0.0f) || !isfinite(temperature) || !isfinite(1.0f / temperature) || !isfinite(ce_weight))
-    return fail(CARDAN_ERR_BAD_SHAPE, "temperature must be finite and > 0, ce_weight finite");
+  if (!(temperature >= 1.0f / 65536.0f && temperature <= 65536.0f) || !isfinite(ce_weight))
+    return fail(CARDAN_ERR_BAD_SHAPE, "temperature must lie within [2^-16, 2^16], and ce_weight be finite");
   if (N == 0) return CARDAN_OK;
   REQ(logits, "logits");
   REQ(loss, "loss");

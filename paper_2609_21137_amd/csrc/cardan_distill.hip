@@ -110,7 +110,7 @@ __device__ __forceinline__ float uniform(float v) {
 // lies past them is read again for the gradient, last vectors first (those
 // are still in the caches).
 template <bool F32, int MODE, int NT, int KEEP>
-__global__ __launch_bounds__(NT) void k_distill(const DistillArgs A) {
+__global__ __launch_bounds__(NT) void k_distill(const DistillArgs A, int first) {
   typedef Logits<F32> L;
   constexpr int NV = L::kVec, NW = NT / 64;
   __shared__ float part[3][NW];    // a wave's maximum and sums
@@ -120,7 +120,7 @@ __global__ __launch_bounds__(NT) void k_distill(const DistillArgs A) {
   __shared__ float tp[kMaxTeacher];
   __shared__ int table[kTable];
   __shared__ int flags[3];         // some entry, an entry named twice, the label is an entry
-  const int n = blockIdx.x, tid = threadIdx.x, wave = tid >> 6, V = A.V, K = A.K;
+  const int n = first + blockIdx.x, tid = threadIdx.x, wave = tid >> 6, V = A.V, K = A.K;
   const char* row = static_cast<const char*>(A.logits) + (int64_t)n * A.ld * L::kSize;
   char* grow = A.dlogits ? static_cast<char*>(A.dlogits) + (int64_t)n * A.dld * L::kSize : nullptr;
   const float invT = 1.0f / A.temperature, ct = kLog2e * invT;
@@ -332,8 +332,14 @@ __global__ __launch_bounds__(NT) void k_distill(const DistillArgs A) {
 
 template <bool F32, int MODE, int NT, int KEEP>
 hipError_t run(const DistillArgs& A, hipStream_t s) {
-  k_distill<F32, MODE, NT, KEEP><<<dim3((unsigned)A.N), dim3(NT), 0, s>>>(A);
-  return hipGetLastError();
+  constexpr int kMost = 1 << 21;  // rows of a launch: its threads are counted in 32 bits
+  hipError_t e = hipSuccess;
+  for (int first = 0; first < A.N && e == hipSuccess; first += kMost) {
+    const int rows = A.N - first < kMost ? A.N - first : kMost;
+    k_distill<F32, MODE, NT, KEEP><<<dim3((unsigned)rows), dim3(NT), 0, s>>>(A, first);
+    e = hipGetLastError();
+  }
+  return e;
 }
 
 // A row's vectors are spread over as few threads as keep it in registers, so

@@ -243,6 +243,55 @@ def test_streams_and_graphs(C):
                 assert torch.equal(o, loss) and torch.equal(g, d)
 
 
+def test_labels_alone_and_other_row_strides(C):
+    """No teacher (K = 0) is the cross entropy; a gradient may have rows of its own alignment."""
+    for V, dtype in ((4097, torch.bfloat16), (1003, torch.float32)):
+        N = 7
+        logits, teacher, ids, labels, w = _inputs(N, V, 5, dtype, seed=V)
+        none_t, none_i = teacher[:, :0].contiguous(), ids[:, :0].contiguous()
+        loss, d = C.distill_loss(logits, none_t, none_i, labels=labels, temperature=3.0, ce_weight=1.5, row_weight=w)
+        gone = torch.full_like(ids, -1)
+        want = _oracle(logits, teacher, gone, labels, 3.0, 1.5, w)
+        _check(loss, d, want, dtype)
+        assert (loss[:, 0] == 0).all()
+        l0, d0 = C.distill_loss(logits, teacher, ids, labels=labels, temperature=3.0, ce_weight=1.5, row_weight=w)
+        out = torch.full((N, V + 3), 7.0, dtype=dtype, device="cuda")
+        l1, d1 = C.distill_loss(logits, teacher, ids, labels=labels, temperature=3.0, ce_weight=1.5, row_weight=w,
+                                dlogits=out[:, :V])
+        assert torch.equal(d1, d0) and torch.equal(l0, l1) and (out[:, V:] == 7.0).all()
+
+
+def test_temperatures(C):
+    """From a hard maximum to a flat one."""
+    N, V, K = 5, 2111, 16
+    logits, teacher, ids, labels, w = _inputs(N, V, K, torch.float32, seed=2)
+    for T in (2.0 ** -6, 0.25, 2.0, 64.0):
+        want = _oracle(logits, teacher, ids, labels, T, 0.5, w)
+        loss, d = C.distill_loss(logits, teacher, ids, labels=labels, temperature=T, ce_weight=0.5, row_weight=w)
+        loss_ref, eloss, grad, egrad = want
+        # an exponent's own rounding grows with its size: |s - max| / T 2^-24, up to 24 / T here
+        scale = max(1.0, 1.0 / T)
+        _check(loss, d, (loss_ref, eloss * scale, grad, egrad * scale), torch.float32)
+
+
+def test_refusals(C):
+    logits, teacher, ids, labels, w = _inputs(3, 50, 4, torch.bfloat16, seed=1)
+    with pytest.raises(ValueError):
+        C.distill_loss(logits.t(), teacher, ids)
+    with pytest.raises(ValueError):
+        C.distill_loss(logits, teacher, ids.long())
+    with pytest.raises(ValueError):
+        C.distill_loss(logits, teacher.bfloat16(), ids)
+    with pytest.raises(ValueError):
+        C.distill_loss(logits, teacher, ids[:, :3])
+    with pytest.raises(ValueError):
+        C.distill_loss(logits, teacher, ids, labels=labels.cpu())
+    with pytest.raises(ValueError):
+        C.distill_loss(logits.expand(3, 50)[:1].expand(3, 50), teacher, ids)
+    with pytest.raises(C.CardanError):
+        C.distill_loss(logits, teacher, ids, temperature=0.0)
+
+
 def test_no_rows(C):
     e = torch.empty((0, 100), dtype=torch.bfloat16, device="cuda")
     t = torch.empty((0, 4), device="cuda")

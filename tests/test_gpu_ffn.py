@@ -298,6 +298,42 @@ def test_repeats_and_parts(C):
     assert torch.equal(only, a["dWd"])
 
 
+def test_rows_of_other_groups_stay_out(C):
+    """NaN in one group's rows reaches neither another group's outputs nor its gradients."""
+    H, I, counts = 192, 96, [70, 5, 130, 60]
+    x, dy, Wg, Wu, Wd, off = _inputs(265, 4, H, I, "silu_glu", seed=6, counts=counts)
+    want = _run(C, x, dy, Wg, Wu, Wd, off, "silu_glu")[3]
+    x[70:75] = float("nan")
+    dy[205:] = float("inf")
+    got = _run(C, x, dy, Wg, Wu, Wd, off, "silu_glu")[3]
+    for k in want:
+        if k in ("y", "dx"):
+            assert torch.equal(got[k][:70], want[k][:70]) and torch.equal(got[k][75:205], want[k][75:205])
+        else:
+            assert torch.equal(got[k][0], want[k][0]) and torch.equal(got[k][2], want[k][2])
+
+
+def test_refusals(C):
+    x, dy, Wg, Wu, Wd, off = _inputs(8, 2, 128, 64, "silu_glu", seed=1, counts=[3, 5])
+    with pytest.raises(ValueError):
+        C.ffn_forward(x, Wg, Wu, Wd)                                   # offsets missing
+    with pytest.raises(ValueError):
+        C.ffn_forward(x, Wg, Wu, Wd, offsets=off.long())
+    with pytest.raises(ValueError):
+        C.ffn_forward(x, Wg, Wu, Wd.transpose(1, 2), offsets=off)
+    with pytest.raises(ValueError):
+        C.ffn_forward(x[:, :64], Wg, Wu, Wd, offsets=off)
+    with pytest.raises(ValueError):
+        C.ffn_forward(x.float(), Wg, Wu, Wd, offsets=off)
+    with pytest.raises(C.CardanError):
+        C.ffn_forward(x, Wg, Wu, Wd, offsets=off, ws=torch.empty(16, dtype=torch.uint8, device="cuda"))
+    _, saved = C.ffn_forward(x, Wg, Wu, Wd, offsets=off, save=True)
+    with pytest.raises(ValueError):
+        C.ffn_backward(dy, x, Wg, Wu, Wd, (None, *saved[1:]), offsets=off)
+    with pytest.raises(C.CardanError):
+        C.ffn_backward(dy, x, Wg, Wu, Wd, saved, offsets=off, need_dx=False, need_dw=False)
+
+
 def test_no_rows(C):
     x, dy, Wg, Wu, Wd, _ = _inputs(0, 1, 128, 64, "silu_glu", seed=1)
     y, _, _, got = _run(C, x, dy, Wg, Wu, Wd, None, "silu_glu")

@@ -32,7 +32,7 @@ def _ffn_bytes(C, shape, N):
 
 
 @pytest.mark.parametrize("dims,N,code", [
-    ((2048, 768, 1, 0), -1, -2), ((0, 768, 1, 0), 1, -2), ((2048, -32, 1, 0), 1, -2), ((2048, 768, 0, 0), 1, -2),
+    ((2048, 768, 1, 0), -1, -2), ((2048, 768, 1, 0), (1 << 30) + 1, -2), ((0, 768, 1, 0), 1, -2), ((2048, -32, 1, 0), 1, -2), ((2048, 768, 0, 0), 1, -2),
     ((2048, 768, 1, 2), 1, -3), ((2048, 768, 1, -1), 1, -3), ((2080, 768, 1, 0), 1, -3), ((2048, 784, 1, 0), 1, -3),
     ((2048, 768, 1025, 0), 1, -3), ((32768, 32768, 1, 0), 1, -3),
 ])
@@ -122,8 +122,9 @@ def test_distill_refusals(C):
     assert _distill(C, ld=99) == -2
     assert _distill(C, d=FAKE + 4096, dld=99) == -2
     assert _distill(C, d=FAKE, dld=101) == -2                  # in place with other rows
-    for T in (0.0, -1.0, inf, nan, 1e-45):
+    for T in (0.0, -1.0, inf, nan, 1e-45, 2.0 ** -17, 2.0 ** 17):
         assert _distill(C, T=T) == -2
+    assert _distill(C, N=(1 << 30) + 1) == -2
     assert _distill(C, c=inf) == -2 and _distill(C, c=nan) == -2
     assert _distill(C, logits=None) == -1 and _distill(C, logits=ODD) == -6
     assert _distill(C, teacher=None) == -1 and _distill(C, ids=None) == -1
