@@ -28,7 +28,8 @@ constexpr uint32_t kSpan = 0x7fffff00u;    // largest resource
 struct TileGrid {
   int32_t col_tiles;  // tiles along the output's columns
   int32_t row_tiles;  // along its rows (weight gradients; others count their groups' rows)
-  int32_t split;      // parts of the sum
+  int32_t full;       // tiles before the split ones
+  int32_t split;      // parts of each split tile; 1: none is split
 };
 
 __device__ __forceinline__ u32x4 make_rsrc(const void* base, int64_t bytes) {
@@ -295,15 +296,142 @@ __device__ __forceinline__ void put_lines(char* p, int64_t row_bytes, int r8, in
   if (r8 + 8 < end) put16<NT>(p + 8 * row_bytes, s1);
 }
 
+// A tile's outputs: group, first row and end of rows, first column, and which
+// of dWg (0) and dWu (1).
+struct Place {
+  int e, row, end, n0, mat;
+};
+
+template <int KIND, bool RELU2, int BM, int BN>
+__device__ __forceinline__ Place place(const FfnArgs& A, const TileGrid& G, const int* cum, int tm, int id) {
+  constexpr int kMats = KIND == K_DWI && !RELU2 ? 2 : 1, BC = KIND == K_UP && !RELU2 ? BN / 2 : BN;
+  Place P;
+  P.mat = 1;
+  if constexpr (KIND == K_DWI || KIND == K_DWD) {
+    // tiles of one group's gradients after another; gate and up in turn
+    const int of = G.row_tiles * G.col_tiles * kMats;
+    P.e = id / of;
+    int t = id - P.e * of;
+    if (kMats == 2) P.mat = t & 1;
+    t /= kMats;
+    P.row = t / G.col_tiles * BM;
+    P.n0 = t % G.col_tiles * BC;
+    P.end = KIND == K_DWI ? A.H : A.I;
+  } else {
+    // 8 row tiles by all column tiles at a time
+    const int band = id / (8 * G.col_tiles), in = id - band * 8 * G.col_tiles;
+    const int rows8 = tm - band * 8 < 8 ? tm - band * 8 : 8;
+    P.n0 = in / rows8 * BC;
+    locate(A, BM, cum, band * 8 + in % rows8, P.e, P.row, P.end);
+  }
+  return P;
+}
+
+// The epilogue of one row of 16x16 blocks: output rows row16 .. row16 + 15,
+// columns from wcol. Lane -> output row (lane & 15), columns (lane >> 4) * 4 + 0..3
+// of a block. `in`: the projections that K_DH needs, of fetch().
+template <int KIND, bool RELU2, int NF>
+struct Emit {
+  static constexpr bool kDual = KIND == K_UP && !RELU2, kDW = KIND == K_DWI || KIND == K_DWD;
+  static constexpr int NC = kDual ? NF / 2 : NF;  // 16-column blocks of the output
+  static constexpr int kIn = KIND == K_DH ? NC : 1, kGu = KIND == K_DH && !RELU2 ? 2 : 1;
+
+  static __device__ __forceinline__ void fetch(const FfnArgs& A, const Place& P, int row16, int wcol, int nout, f32x4 (&in)[kIn][kGu]) {
+    if constexpr (KIND == K_DH) {
+      const int lane = threadIdx.x & 63, r = min(row16 + (lane & 15), P.end - 1);
+      const int64_t rb = (int64_t)r * nout + (lane >> 4) * 4;
+#pragma unroll
+      for (int j = 0; j < NC; ++j) {
+        const int c = wcol + j * 16 < nout ? wcol + j * 16 : wcol;
+        in[j][0] = __builtin_nontemporal_load((const f32x4*)(A.u + rb + c));
+        if constexpr (!RELU2) in[j][1] = __builtin_nontemporal_load((const f32x4*)(A.g + rb + c));
+      }
+    }
+  }
+
+  static __device__ __forceinline__ void put(const FfnArgs& A, const Place& P, int row16, int wcol, int nout, const f32x4 (&acc)[NF], const f32x4 (&in)[kIn][kGu]) {
+    const int lane = threadIdx.x & 63, q4 = (lane >> 4) * 4;
+    uint16_t* o0 = KIND == K_UP ? A.h : KIND == K_DH ? A.du : KIND == K_DOWN ? A.y : KIND == K_DX ? A.dx
+                 : (KIND == K_DWD ? A.dWd : P.mat ? A.dWu : A.dWg) + (int64_t)P.e * A.H * A.I;
+    uint2 v0[NC], v1[NC];
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      if constexpr (KIND == K_UP) {
+        v0[j] = pack4(activate<RELU2>(acc[j], acc[kDual ? j + NC : j]));
+      } else if constexpr (KIND == K_DH) {
+        f32x4 dg, du;
+        activate_grad<RELU2>(acc[j], in[j][kGu - 1], in[j][0], dg, du);
+        v0[j] = pack4(du);
+        if constexpr (!RELU2) v1[j] = pack4(dg);
+      } else {
+        v0[j] = pack4(acc[j]);
+      }
+    }
+    const int r = row16 + (lane & 15), r8 = row16 + (lane & 7), high = lane >> 3 & 1;
+    const int64_t rb = (int64_t)r * nout, rb8 = (int64_t)r8 * nout;
+    const auto bits = [](f32x4 v) { return __builtin_bit_cast(u32x4, v); };
+    if constexpr (KIND == K_UP && NC % 2 == 0) {  // kept projections: pieces are blocks of 16 float32
+      if (A.u) {
+#pragma unroll
+        for (int j = 0; j < NC; j += 2) {
+          if (wcol + j * 16 >= nout) continue;
+          const int64_t at = rb8 + wcol + j * 16 + high * 16 + q4;
+          constexpr int U = kDual ? NC : 0;
+          if constexpr (!RELU2) put_lines<true>((char*)(A.g + at), (int64_t)nout * 4, r8, P.end, bits(acc[j]), bits(acc[j + 1]));
+          put_lines<true>((char*)(A.u + at), (int64_t)nout * 4, r8, P.end, bits(acc[U + j]), bits(acc[U + j + 1]));
+        }
+      }
+    } else if constexpr (KIND == K_UP) {
+      static_assert(NC == 1, "blocks come in pairs or alone");
+      if (r < P.end && A.u && wcol < nout) {
+        if constexpr (!RELU2) *(f32x4*)(A.g + rb + wcol + q4) = acc[0];
+        *(f32x4*)(A.u + rb + wcol + q4) = acc[kDual ? NC : 0];
+      }
+    }
+    if constexpr (NC % 2 == 0) {  // pieces are pairs of bf16 blocks, two where both lie inside
+#pragma unroll
+      for (int j = 0; j < NC; j += 2) {
+        const int c = wcol + j * 16;
+        if (c >= nout) continue;
+        if constexpr (NC % 4 == 0) {
+          if (j % 4 == 2 && c < nout) continue;  // stored with the pair before it
+          if (c + 32 < nout) {
+            const int64_t at = rb8 + c + high * 32 + pair_col();
+            put_lines<kDW>((char*)(o0 + at), (int64_t)nout * 2, r8, P.end, pair_up(v0[j], v0[j + 1]), pair_up(v0[j + 2], v0[j + 3]));
+            if constexpr (KIND == K_DH && !RELU2)
+              put_lines<false>((char*)(A.dg + at), (int64_t)nout * 2, r8, P.end, pair_up(v1[j], v1[j + 1]), pair_up(v1[j + 2], v1[j + 3]));
+            continue;
+          }
+        }
+        const u32x4 a = pair_up(v0[j], v0[j + 1]);
+        if (r < P.end) put16<false>(o0 + rb + c + pair_col(), a);
+        if constexpr (KIND == K_DH && !RELU2) {
+          const u32x4 b = pair_up(v1[j], v1[j + 1]);
+          if (r < P.end) put16<false>(A.dg + rb + c + pair_col(), b);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < NC; ++j) {
+        const int c = wcol + j * 16;
+        if (c >= nout || r >= P.end) continue;
+        *(uint2*)(o0 + rb + c + q4) = v0[j];
+        if constexpr (KIND == K_DH && !RELU2) *(uint2*)(A.dg + rb + c + q4) = v1[j];
+      }
+    }
+  }
+};
+
 // Output tiles [BM x BN] of one product. WM x WN waves; a wave holds
 // (BM / WM) x (BN / WN) outputs as 16x16 blocks whose columns are the output's
 // rows, so a lane has four consecutive columns of one row.
 //
-// Workgroups take units (part of the sum, tile) in turn. Loads run NS steps of
+// Workgroups take units (a tile, or a part of a split tile's sum) in turn. Loads run NS steps of
 // 64 ahead of the products, through the end of a unit into the next one, so
 // only a workgroup's first unit waits for memory and an epilogue's stores and
 // reads overlap the next unit's loads. A unit that is one of several parts
-// writes its float32 partial output, which k_ffn_join adds in order.
+// writes its float32 partial output, in the order of the accumulators, and
+// k_ffn_join adds the parts in order.
 template <int KIND, bool RELU2, int BM, int BN, int WM, int WN, int NS>
 __global__ __launch_bounds__(64 * WM * WN, 2) void k_ffn(const FfnArgs A, const TileGrid G) {
   constexpr int NW = WM * WN;
@@ -332,64 +460,57 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_ffn(const FfnArgs A, const 
   // units of this workgroup: workgroups go round robin over the 8 XCDs; an XCD
   // takes runs of neighbouring tiles, which share operands in its L2
   const int tm = kDW ? G.row_tiles * kMats * A.E : count_tiles(A, BM, cum);
-  const int tiles = tm * G.col_tiles, units = tiles * G.split;
+  const int tiles = tm * G.col_tiles, full = G.split > 1 ? G.full : tiles;
+  const int rest = tiles - full, units = full + rest * G.split;
   const int per = gridDim.x >> 3;
   const int stride = gridDim.x, first = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
 
-  struct Unit {  // where a unit's operands are, and its output
+  struct Unit {  // where a unit's operands are
     const char *a, *b, *a1, *b1;
-    int64_t ab, bb;       // bytes from there to the operand's end
-    int k, kend, kt1;     // next step, end, and steps of a phase
-    int e, row, end, n0, mat, part;
+    int64_t ab, bb;    // bytes from there to the operand's end
+    int k, kend, kt1;  // next step, end, and steps of a phase
+    int slot;          // of its partial output, or -1
+    Place p;
   };
   auto setup = [&](int u, Unit& U) {
-    U.part = G.split > 1 ? u / tiles : 0;
-    const int id = u - U.part * tiles;
+    int id = u, part = 0, parts = 1;
+    U.slot = -1;
+    if (u >= full) {
+      U.slot = u - full;
+      part = U.slot / rest;
+      parts = G.split;
+      id = full + U.slot - part * rest;
+    }
+    U.p = place<KIND, RELU2, BM, BN>(A, G, cum, tm, id);
     if constexpr (kDW) {
-      // tiles of one group's gradients after another; gate and up in turn
-      const int of = G.row_tiles * G.col_tiles * kMats;
-      U.e = id / of;
-      int t = id - U.e * of;
-      U.mat = kMats == 2 ? t & 1 : 1;
-      t /= kMats;
       // (a scalar load: a vector load's wait would be one for the stores of the
       // unit before, too)
       int lo = 0, hi = A.N;
       if (A.off) {
         const auto* off = (const __attribute__((address_space(4))) int32_t*)A.off;
-        lo = clampi(off[U.e], 0, A.N);
-        hi = clampi(off[U.e + 1], lo, A.N);
+        lo = clampi(off[U.p.e], 0, A.N);
+        hi = clampi(off[U.p.e + 1], lo, A.N);
       }
       const int rows = hi - lo;
-      U.row = t / G.col_tiles * BM;
-      U.n0 = t % G.col_tiles * BN;
-      U.end = mout;
-      U.a = (const char*)((KIND == K_DWD ? A.h : A.x) + (int64_t)lo * lda + U.row);
-      U.b = (const char*)((KIND == K_DWD ? A.dy : U.mat ? A.du : A.dg) + (int64_t)lo * ldb + U.n0);
-      U.ab = ((int64_t)rows * lda - U.row) * 2;
-      U.bb = ((int64_t)rows * ldb - U.n0) * 2;
+      U.a = (const char*)((KIND == K_DWD ? A.h : A.x) + (int64_t)lo * lda + U.p.row);
+      U.b = (const char*)((KIND == K_DWD ? A.dy : U.p.mat ? A.du : A.dg) + (int64_t)lo * ldb + U.p.n0);
+      U.ab = ((int64_t)rows * lda - U.p.row) * 2;
+      U.bb = ((int64_t)rows * ldb - U.p.n0) * 2;
       U.kt1 = rows > 0 ? (rows + 63) >> 6 : 1;  // a group without rows: one step of zeros
-      U.k = 0;
-      U.kend = U.kt1;
     } else {
-      // 8 row tiles by all column tiles at a time
-      const int band = id / (8 * G.col_tiles), in = id - band * 8 * G.col_tiles;
-      const int rows8 = tm - band * 8 < 8 ? tm - band * 8 : 8;
-      U.n0 = in / rows8 * BC;
-      locate(A, BM, cum, band * 8 + in % rows8, U.e, U.row, U.end);
-      U.ab = (int64_t)(U.end - U.row) * lda * 2;
-      const int64_t ar = (int64_t)U.row * lda;
-      const int64_t w = (int64_t)U.e * H * I + (kBT ? U.n0 : (int64_t)U.n0 * ldb);
+      U.ab = (int64_t)(U.p.end - U.p.row) * lda * 2;
+      const int64_t ar = (int64_t)U.p.row * lda;
+      const int64_t w = (int64_t)U.p.e * H * I + (kBT ? U.p.n0 : (int64_t)U.p.n0 * ldb);
       U.a = (const char*)((KIND == K_UP ? A.x : KIND == K_DOWN ? A.h : KIND == K_DH ? A.dy : kPh == 2 ? A.dg : A.du) + ar);
       U.b = (const char*)((KIND == K_UP || KIND == K_DX ? (RELU2 ? A.Wu : A.Wg) : A.Wd) + w);
-      U.bb = kBT ? ((int64_t)ksum * ldb - U.n0) * 2 : (int64_t)(nout - U.n0) * ldb * 2;
+      U.bb = kBT ? ((int64_t)ksum * ldb - U.p.n0) * 2 : (int64_t)(nout - U.p.n0) * ldb * 2;
       if constexpr (kPh == 2) U.a1 = (const char*)(A.du + ar);
       if constexpr (kPh == 2 || kDual) U.b1 = (const char*)(A.Wu + w);
       U.kt1 = (ksum + 63) >> 6;
-      const int64_t all = (int64_t)U.kt1 * kPh;
-      U.k = (int)(all * U.part / G.split);
-      U.kend = (int)(all * (U.part + 1) / G.split);
     }
+    const int64_t all = (int64_t)U.kt1 * kPh;
+    U.k = (int)(all * part / parts);
+    U.kend = (int)(all * (part + 1) / parts);
   };
 
   OpA opa;
@@ -460,124 +581,24 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_ffn(const FfnArgs A, const 
     }
   };
 
-  // lane -> output row (lane & 15) of a block, columns (lane >> 4) * 4 + 0..3
+  typedef Emit<KIND, RELU2, NF> Out;
   auto epilogue = [&](const Unit& C, int wrow, int wcol) {
-    constexpr int NC = kDual ? NF / 2 : NF;  // 16-column blocks of the output
-    const int r0 = wrow + (lane & 15), q4 = (lane >> 4) * 4;
-    if (!kDW && G.split > 1) {
-      const int64_t plane = (int64_t)A.N * nout;
-      float* part = A.part + C.part * plane * (kDual ? 2 : 1);
+    if (C.slot >= 0) {
+      float* p = A.part + ((int64_t)C.slot * NW + wave) * (MF * NF * 256) + lane * 4;
 #pragma unroll
-      for (int i = 0; i < MF; ++i) {
-        const int r = r0 + i * 16;
-        if (r >= C.end) continue;
-        float* p = part + (int64_t)r * nout + q4;
+      for (int i = 0; i < MF; ++i)
 #pragma unroll
-        for (int j = 0; j < NC; ++j) {
-          const int c = wcol + j * 16;
-          if (c >= nout) continue;
-          *(f32x4*)(p + c) = acc[i][j];
-          if constexpr (kDual) *(f32x4*)(p + c + plane) = acc[i][j + NC];
-        }
-      }
+        for (int j = 0; j < NF; ++j) *(f32x4*)(p + (i * NF + j) * 256) = acc[i][j];
       return;
     }
-    // the projections that a gradient block needs are read one block row ahead
-    constexpr int kIn = KIND == K_DH ? NC : 1, kGu = KIND == K_DH ? (RELU2 ? 1 : 2) : 1;
-    f32x4 in[2][kIn][kGu];
-    auto fetch = [&](int i) {
-      if constexpr (KIND == K_DH) {
-        const int r = r0 + i * 16 < C.end ? r0 + i * 16 : C.end - 1;
-        const int64_t rb = (int64_t)r * nout + q4;
-#pragma unroll
-        for (int j = 0; j < NC; ++j) {
-          const int c = wcol + j * 16 < nout ? wcol + j * 16 : wcol;
-          in[i & 1][j][0] = __builtin_nontemporal_load((const f32x4*)(A.u + rb + c));
-          if constexpr (!RELU2) in[i & 1][j][1] = __builtin_nontemporal_load((const f32x4*)(A.g + rb + c));
-        }
-      }
-    };
-    uint16_t* o0 = KIND == K_UP ? A.h : KIND == K_DH ? A.du : KIND == K_DOWN ? A.y : KIND == K_DX ? A.dx
-                 : (KIND == K_DWD ? A.dWd : C.mat ? A.dWu : A.dWg) + (int64_t)C.e * H * I;
-    fetch(0);
+    // what a block row needs is read one block row ahead
+    f32x4 in[2][Out::kIn][Out::kGu];
+    Out::fetch(A, C.p, wrow, wcol, nout, in[0]);
 #pragma unroll
     for (int i = 0; i < MF; ++i) {
-      if (i + 1 < MF) fetch(i + 1);
-      if (wrow + i * 16 >= C.end) break;
-      uint2 v0[NC], v1[NC];
-#pragma unroll
-      for (int j = 0; j < NC; ++j) {
-        if constexpr (KIND == K_UP) {
-          v0[j] = pack4(activate<RELU2>(acc[i][j], acc[i][kDual ? j + NC : j]));
-        } else if constexpr (KIND == K_DH) {
-          f32x4 dg, du;
-          activate_grad<RELU2>(acc[i][j], in[i & 1][j][kGu - 1], in[i & 1][j][0], dg, du);
-          v0[j] = pack4(du);
-          if constexpr (!RELU2) v1[j] = pack4(dg);
-        } else {
-          v0[j] = pack4(acc[i][j]);
-        }
-      }
-      const int r = r0 + i * 16, r8 = wrow + i * 16 + (lane & 7), high = lane >> 3 & 1;
-      const int64_t rb = (int64_t)r * nout, rb8 = (int64_t)r8 * nout;
-      if constexpr (KIND == K_UP && NC % 2 == 0) {  // kept projections: pieces are blocks of 16 float32
-        if (A.u) {
-#pragma unroll
-          for (int j = 0; j < NC; j += 2) {
-            if (wcol + j * 16 >= nout) continue;
-            const int64_t at = rb8 + wcol + j * 16 + high * 16 + q4;
-            if constexpr (!RELU2)
-              put_lines<true>((char*)(A.g + at), (int64_t)nout * 4, r8, C.end, __builtin_bit_cast(u32x4, acc[i][j]), __builtin_bit_cast(u32x4, acc[i][j + 1]));
-            put_lines<true>((char*)(A.u + at), (int64_t)nout * 4, r8, C.end, __builtin_bit_cast(u32x4, acc[i][kDual ? j + NC : j]), __builtin_bit_cast(u32x4, acc[i][kDual ? j + 1 + NC : j + 1]));
-          }
-        }
-      } else if constexpr (KIND == K_UP) {
-        if (r < C.end && A.u && wcol < nout) {
-          static_assert(NC == 1, "blocks come in pairs or alone");
-          if constexpr (!RELU2) *(f32x4*)(A.g + rb + wcol + q4) = acc[i][0];
-          *(f32x4*)(A.u + rb + wcol + q4) = acc[i][kDual ? NC : 0];
-        }
-      }
-      if constexpr (NC % 4 == 0) {  // pieces are pairs of bf16 blocks
-#pragma unroll
-        for (int j = 0; j < NC; j += 4) {
-          const int c = wcol + j * 16;
-          if (c >= nout) continue;
-          if (c + 32 < nout) {
-            const int64_t at = rb8 + c + high * 32 + pair_col();
-            put_lines<kDW>((char*)(o0 + at), (int64_t)nout * 2, r8, C.end, pair_up(v0[j], v0[j + 1]), pair_up(v0[j + 2], v0[j + 3]));
-            if constexpr (KIND == K_DH && !RELU2)
-              put_lines<false>((char*)(A.dg + at), (int64_t)nout * 2, r8, C.end, pair_up(v1[j], v1[j + 1]), pair_up(v1[j + 2], v1[j + 3]));
-          } else {
-            const u32x4 a = pair_up(v0[j], v0[j + 1]);
-            if (r < C.end) put16<false>(o0 + rb + c + pair_col(), a);
-            if constexpr (KIND == K_DH && !RELU2) {
-              const u32x4 b = pair_up(v1[j], v1[j + 1]);
-              if (r < C.end) put16<false>(A.dg + rb + c + pair_col(), b);
-            }
-          }
-        }
-      } else if constexpr (NC % 2 == 0) {
-#pragma unroll
-        for (int j = 0; j < NC; j += 2) {
-          const int c = wcol + j * 16;
-          if (c >= nout) continue;
-          const u32x4 a = pair_up(v0[j], v0[j + 1]);
-          if (r < C.end) put16<false>(o0 + rb + c + pair_col(), a);
-          if constexpr (KIND == K_DH && !RELU2) {
-            const u32x4 b = pair_up(v1[j], v1[j + 1]);
-            if (r < C.end) put16<false>(A.dg + rb + c + pair_col(), b);
-          }
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < NC; ++j) {
-          const int c = wcol + j * 16;
-          if (c >= nout || r >= C.end) continue;
-          *(uint2*)(o0 + rb + c + q4) = v0[j];
-          if constexpr (KIND == K_DH && !RELU2) *(uint2*)(A.dg + rb + c + q4) = v1[j];
-        }
-      }
+      if (wrow + i * 16 >= C.p.end) break;
+      if (i + 1 < MF) Out::fetch(A, C.p, wrow + i * 16 + 16, wcol, nout, in[(i + 1) & 1]);
+      Out::put(A, C.p, wrow + i * 16, wcol, nout, acc[i], in[i & 1]);
     }
   };
 
@@ -613,8 +634,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_ffn(const FfnArgs A, const 
     for (int i = 0; i < MF; ++i)
 #pragma unroll
       for (int j = 0; j < NF; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int wrow = C.row + wm * (BM / WM), wcol = C.n0 + wn * (BC / WN);
-    if (wrow < C.end && wcol < nout) {
+    const int wrow = C.p.row + wm * (BM / WM), wcol = C.p.n0 + wn * (BC / WN);
+    if (wrow < C.p.end && wcol < nout) {
       for (int kt = C.k; kt < C.kend; ++kt) {
         half(a0f, b0f, stage, 1, a1f, b1f, false, 0);
         // the next step has landed, and this step's stage has been read by every wave
@@ -640,100 +661,87 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_ffn(const FfnArgs A, const 
     }
 
     epilogue(C, wrow, wcol);
-    stored = wrow + BM / WM <= C.end && wcol + BC / WN <= nout;
+    stored = wrow + BM / WM <= C.p.end && wcol + BC / WN <= nout;
     read_first(stage);
   }
   __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): no load to LDS outlives the workgroup
 }
 
-// Sum of the parts of a split product, in order, and its epilogue.
-template <int KIND, bool RELU2>
-__global__ __launch_bounds__(256) void k_ffn_join(const FfnArgs A, int split) {
-  constexpr bool kDual = KIND == K_UP && !RELU2;
-  const int nout = KIND == K_UP || KIND == K_DH ? A.I : A.H;
-  int lo = 0, hi = A.N, t;
-  if (A.off) {  // rows in no group have no sums
-    group_rows(A, 0, lo, t);
-    group_rows(A, A.E - 1, t, hi);
-  }
-  const int64_t plane = (int64_t)A.N * nout;
-  const int64_t at = (int64_t)lo * nout + ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-  if (at >= (int64_t)hi * nout) return;
-  const float* p = A.part + at;
-  f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
-  const int64_t step = plane * (kDual ? 2 : 1);
-  for (int s0 = 0; s0 < split; s0 += 8) {  // eight parts' loads at once; a part past the end is read as the last
-    f32x4 pa[8], pb[8];
+// Sums of the parts of split tiles, in order, and their epilogue: a workgroup
+// per tile and row of blocks, with the waves of the tile.
+template <int KIND, bool RELU2, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void k_ffn_join(const FfnArgs A, const TileGrid G) {
+  constexpr bool kDW = KIND == K_DWI || KIND == K_DWD;
+  constexpr int NW = WM * WN, MF = BM / WM / 16, NF = BN / WN / 16, BC = KIND == K_UP && !RELU2 ? BN / 2 : BN;
+  extern __shared__ __align__(16) int cum_[];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int nout = KIND == K_UP || KIND == K_DH || KIND == K_DWI ? A.I : A.H;
+  const int tm = kDW ? G.row_tiles * (KIND == K_DWI && !RELU2 ? 2 : 1) * A.E : count_tiles(A, BM, cum_);
+  const int rest = tm * G.col_tiles - G.full, tile = blockIdx.x, i = blockIdx.y;
+  if (tile >= rest) return;
+  const Place P = place<KIND, RELU2, BM, BN>(A, G, cum_, tm, G.full + tile);
+  const int row16 = P.row + wave / WN * (BM / WM) + i * 16, wcol = P.n0 + wave % WN * (BC / WN);
+  if (row16 >= P.end || wcol >= nout) return;
+  typedef Emit<KIND, RELU2, NF> Out;
+  f32x4 in[Out::kIn][Out::kGu];
+  Out::fetch(A, P, row16, wcol, nout, in);
+  const float* p = A.part + ((int64_t)tile * NW + wave) * (MF * NF * 256) + i * NF * 256 + lane * 4;
+  const int64_t step = (int64_t)rest * NW * MF * NF * 256;
+  f32x4 acc[NF];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float* q = p + step * (s0 + k < split ? s0 + k : split - 1);
-      pa[k] = *(const f32x4*)q;
-      if constexpr (kDual) pb[k] = *(const f32x4*)(q + plane);
-    }
+  for (int j = 0; j < NF; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < G.split; s0 += 4) {  // four parts' loads at once; a part past the end is read as the last
+    f32x4 v[4][NF];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      if (s0 + k >= split) break;
-      a += pa[k];
-      if constexpr (kDual) b += pb[k];
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int j = 0; j < NF; ++j) v[k][j] = *(const f32x4*)(p + step * (s0 + k < G.split ? s0 + k : G.split - 1) + j * 256);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (s0 + k >= G.split) break;
+#pragma unroll
+      for (int j = 0; j < NF; ++j) acc[j] += v[k][j];
     }
   }
-  if constexpr (KIND == K_UP) {
-    if constexpr (!RELU2)
-      if (A.g) *(f32x4*)(A.g + at) = a;
-    const f32x4 u = kDual ? b : a;
-    if (A.u) *(f32x4*)(A.u + at) = u;
-    *(uint2*)(A.h + at) = pack4(activate<RELU2>(a, u));
-  } else if constexpr (KIND == K_DH) {
-    f32x4 dg, du;
-    activate_grad<RELU2>(a, RELU2 ? a : *(const f32x4*)(A.g + at), *(const f32x4*)(A.u + at), dg, du);
-    if constexpr (!RELU2) *(uint2*)(A.dg + at) = pack4(dg);
-    *(uint2*)(A.du + at) = pack4(du);
-  } else {
-    *(uint2*)((KIND == K_DOWN ? A.y : A.dx) + at) = pack4(a);
-  }
+  Out::put(A, P, row16, wcol, nout, acc, in);
 }
 
 template <int KIND, bool RELU2, int BM, int BN, int WM, int WN, int NS>
-hipError_t run(const FfnArgs& A, int split, int cus, hipStream_t s) {
+hipError_t run(const FfnArgs& A, const FfnProduct& p, const FfnChoice& c, int cus, hipStream_t s) {
   constexpr bool kDual = KIND == K_UP && !RELU2, kDW = KIND == K_DWI || KIND == K_DWD;
   constexpr int BC = kDual ? BN / 2 : BN;
-  const int nout = KIND == K_UP || KIND == K_DH || KIND == K_DWI ? A.I : A.H;
-  const int mout = KIND == K_DWI ? A.H : A.I;
   TileGrid G;
-  G.col_tiles = (nout + BC - 1) / BC;
-  G.row_tiles = kDW ? (mout + BM - 1) / BM : 0;
-  G.split = split;
+  G.col_tiles = (p.cols + BC - 1) / BC;
+  G.row_tiles = kDW ? (int)((p.rows + BM - 1) / BM) : 0;
   // at most this many tiles (groups end inside tiles); the kernel counts them
-  const int64_t rows = kDW ? (int64_t)G.row_tiles * A.E * (KIND == K_DWI && !RELU2 ? 2 : 1)
-                           : A.off ? A.N / BM + (A.E < A.N ? A.E : A.N) : (A.N + BM - 1) / BM;
-  const int64_t units = rows * G.col_tiles * G.split;
+  const int64_t tiles = ffn_tiles(p, kFfnTiles[c.tile]), rest = c.split > 1 ? tiles - c.full : 0;
+  const int64_t units = tiles + rest * (c.split - 1);
   if (units == 0) return hipSuccess;
   if (units > 0x40000000) return hipErrorInvalidValue;
-  const size_t lds = (size_t)NS * (BM + BN) * 128 + (A.off && !kDW ? (size_t)A.E * 12 : 0);
+  G.full = (int)c.full;
+  G.split = c.split;
+  const size_t list = A.off && !kDW ? (size_t)A.E * 12 : 0, lds = (size_t)NS * (BM + BN) * 128 + list;
   const int fit = (int)(kLdsBytes / lds), wave_fit = 8 / (WM * WN);  // workgroups a CU holds at once
   const int64_t most = (int64_t)cus * (fit < wave_fit ? fit : wave_fit);
   const int64_t per = (std::min(units, most) + 7) / 8;
   k_ffn<KIND, RELU2, BM, BN, WM, WN, NS><<<dim3((unsigned)(8 * per)), dim3(64 * WM * WN), lds, s>>>(A, G);
   hipError_t e = hipGetLastError();
-  if (G.split == 1 || e != hipSuccess) return e;
-  if constexpr (!kDW) {
-    const int64_t vecs = (int64_t)A.N * nout / 4;
-    k_ffn_join<KIND, RELU2><<<dim3((unsigned)((vecs + 255) / 256)), dim3(256), 0, s>>>(A, split);
-    e = hipGetLastError();
-  }
-  return e;
+  if (rest == 0 || e != hipSuccess) return e;
+  k_ffn_join<KIND, RELU2, BM, BN, WM, WN><<<dim3((unsigned)rest, BM / WM / 16), dim3(64 * WM * WN), list, s>>>(A, G);
+  return hipGetLastError();
 }
 
 template <int KIND, bool RELU2>
 hipError_t run_kind(const FfnArgs& A, int cus, hipStream_t s) {
-  const FfnChoice c = choose_ffn(ffn_product((FfnKind)KIND, A.N, A.E, A.H, A.I, !RELU2), cus);
+  const FfnProduct p = ffn_product((FfnKind)KIND, A.N, A.E, A.H, A.I, !RELU2, A.off != nullptr);
+  const FfnChoice c = choose_ffn(p, cus);
   switch (c.tile) {
-    case 0: return run<KIND, RELU2, 256, 256, 2, 4, 2>(A, c.split, cus, s);
-    case 1: return run<KIND, RELU2, 128, 256, 2, 4, 3>(A, c.split, cus, s);
-    case 2: return run<KIND, RELU2, 64, 256, 1, 8, 3>(A, c.split, cus, s);
-    case 3: return run<KIND, RELU2, 128, 128, 2, 2, 2>(A, c.split, cus, s);
-    case 4: return run<KIND, RELU2, 64, 128, 1, 4, 3>(A, c.split, cus, s);
-    default: return run<KIND, RELU2, 32, 128, 1, 4, 4>(A, c.split, cus, s);
+    case 0: return run<KIND, RELU2, 256, 256, 2, 4, 2>(A, p, c, cus, s);
+    case 1: return run<KIND, RELU2, 128, 256, 2, 4, 3>(A, p, c, cus, s);
+    case 2: return run<KIND, RELU2, 64, 256, 1, 8, 3>(A, p, c, cus, s);
+    case 3: return run<KIND, RELU2, 128, 128, 2, 2, 2>(A, p, c, cus, s);
+    case 4: return run<KIND, RELU2, 64, 128, 1, 4, 3>(A, p, c, cus, s);
+    default: return run<KIND, RELU2, 32, 128, 1, 4, 4>(A, p, c, cus, s);
   }
 }
 

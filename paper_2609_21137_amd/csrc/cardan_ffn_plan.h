@@ -20,15 +20,15 @@ enum FfnKind {
   K_DWD = 5    // h^T dy, likewise
 };
 
-// A product of few tiles is split over its sum into at most kMaxSplit parts,
-// whose float32 partial outputs take at most this many bytes for N rows or
-// fewer (the widest output is the 2 I projections or H).
+// The tiles of a product's last round, or all of them where they are few, are
+// split over the sum into at most kMaxSplit parts, whose float32 partial
+// outputs take at most this many bytes for N rows or fewer.
 constexpr int kMaxSplit = 32;
 constexpr size_t kPartialMax = (size_t)64 << 20;
 inline size_t ffn_partial_bytes(int32_t N, int32_t H, int32_t I, bool gated) {
-  const size_t wide = (size_t)(gated ? 2 : 1) * I;
-  const size_t all = (size_t)kMaxSplit * N * ((size_t)H > wide ? (size_t)H : wide) * 4;
-  return all < kPartialMax ? all : kPartialMax;
+  const auto up = [](int64_t v) { return (size_t)((v + 255) / 256 * 256); };
+  const size_t wide = std::max(up(H), up((gated ? 2 : 1) * (int64_t)I));
+  return std::min(kPartialMax, (size_t)kMaxSplit * 4 * std::max(up(N) * wide, (gated ? 2 : 1) * up(H) * up(I)));
 }
 
 // Tiles (output rows x columns), the workgroups that a CU holds of them, and
@@ -52,64 +52,79 @@ constexpr double kStreamBytesUs = 4.5e6;  // bytes per us that weights stream at
 struct FfnProduct {
   int64_t rows, groups, mats;
   int cols;
-  bool dual;      // two products side by side in a tile (gate and up)
-  bool grad;      // a weight gradient: every group has `rows` rows of its own
+  bool dual;   // two products side by side in a tile (gate and up)
+  bool grad;   // a weight gradient: every group has `rows` rows of its own
+  bool known;  // the number of tiles is known on the host
   int64_t steps;
-  int max_split;  // parts that the workspace holds
+  int max_split;
+  size_t partial_bytes;
   double weight_bytes;
 };
 
-inline FfnProduct ffn_product(FfnKind kind, int32_t N, int32_t E, int32_t H, int32_t I, bool gated) {
+inline FfnProduct ffn_product(FfnKind kind, int32_t N, int32_t E, int32_t H, int32_t I, bool gated, bool grouped) {
   const bool grad = kind == K_DWI || kind == K_DWD;
   const bool over_h = kind == K_UP || kind == K_DH;  // the sum runs over H
   const int64_t active = std::max(1, std::min(E, N));
   FfnProduct p;
   p.dual = kind == K_UP && gated;
   p.grad = grad;
+  p.known = grad || !grouped;
   p.cols = over_h || kind == K_DWI ? I : H;
   p.groups = grad ? E : active;
   p.rows = kind == K_DWI ? H : kind == K_DWD ? I : N;
   p.mats = kind == K_DWI && gated ? 2 : 1;
   p.steps = grad ? (N / active + 63) / 64 : ((over_h ? H : I) + 63) / 64 * (kind == K_DX && gated ? 2 : 1);
   p.weight_bytes = (double)p.groups * H * I * 2 * (p.dual || p.mats == 2 || (kind == K_DX && gated) ? 2 : 1);
-  // every part has a step, and its partial outputs a place in the workspace
-  const size_t plane = std::max((size_t)N * p.cols * 4 * (p.dual ? 2 : 1), (size_t)1);
-  const int64_t room = (int64_t)(ffn_partial_bytes(N, H, I, gated) / plane);
-  p.max_split = grad ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(room, p.steps), kMaxSplit));
+  p.partial_bytes = ffn_partial_bytes(N, H, I, gated);
+  // every part has a step (the groups' rows, and so a gradient's steps, are not known here)
+  p.max_split = grad && grouped ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(p.steps, kMaxSplit));
   return p;
 }
 
+// Tiles of a product, at most (groups end inside tiles).
+inline int64_t ffn_tiles(const FfnProduct& p, const FfnTile& t) {
+  const int bc = p.dual ? t.bn / 2 : t.bn;
+  const int64_t cols = (p.cols + bc - 1) / bc, own = (p.rows + t.bm - 1) / t.bm;
+  return cols * (p.grad ? own * p.groups * p.mats : p.known ? own : p.rows / t.bm + p.groups);
+}
+
 struct FfnChoice {
-  int tile, split;
+  int tile;
+  int split;     // parts of each split tile; 1: none is split
+  int64_t full;  // tiles before the split ones
 };
 
-// The tile and split of least estimated time: rounds of units over the chip's
+// The tile and split of least estimated time: rounds of tiles over the chip's
 // slots, each as long as its steps, against the time that the weights take to
-// stream; a split adds its joining kernel and the partial sums' bytes.
-// Groups end inside tiles: half a tile of each is counted as lost.
+// stream. The tiles of a last round that does not fill the slots are split
+// (where their number is known; else all are, or none), which adds the joining
+// kernel and the partial sums' bytes. Groups end inside tiles: half a tile of
+// each is counted as lost.
 inline FfnChoice choose_ffn(const FfnProduct& p, int cus) {
-  FfnChoice best = {0, 1};
+  FfnChoice best = {0, 1, 0};
   double best_us = 1e30;
   for (int t = 0; t < kFfnTileCount; ++t) {
     const FfnTile& T = kFfnTiles[t];
     const int bc = p.dual ? T.bn / 2 : T.bn;
-    const double cols = (double)((p.cols + bc - 1) / bc);
-    const double own = (double)((p.rows + T.bm - 1) / T.bm);
-    const double rows = p.grad ? own * p.groups * p.mats
-                               : p.groups == 1 ? own
-                                               : std::max((double)std::min(p.groups, p.rows), (double)p.rows / T.bm + 0.5 * p.groups);
+    const int64_t most = ffn_tiles(p, T), slots = (int64_t)cus * T.per_cu;
+    const int64_t tiles = p.known ? most
+                                  : (int64_t)(std::max((double)std::min(p.groups, p.rows), (double)p.rows / T.bm + 0.5 * p.groups) *
+                                              ((p.cols + bc - 1) / bc));
     const double unit_us = kUnitUs + kUnitAreaUs * T.bm * T.bn / 65536.0;
     const double stream_us = p.weight_bytes / kStreamBytesUs;
-    for (int s = 1; s <= p.max_split; s = s < 4 ? s + 1 : s * 2) {
-      const double slots = (double)cus * T.per_cu;
-      const double units = rows * cols * s;
-      const double rounds = units <= slots ? 1.0 : (double)(int64_t)((units + slots - 1) / slots);
-      const double work = rounds * (T.step_us * (double)((p.steps + s - 1) / s) + unit_us);
-      const double join = s == 1 ? 0.0 : kJoinUs + s * (double)p.rows * p.cols * (p.dual ? 8.0 : 4.0) / 4.0e6;
+    for (int s = 1; s <= p.max_split; s = s < 8 ? s + 1 : s * 2) {
+      const int64_t full = s == 1 || !p.known ? 0 : tiles / slots * slots;
+      const double bytes = (double)(most - full) * s * T.bm * T.bn * 4.0;
+      if (s > 1 && (most == full || bytes > (double)p.partial_bytes)) continue;
+      const int64_t rest = tiles - full;
+      const double rounds = (double)(full / slots), last = (double)((rest * s + slots - 1) / slots);
+      const double work = rounds * (T.step_us * (double)p.steps + unit_us) +
+                          last * (T.step_us * (double)((p.steps + s - 1) / s) + unit_us);
+      const double join = s == 1 ? 0.0 : kJoinUs + (double)rest * s * T.bm * T.bn * 4.0 / 4.0e6;
       const double us = std::max(work, stream_us) + 0.1 * std::min(work, stream_us) + join;
       if (us < best_us) {
         best_us = us;
-        best = {t, s};
+        best = {t, s, full};
       }
     }
   }

@@ -15,27 +15,35 @@ int main(int argc, char** argv) {
     return (int64_t)(lo * pow(hi / lo, std::uniform_real_distribution<double>(0, 1)(rng)));
   };
   const int n = argc > 1 ? atoi(argv[1]) : 1000;
-  long failures = 0, splits = 0;
+  long failures = 0, splits = 0, tails = 0;
   for (int i = 0; i < n; ++i) {
     const int N = i % 50 == 0 ? 0 : (int)log_uniform(1, 4.0e6);
     const int E = i % 2 ? 1 : (int)log_uniform(1, 1024);
     const int H = 64 * (int)log_uniform(1, 512), I = 32 * (int)log_uniform(1, 1024);
     for (int kind = K_UP; kind <= K_DWD; ++kind)
-      for (bool gated : {false, true}) {
-        const FfnProduct p = ffn_product((FfnKind)kind, N, E, H, I, gated);
-        for (int cus : {304, 256, 1}) {
-          const FfnChoice c = choose_ffn(p, cus);
-          const size_t plane = (size_t)N * p.cols * 4 * (p.dual ? 2 : 1);
-          bool ok = c.tile >= 0 && c.tile < kFfnTileCount && c.split >= 1 && c.split <= kMaxSplit;
-          ok = ok && (c.split == 1 || (!p.grad && c.split <= p.steps && c.split * plane <= ffn_partial_bytes(N, H, I, gated)));
-          // a workspace for more rows holds a call over fewer
-          ok = ok && ffn_partial_bytes(N, H, I, gated) <= ffn_partial_bytes(N + 1, H, I, gated);
-          splits += c.split > 1;
-          if (!ok && ++failures < 20)
-            printf("N=%d E=%d H=%d I=%d kind=%d gated=%d: tile %d split %d\n", N, E, H, I, kind, gated, c.tile, c.split);
+      for (bool gated : {false, true})
+        for (bool grouped : {false, true}) {
+          if (E > 1 && !grouped) continue;
+          const FfnProduct p = ffn_product((FfnKind)kind, N, E, H, I, gated, grouped);
+          for (int cus : {304, 256, 1}) {
+            const FfnChoice c = choose_ffn(p, cus);
+            bool ok = c.tile >= 0 && c.tile < kFfnTileCount && c.split >= 1 && c.split <= kMaxSplit;
+            if (ok && c.split > 1) {
+              const FfnTile& T = kFfnTiles[c.tile];
+              const int64_t most = ffn_tiles(p, T), rest = most - c.full;
+              ok = !(p.grad && grouped) && c.split <= p.steps && rest > 0 && c.full >= 0 && (p.known || c.full == 0);
+              ok = ok && (size_t)rest * c.split * T.bm * T.bn * 4 <= ffn_partial_bytes(N, H, I, gated);
+              ++splits;
+              tails += c.full > 0;
+            }
+            // a workspace for more rows holds a call over fewer
+            ok = ok && ffn_partial_bytes(N, H, I, gated) <= ffn_partial_bytes(N + 1, H, I, gated);
+            if (!ok && ++failures < 20)
+              printf("N=%d E=%d H=%d I=%d kind=%d gated=%d: tile %d split %d full %ld\n", N, E, H, I, kind, gated, c.tile,
+                     c.split, (long)c.full);
+          }
         }
-      }
   }
-  printf("%ld split products, %ld failures\n", splits, failures);
-  return failures != 0 || splits == 0;
+  printf("%ld split products, %ld of them in a last round, %ld failures\n", splits, tails, failures);
+  return failures != 0 || splits == 0 || tails == 0;
 }

@@ -131,6 +131,8 @@ DENSE = [
     (16, 512, 384, "silu_glu"), (17, 512, 352, "silu_glu"), (33, 256, 128, "silu_glu"), (63, 320, 224, "silu_glu"),
     (64, 576, 160, "relu2_up"), (65, 1024, 512, "silu_glu"), (130, 704, 1056, "silu_glu"), (255, 256, 288, "relu2_up"),
     (257, 832, 544, "silu_glu"), (600, 2048, 768, "silu_glu"), (1000, 448, 2080, "relu2_up"), (2049, 1024, 736, "silu_glu"),
+    # more tiles than fit the chip at once, and a last round that does not fill it
+    (8200, 2560, 288, "silu_glu"), (8200, 2560, 224, "relu2_up"), (3000, 640, 4128, "silu_glu"),
 ]
 
 
