@@ -433,7 +433,7 @@ struct Emit {
 // writes its float32 partial output, in the order of the accumulators, and
 // k_ffn_join adds the parts in order.
 template <int KIND, bool RELU2, int BM, int BN, int WM, int WN, int NS>
-__global__ __launch_bounds__(64 * WM * WN, 2) void k_ffn(const FfnArgs A, const TileGrid G) {
+__device__ __forceinline__ void run_units(const FfnArgs& A, const TileGrid& G, int block, int grid) {
   constexpr int NW = WM * WN;
   constexpr bool kDW = KIND == K_DWI || KIND == K_DWD;
   constexpr bool kAT = kDW, kBT = kDW || KIND == K_UP || KIND == K_DOWN;
@@ -462,8 +462,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_ffn(const FfnArgs A, const 
   const int tm = kDW ? G.row_tiles * kMats * A.E : count_tiles(A, BM, cum);
   const int tiles = tm * G.col_tiles, full = G.split > 1 ? G.full : tiles;
   const int rest = tiles - full, units = full + rest * G.split;
-  const int per = gridDim.x >> 3;
-  const int stride = gridDim.x, first = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  const int per = grid >> 3;
+  const int stride = grid, first = (block & 7) * per + (block >> 3);
 
   struct Unit {  // where a unit's operands are
     const char *a, *b, *a1, *b1;
@@ -667,6 +667,25 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_ffn(const FfnArgs A, const 
   __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): no load to LDS outlives the workgroup
 }
 
+template <int KIND, bool RELU2, int BM, int BN, int WM, int WN, int NS>
+__global__ __launch_bounds__(64 * WM * WN, 2) void k_ffn(const FfnArgs A, const TileGrid G) {
+  run_units<KIND, RELU2, BM, BN, WM, WN, NS>(A, G, blockIdx.x, gridDim.x);
+}
+
+// The three products behind dg and du in one launch, for the smallest problems:
+// `at` workgroups for the first, up to at[1] for the second.
+struct GradGrids {
+  TileGrid g[3];
+  int at[3];
+};
+template <bool RELU2, int BM, int BN, int WM, int WN, int NS>
+__global__ __launch_bounds__(64 * WM * WN, 2) void k_ffn_grads(const FfnArgs A, const GradGrids S) {
+  const int b = blockIdx.x;
+  if (b < S.at[0]) run_units<K_DX, RELU2, BM, BN, WM, WN, NS>(A, S.g[0], b, S.at[0]);
+  else if (b < S.at[1]) run_units<K_DWI, RELU2, BM, BN, WM, WN, NS>(A, S.g[1], b - S.at[0], S.at[1] - S.at[0]);
+  else run_units<K_DWD, RELU2, BM, BN, WM, WN, NS>(A, S.g[2], b - S.at[1], S.at[2] - S.at[1]);
+}
+
 // Sums of the parts of split tiles, in order, and their epilogue: a workgroup
 // per tile and row of blocks, with the waves of the tile.
 template <int KIND, bool RELU2, int BM, int BN, int WM, int WN>
@@ -706,28 +725,44 @@ __global__ __launch_bounds__(64 * WM * WN) void k_ffn_join(const FfnArgs A, cons
   Out::put(A, P, row16, wcol, nout, acc, in);
 }
 
+// Grid of a product: its tiles, the number of workgroups and their LDS.
+struct Launch {
+  TileGrid G;
+  int64_t units, rest;
+  int grid;
+  size_t list, lds;  // of the groups' list, and of all
+};
+
+template <int KIND, bool RELU2, int BM, int BN, int WM, int WN, int NS>
+Launch plan(const FfnArgs& A, const FfnProduct& p, const FfnChoice& c, int cus) {
+  constexpr bool kDW = KIND == K_DWI || KIND == K_DWD;
+  constexpr int BC = KIND == K_UP && !RELU2 ? BN / 2 : BN;
+  Launch L;
+  L.G.col_tiles = (p.cols + BC - 1) / BC;
+  L.G.row_tiles = kDW ? (int)((p.rows + BM - 1) / BM) : 0;
+  // at most this many tiles (groups end inside tiles); the kernel counts them
+  const int64_t tiles = ffn_tiles(p, kFfnTiles[c.tile]);
+  L.rest = c.split > 1 ? tiles - c.full : 0;
+  L.units = tiles + L.rest * (c.split - 1);
+  L.G.full = (int)c.full;
+  L.G.split = c.split;
+  L.list = A.off && !kDW ? (size_t)A.E * 12 : 0;
+  L.lds = (size_t)NS * (BM + BN) * 128 + L.list;
+  const int fit = (int)(kLdsBytes / L.lds), wave_fit = 8 / (WM * WN);  // workgroups a CU holds at once
+  const int64_t most = (int64_t)cus * (fit < wave_fit ? fit : wave_fit);
+  L.grid = (int)((std::min(L.units, most) + 7) / 8 * 8);
+  return L;
+}
+
 template <int KIND, bool RELU2, int BM, int BN, int WM, int WN, int NS>
 hipError_t run(const FfnArgs& A, const FfnProduct& p, const FfnChoice& c, int cus, hipStream_t s) {
-  constexpr bool kDual = KIND == K_UP && !RELU2, kDW = KIND == K_DWI || KIND == K_DWD;
-  constexpr int BC = kDual ? BN / 2 : BN;
-  TileGrid G;
-  G.col_tiles = (p.cols + BC - 1) / BC;
-  G.row_tiles = kDW ? (int)((p.rows + BM - 1) / BM) : 0;
-  // at most this many tiles (groups end inside tiles); the kernel counts them
-  const int64_t tiles = ffn_tiles(p, kFfnTiles[c.tile]), rest = c.split > 1 ? tiles - c.full : 0;
-  const int64_t units = tiles + rest * (c.split - 1);
-  if (units == 0) return hipSuccess;
-  if (units > 0x40000000) return hipErrorInvalidValue;
-  G.full = (int)c.full;
-  G.split = c.split;
-  const size_t list = A.off && !kDW ? (size_t)A.E * 12 : 0, lds = (size_t)NS * (BM + BN) * 128 + list;
-  const int fit = (int)(kLdsBytes / lds), wave_fit = 8 / (WM * WN);  // workgroups a CU holds at once
-  const int64_t most = (int64_t)cus * (fit < wave_fit ? fit : wave_fit);
-  const int64_t per = (std::min(units, most) + 7) / 8;
-  k_ffn<KIND, RELU2, BM, BN, WM, WN, NS><<<dim3((unsigned)(8 * per)), dim3(64 * WM * WN), lds, s>>>(A, G);
+  const Launch L = plan<KIND, RELU2, BM, BN, WM, WN, NS>(A, p, c, cus);
+  if (L.units == 0) return hipSuccess;
+  if (L.units > 0x40000000) return hipErrorInvalidValue;
+  k_ffn<KIND, RELU2, BM, BN, WM, WN, NS><<<dim3(L.grid), dim3(64 * WM * WN), L.lds, s>>>(A, L.G);
   hipError_t e = hipGetLastError();
-  if (rest == 0 || e != hipSuccess) return e;
-  k_ffn_join<KIND, RELU2, BM, BN, WM, WN><<<dim3((unsigned)rest, BM / WM / 16), dim3(64 * WM * WN), list, s>>>(A, G);
+  if (L.rest == 0 || e != hipSuccess) return e;
+  k_ffn_join<KIND, RELU2, BM, BN, WM, WN><<<dim3((unsigned)L.rest, BM / WM / 16), dim3(64 * WM * WN), L.list, s>>>(A, L.G);
   return hipGetLastError();
 }
 
@@ -743,6 +778,39 @@ hipError_t run_kind(const FfnArgs& A, int cus, hipStream_t s) {
     case 4: return run<KIND, RELU2, 64, 128, 1, 4, 3>(A, p, c, cus, s);
     default: return run<KIND, RELU2, 32, 128, 1, 4, 4>(A, p, c, cus, s);
   }
+}
+
+// dx and the weights' gradients. Where all three products take the smallest
+// tile unsplit they share a launch, which is most of such a call's time.
+template <bool RELU2>
+hipError_t run_grads(const FfnArgs& A, int cus, hipStream_t s) {
+  const FfnKind kinds[3] = {K_DX, K_DWI, K_DWD};
+  FfnProduct p[3];
+  FfnChoice c[3];
+  bool one = A.N > 0 && A.dx && A.dWu && A.dWd;
+  for (int i = 0; i < 3; ++i) {
+    p[i] = ffn_product(kinds[i], A.N, A.E, A.H, A.I, !RELU2, A.off != nullptr);
+    c[i] = choose_ffn(p[i], cus);
+    one = one && c[i].tile == kFfnTileCount - 1 && c[i].split == 1;
+  }
+  if (one) {
+    const Launch L[3] = {plan<K_DX, RELU2, 32, 128, 1, 4, 4>(A, p[0], c[0], cus),
+                         plan<K_DWI, RELU2, 32, 128, 1, 4, 4>(A, p[1], c[1], cus),
+                         plan<K_DWD, RELU2, 32, 128, 1, 4, 4>(A, p[2], c[2], cus)};
+    GradGrids S;
+    int at = 0;
+    for (int i = 0; i < 3; ++i) {
+      if (L[i].units > 0x40000000) return hipErrorInvalidValue;
+      S.g[i] = L[i].G;
+      S.at[i] = at += L[i].grid;
+    }
+    k_ffn_grads<RELU2, 32, 128, 1, 4, 4><<<dim3(at), dim3(256), L[0].lds, s>>>(A, S);
+    return hipGetLastError();
+  }
+  hipError_t e = A.N > 0 && A.dx ? run_kind<K_DX, RELU2>(A, cus, s) : hipSuccess;
+  if (e == hipSuccess && A.dWu) e = run_kind<K_DWI, RELU2>(A, cus, s);
+  if (e == hipSuccess && A.dWd) e = run_kind<K_DWD, RELU2>(A, cus, s);
+  return e;
 }
 
 template <int KIND>
@@ -943,9 +1011,7 @@ hipError_t launch_ffn_backward(const FfnArgs& A, hipStream_t s) {
   int cus = 0;
   hipError_t e = device_cus(&cus);
   if (e == hipSuccess && A.N > 0 && (A.dx || A.dWu)) e = run_act<K_DH>(A, cus, s);
-  if (e == hipSuccess && A.N > 0 && A.dx) e = run_act<K_DX>(A, cus, s);
-  if (e == hipSuccess && A.dWu) e = run_act<K_DWI>(A, cus, s);
-  if (e == hipSuccess && A.dWd) e = run_act<K_DWD>(A, cus, s);
+  if (e == hipSuccess) e = A.relu2 ? run_grads<true>(A, cus, s) : run_grads<false>(A, cus, s);
   return e;
 }
 
