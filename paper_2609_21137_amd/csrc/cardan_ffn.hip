@@ -54,9 +54,12 @@ __device__ __forceinline__ uint32_t bf16_bits(float f) {
   const __bf16 b = (__bf16)f;
   return (uint32_t)__builtin_bit_cast(unsigned short, b);
 }
-__device__ __forceinline__ uint2 pack4(f32x4 v) {
-  return make_uint2(bf16_bits(v[0]) | bf16_bits(v[1]) << 16, bf16_bits(v[2]) | bf16_bits(v[3]) << 16);
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, bf16x2));
 }
+__device__ __forceinline__ uint2 pack4(f32x4 v) { return make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3])); }
 
 __device__ __forceinline__ int clampi(int v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : v; }
 
@@ -206,8 +209,12 @@ struct Operand {
   }
 };
 
-// s(g) = 1 / (1 + e^-g); e^-g overflows to infinity for g < -88 and gives 0
-__device__ __forceinline__ float sigmoid(float g) { return 1.0f / (1.0f + __expf(-g)); }
+// s(g) = 1 / (1 + e^-g) by the reciprocal instruction (1 ulp; the division's
+// dozen instructions were a third of an epilogue's). e^-g overflows to infinity
+// for g < -88 and gives 0.
+__device__ __forceinline__ float sigmoid(float g) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * g));
+}
 
 // Waits until at most N loads of this wave are in flight and all of its LDS
 // reads have returned, then for the workgroup's other waves.

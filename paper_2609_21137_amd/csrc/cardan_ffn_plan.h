@@ -32,14 +32,14 @@ inline size_t ffn_partial_bytes(int32_t N, int32_t H, int32_t I, bool gated) {
 }
 
 // Tiles (output rows x columns), the workgroups that a CU holds of them, and
-// the time of one step of 64 of the sum, measured with every CU busy
-// (8192 x 4096 x 11008 and 1000 x 4096 x 11008, operands in L2).
+// the time of one step of 64 of the sum, measured with every CU busy (y = h Wd
+// of 8192 rows, 4096 x 11008: 1.31, 1.07, 0.85, 0.99, 0.70 and 0.44 PFLOP/s).
 struct FfnTile {
   int bm, bn, per_cu;
   double step_us;
 };
-constexpr FfnTile kFfnTiles[] = {{256, 256, 1, 1.70}, {128, 256, 1, 1.03}, {64, 256, 1, 0.66},
-                                 {128, 128, 2, 1.06}, {64, 128, 2, 0.83},  {32, 128, 2, 0.63}};
+constexpr FfnTile kFfnTiles[] = {{256, 256, 1, 1.60}, {128, 256, 1, 0.98}, {64, 256, 1, 0.62},
+                                 {128, 128, 2, 1.06}, {64, 128, 2, 0.78},  {32, 128, 2, 0.61}};
 constexpr int kFfnTileCount = sizeof kFfnTiles / sizeof kFfnTiles[0];
 constexpr double kUnitUs = 3.8;         // a unit's setup and epilogue ...
 constexpr double kUnitAreaUs = 4.0;     // ... plus this for 256 x 256 outputs
