@@ -286,8 +286,8 @@ int cardan_rmsnorm_bf16(int32_t B, int32_t H, const float* y, float eps,
  * current one. */
 
 /* Shape of a feed-forward block: E matrix sets (experts) of hidden size H and
- * intermediate size I. H % 64 == 0, I % 32 == 0, 1 <= E <= 1024, H * I * 2
- * below 2^31; calls take 0 <= N <= 2^30 rows. */
+ * intermediate size I. H % 64 == 0, I % 32 == 0, both at most 2^20, H * I * 2
+ * below 2^31, 1 <= E <= 1024; calls take 0 <= N <= 2^30 rows. */
 typedef struct {
   int32_t H, I, E;
   int32_t act; /* CARDAN_FFN_SILU_GLU or CARDAN_FFN_RELU2_UP */

@@ -724,6 +724,8 @@ int check_ffn(const cardan_ffn_shape* s, int32_t N) {
   if (s->H % 64) return fail(CARDAN_ERR_UNSUPPORTED, "H=%d must be a multiple of 64", s->H);
   if (s->I % 32) return fail(CARDAN_ERR_UNSUPPORTED, "I=%d must be a multiple of 32", s->I);
   if (s->E > kMaxE) return fail(CARDAN_ERR_UNSUPPORTED, "E=%d exceeds %d", s->E, kMaxE);
+  // (256 rows of the widest tile are addressed with 32-bit byte offsets)
+  if (s->H > (1 << 20) || s->I > (1 << 20)) return fail(CARDAN_ERR_UNSUPPORTED, "H=%d or I=%d exceeds 2^20", s->H, s->I);
   if ((size_t)s->H * s->I * 2 >= 0x80000000ull)
     return fail(CARDAN_ERR_UNSUPPORTED, "matrix of H=%d x I=%d exceeds 2 GiB", s->H, s->I);
   return CARDAN_OK;

@@ -23,7 +23,6 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr uint32_t kOob = 0x80000000u;     // an offset past every resource
 constexpr size_t kLdsBytes = 160 * 1024;   // of a CU
-constexpr uint32_t kSpan = 0x7fffff00u;    // largest resource
 
 struct TileGrid {
   int32_t col_tiles;  // tiles along the output's columns
@@ -32,8 +31,8 @@ struct TileGrid {
   int32_t split;      // parts of each split tile; 1: none is split
 };
 
-__device__ __forceinline__ u32x4 make_rsrc(const void* base, int64_t bytes) {
-  const uint32_t n = bytes <= 0 ? 0u : bytes > (int64_t)kSpan ? kSpan : (uint32_t)bytes;
+__device__ __forceinline__ u32x4 make_rsrc(const void* base, int bytes) {
+  const uint32_t n = bytes < 0 ? 0u : (uint32_t)bytes;
   const uint64_t b = reinterpret_cast<uintptr_t>(base);
   return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)b),
                (uint32_t)__builtin_amdgcn_readfirstlane((int)(b >> 32)) & 0xffffu,
@@ -472,52 +471,75 @@ __device__ __forceinline__ void run_units(const FfnArgs& A, const TileGrid& G, i
   const int per = grid >> 3;
   const int stride = grid, first = (block & 7) * per + (block >> 3);
 
-  struct Unit {  // where a unit's operands are
+  // Where the loads of a unit are: the next step's operands, the bytes that
+  // they may read (a resource ends with its operand: what lies past it is
+  // zero), and the steps. Operands with the sum along memory rows have `na` (nb)
+  // bytes from there to the end of the tile's last row; those with the sum down
+  // the columns have `rows` memory rows left.
+  struct Unit {
     const char *a, *b, *a1, *b1;
-    int64_t ab, bb;    // bytes from there to the operand's end
+    int na, nb, na0, nb0, rows;
     int k, kend, kt1;  // next step, end, and steps of a phase
-    int slot;          // of its partial output, or -1
-    Place p;
+  };
+  auto where = [&](int u, int& slot, int& part, int& parts) {
+    int id = u;
+    slot = -1;
+    part = 0;
+    parts = 1;
+    if (u >= full) {
+      slot = u - full;
+      part = slot / rest;
+      parts = G.split;
+      id = full + slot - part * rest;
+    }
+    return place<KIND, RELU2, BM, BN>(A, G, cum, tm, id);
   };
   auto setup = [&](int u, Unit& U) {
-    int id = u, part = 0, parts = 1;
-    U.slot = -1;
-    if (u >= full) {
-      U.slot = u - full;
-      part = U.slot / rest;
-      parts = G.split;
-      id = full + U.slot - part * rest;
-    }
-    U.p = place<KIND, RELU2, BM, BN>(A, G, cum, tm, id);
+    int slot, part, parts;
+    const Place p = where(u, slot, part, parts);
     if constexpr (kDW) {
       // (a scalar load: a vector load's wait would be one for the stores of the
       // unit before, too)
       int lo = 0, hi = A.N;
       if (A.off) {
         const auto* off = (const __attribute__((address_space(4))) int32_t*)A.off;
-        lo = clampi(off[U.p.e], 0, A.N);
-        hi = clampi(off[U.p.e + 1], lo, A.N);
+        lo = clampi(off[p.e], 0, A.N);
+        hi = clampi(off[p.e + 1], lo, A.N);
       }
-      const int rows = hi - lo;
-      U.a = (const char*)((KIND == K_DWD ? A.h : A.x) + (int64_t)lo * lda + U.p.row);
-      U.b = (const char*)((KIND == K_DWD ? A.dy : U.p.mat ? A.du : A.dg) + (int64_t)lo * ldb + U.p.n0);
-      U.ab = ((int64_t)rows * lda - U.p.row) * 2;
-      U.bb = ((int64_t)rows * ldb - U.p.n0) * 2;
-      U.kt1 = rows > 0 ? (rows + 63) >> 6 : 1;  // a group without rows: one step of zeros
+      U.rows = hi - lo;
+      U.a = (const char*)((KIND == K_DWD ? A.h : A.x) + (int64_t)lo * lda + p.row);
+      U.b = (const char*)((KIND == K_DWD ? A.dy : p.mat ? A.du : A.dg) + (int64_t)lo * ldb + p.n0);
+      U.na0 = p.row * 2;  // (bytes of a memory row before the tile)
+      U.nb0 = p.n0 * 2;
+      U.kt1 = U.rows > 0 ? (U.rows + 63) >> 6 : 1;  // a group without rows: one step of zeros
     } else {
-      U.ab = (int64_t)(U.p.end - U.p.row) * lda * 2;
-      const int64_t ar = (int64_t)U.p.row * lda;
-      const int64_t w = (int64_t)U.p.e * H * I + (kBT ? U.p.n0 : (int64_t)U.p.n0 * ldb);
+      const int64_t ar = (int64_t)p.row * lda;
+      const int64_t w = (int64_t)p.e * H * I + (kBT ? p.n0 : (int64_t)p.n0 * ldb);
       U.a = (const char*)((KIND == K_UP ? A.x : KIND == K_DOWN ? A.h : KIND == K_DH ? A.dy : kPh == 2 ? A.dg : A.du) + ar);
       U.b = (const char*)((KIND == K_UP || KIND == K_DX ? (RELU2 ? A.Wu : A.Wg) : A.Wd) + w);
-      U.bb = kBT ? ((int64_t)ksum * ldb - U.p.n0) * 2 : (int64_t)(nout - U.p.n0) * ldb * 2;
+      U.na0 = min(p.end - p.row, BM) * lda * 2;
+      U.nb0 = kBT ? p.n0 * 2 : min(nout - p.n0, BN) * ldb * 2;
       if constexpr (kPh == 2) U.a1 = (const char*)(A.du + ar);
       if constexpr (kPh == 2 || kDual) U.b1 = (const char*)(A.Wu + w);
+      U.rows = ksum;
       U.kt1 = (ksum + 63) >> 6;
     }
     const int64_t all = (int64_t)U.kt1 * kPh;
     U.k = (int)(all * part / parts);
     U.kend = (int)(all * (part + 1) / parts);
+    // to the first step
+    const bool second = kPh == 2 && U.k >= U.kt1;
+    const int k = second ? U.k - U.kt1 : U.k;
+    if (second) {
+      U.a = U.a1;
+      U.b = U.b1;
+    }
+    U.a += k * astep;
+    U.b += k * bstep;
+    if constexpr (kDual) U.b1 += k * bstep;
+    U.na = U.na0 - k * 128;
+    U.nb = U.nb0 - k * 128;
+    U.rows -= k * 64;
   };
 
   OpA opa;
@@ -540,14 +562,26 @@ __device__ __forceinline__ void run_units(const FfnArgs& A, const TileGrid& G, i
   bool last = false;
   auto step_ahead = [&]() {
     const bool some = pu < units;
-    const bool ph = kPh == 2 && P.k >= P.kt1;
-    const int k = P.k - (ph ? P.kt1 : 0);
-    last = k == P.kt1 - 1;
-    const int64_t ao = k * astep, bo = k * bstep;
-    ra = make_rsrc((ph ? P.a1 : P.a) + ao, some ? P.ab - ao : 0);
-    rb = make_rsrc((ph ? P.b1 : P.b) + bo, some ? P.bb - bo : 0);
-    if constexpr (kDual) rb1 = make_rsrc(P.b1 + bo, some ? P.bb - bo : 0);
-    if (some && ++P.k == P.kend) {
+    const int rows = P.rows < 64 ? P.rows : 64;
+    last = P.k == P.kt1 - 1 || P.k == P.kt1 * kPh - 1;
+    ra = make_rsrc(P.a, !some ? 0 : kAT ? rows * lda * 2 - P.na0 : P.na);
+    rb = make_rsrc(P.b, !some ? 0 : kBT ? rows * ldb * 2 - P.nb0 : P.nb);
+    if constexpr (kDual) rb1 = make_rsrc(P.b1, !some ? 0 : rows * ldb * 2 - P.nb0);
+    if (!some) return;
+    ++P.k;
+    P.a += astep;
+    P.b += bstep;
+    if constexpr (kDual) P.b1 += bstep;
+    P.na -= 128;
+    P.nb -= 128;
+    P.rows -= 64;
+    if (kPh == 2 && P.k == P.kt1) {
+      P.a = P.a1;
+      P.b = P.b1;
+      P.na = P.na0;
+      P.nb = P.nb0;
+    }
+    if (P.k == P.kend) {
       pu += stride;
       if (pu < units) setup(pu, P);
     }
@@ -589,9 +623,9 @@ __device__ __forceinline__ void run_units(const FfnArgs& A, const TileGrid& G, i
   };
 
   typedef Emit<KIND, RELU2, NF> Out;
-  auto epilogue = [&](const Unit& C, int wrow, int wcol) {
-    if (C.slot >= 0) {
-      float* p = A.part + ((int64_t)C.slot * NW + wave) * (MF * NF * 256) + lane * 4;
+  auto epilogue = [&](const Place& C, int slot, int wrow, int wcol) {
+    if (slot >= 0) {
+      float* p = A.part + ((int64_t)slot * NW + wave) * (MF * NF * 256) + lane * 4;
 #pragma unroll
       for (int i = 0; i < MF; ++i)
 #pragma unroll
@@ -600,12 +634,12 @@ __device__ __forceinline__ void run_units(const FfnArgs& A, const TileGrid& G, i
     }
     // what a block row needs is read one block row ahead
     f32x4 in[2][Out::kIn][Out::kGu];
-    Out::fetch(A, C.p, wrow, wcol, nout, in[0]);
+    Out::fetch(A, C, wrow, wcol, nout, in[0]);
 #pragma unroll
     for (int i = 0; i < MF; ++i) {
-      if (wrow + i * 16 >= C.p.end) break;
-      if (i + 1 < MF) Out::fetch(A, C.p, wrow + i * 16 + 16, wcol, nout, in[(i + 1) & 1]);
-      Out::put(A, C.p, wrow + i * 16, wcol, nout, acc[i], in[i & 1]);
+      if (wrow + i * 16 >= C.end) break;
+      if (i + 1 < MF) Out::fetch(A, C, wrow + i * 16 + 16, wcol, nout, in[(i + 1) & 1]);
+      Out::put(A, C, wrow + i * 16, wcol, nout, acc[i], in[i & 1]);
     }
   };
 
@@ -635,15 +669,30 @@ __device__ __forceinline__ void run_units(const FfnArgs& A, const TileGrid& G, i
   bool stored = false;
   int stage = 0;
   for (int u = first; u < units; u += stride) {
-    Unit C;
-    setup(u, C);
+    int slot, part, parts;
+    const Place C = where(u, slot, part, parts);
+    int steps;  // of this unit
+    {
+      int kt1 = (ksum + 63) >> 6;
+      if constexpr (kDW) {
+        int lo = 0, hi = A.N;
+        if (A.off) {
+          const auto* off = (const __attribute__((address_space(4))) int32_t*)A.off;
+          lo = clampi(off[C.e], 0, A.N);
+          hi = clampi(off[C.e + 1], lo, A.N);
+        }
+        kt1 = hi > lo ? (hi - lo + 63) >> 6 : 1;
+      }
+      const int64_t all = (int64_t)kt1 * kPh;
+      steps = (int)(all * (part + 1) / parts) - (int)(all * part / parts);
+    }
 #pragma unroll
     for (int i = 0; i < MF; ++i)
 #pragma unroll
       for (int j = 0; j < NF; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int wrow = C.p.row + wm * (BM / WM), wcol = C.p.n0 + wn * (BC / WN);
-    if (wrow < C.p.end && wcol < nout) {
-      for (int kt = C.k; kt < C.kend; ++kt) {
+    const int wrow = C.row + wm * (BM / WM), wcol = C.n0 + wn * (BC / WN);
+    if (wrow < C.end && wcol < nout) {
+      for (int kt = 0; kt < steps; ++kt) {
         half(a0f, b0f, stage, 1, a1f, b1f, false, 0);
         // the next step has landed, and this step's stage has been read by every wave
         if (kDW && stored) wait_loads<kBehindStores>();
@@ -656,7 +705,7 @@ __device__ __forceinline__ void run_units(const FfnArgs& A, const TileGrid& G, i
       }
     } else {  // a wave whose outputs lie past the end only loads
       stored = false;
-      for (int kt = C.k; kt < C.kend; ++kt) {
+      for (int kt = 0; kt < steps; ++kt) {
         wait_loads<kBehind>();
 #pragma unroll
         for (int q = 0; q < kLoads; ++q) fill(stage, q);
@@ -667,8 +716,8 @@ __device__ __forceinline__ void run_units(const FfnArgs& A, const TileGrid& G, i
       continue;
     }
 
-    epilogue(C, wrow, wcol);
-    stored = wrow + BM / WM <= C.p.end && wcol + BC / WN <= nout;
+    epilogue(C, slot, wrow, wcol);
+    stored = wrow + BM / WM <= C.end && wcol + BC / WN <= nout;
     read_first(stage);
   }
   __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): no load to LDS outlives the workgroup

@@ -34,7 +34,7 @@ def _ffn_bytes(C, shape, N):
 @pytest.mark.parametrize("dims,N,code", [
     ((2048, 768, 1, 0), -1, -2), ((2048, 768, 1, 0), (1 << 30) + 1, -2), ((0, 768, 1, 0), 1, -2), ((2048, -32, 1, 0), 1, -2), ((2048, 768, 0, 0), 1, -2),
     ((2048, 768, 1, 2), 1, -3), ((2048, 768, 1, -1), 1, -3), ((2080, 768, 1, 0), 1, -3), ((2048, 784, 1, 0), 1, -3),
-    ((2048, 768, 1025, 0), 1, -3), ((32768, 32768, 1, 0), 1, -3),
+    ((2048, 768, 1025, 0), 1, -3), ((32768, 32768, 1, 0), 1, -3), ((1 << 21, 32, 1, 0), 1, -3), ((64, 1 << 21, 1, 0), 1, -3),
 ])
 def test_ffn_bad_shapes(C, dims, N, code):
     rc, _ = _ffn_bytes(C, C.FfnShape(*dims), N)
