@@ -24,7 +24,29 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr uint32_t kOob = 0x80000000u;     // an offset past every resource
 constexpr size_t kLdsBytes = 160 * 1024;   // of a CU
 
+// Division of 0 <= n < 2^31 by a constant of the launch: with l = ceil(log2 d)
+// and m = floor(2^(31 + l) / d) + 1, n m / 2^(31 + l) exceeds n / d by less than
+// 1 / d. (The compiler's division takes two dozen vector instructions.)
+struct Divisor {
+  uint32_t d, m, shift;
+  Divisor() : d(1), m(0), shift(0) {}
+  explicit Divisor(int64_t by) : d((uint32_t)by), m(0), shift(0) {
+    int l = 0;
+    while (((int64_t)1 << l) < by) ++l;
+    if (l > 0) {
+      m = (uint32_t)((((uint64_t)1 << (31 + l)) / d) + 1);
+      shift = l - 1;
+    }
+  }
+  __device__ __forceinline__ int quotient(int n) const {
+    return d == 1 ? n : (int)(__umulhi((uint32_t)n, m) >> shift);
+  }
+};
+
 struct TileGrid {
+  Divisor band;       // tiles of a band of row tiles (below: place())
+  Divisor group;      // tiles of one group's gradients
+  int32_t band_log;   // log2 of a band's row tiles
   int32_t col_tiles;  // tiles along the output's columns
   int32_t row_tiles;  // along its rows (weight gradients; others count their groups' rows)
   int32_t full;       // tiles before the split ones
@@ -308,27 +330,46 @@ struct Place {
   int e, row, end, n0, mat;
 };
 
+// Tiles are numbered band by band of 2^band_log row tiles, all columns of a
+// band with the rows fastest: a run of neighbours shares its operands in the
+// XCD's L2. `rows` row tiles (of a group's gradient); the last band may be
+// lower: inv = ceil(2^32 / its height), 0 for a height of one.
+__device__ __forceinline__ uint32_t last_band(const TileGrid& G, int rows) {
+  const uint32_t low = (uint32_t)rows & ((1u << G.band_log) - 1);
+  return (uint32_t)__builtin_amdgcn_readfirstlane(low > 1 ? (int)(0xffffffffu / low + 1) : 0);
+}
+
 template <int KIND, bool RELU2, int BM, int BN>
-__device__ __forceinline__ Place place(const FfnArgs& A, const TileGrid& G, const int* cum, int tm, int id) {
+__device__ __forceinline__ Place place(const FfnArgs& A, const TileGrid& G, const int* cum, int rows, uint32_t inv, int id) {
   constexpr int kMats = KIND == K_DWI && !RELU2 ? 2 : 1, BC = KIND == K_UP && !RELU2 ? BN / 2 : BN;
+  constexpr bool kDW = KIND == K_DWI || KIND == K_DWD;
   Place P;
+  P.e = 0;
   P.mat = 1;
-  if constexpr (KIND == K_DWI || KIND == K_DWD) {
-    // tiles of one group's gradients after another; gate and up in turn
-    const int of = G.row_tiles * G.col_tiles * kMats;
-    P.e = id / of;
-    int t = id - P.e * of;
-    if (kMats == 2) P.mat = t & 1;
-    t /= kMats;
-    P.row = t / G.col_tiles * BM;
-    P.n0 = t % G.col_tiles * BC;
+  if constexpr (kDW) {
+    P.e = G.group.quotient(id);
+    id -= P.e * (int)G.group.d;
+    if (kMats == 2) {
+      P.mat = id & 1;
+      id >>= 1;
+    }
+  }
+  const int band = G.band.quotient(id), in = id - band * (int)G.band.d, left = rows - (band << G.band_log);
+  int row, col;
+  if (left >> G.band_log) {
+    col = in >> G.band_log;
+    row = in & ((1 << G.band_log) - 1);
+  } else {
+    col = inv ? (int)__umulhi((uint32_t)in, inv) : in;
+    row = in - col * left;
+  }
+  row += band << G.band_log;
+  P.n0 = col * BC;
+  if constexpr (kDW) {
+    P.row = row * BM;
     P.end = KIND == K_DWI ? A.H : A.I;
   } else {
-    // 8 row tiles by all column tiles at a time
-    const int band = id / (8 * G.col_tiles), in = id - band * 8 * G.col_tiles;
-    const int rows8 = tm - band * 8 < 8 ? tm - band * 8 : 8;
-    P.n0 = in / rows8 * BC;
-    locate(A, BM, cum, band * 8 + in % rows8, P.e, P.row, P.end);
+    locate(A, BM, cum, row, P.e, P.row, P.end);
   }
   return P;
 }
@@ -465,8 +506,9 @@ __device__ __forceinline__ void run_units(const FfnArgs& A, const TileGrid& G, i
 
   // units of this workgroup: workgroups go round robin over the 8 XCDs; an XCD
   // takes runs of neighbouring tiles, which share operands in its L2
-  const int tm = kDW ? G.row_tiles * kMats * A.E : count_tiles(A, BM, cum);
-  const int tiles = tm * G.col_tiles, full = G.split > 1 ? G.full : tiles;
+  const int rows = kDW ? G.row_tiles : count_tiles(A, BM, cum);  // row tiles
+  const uint32_t inv = last_band(G, rows);
+  const int tiles = rows * G.col_tiles * (kDW ? kMats * A.E : 1), full = G.split > 1 ? G.full : tiles;
   const int rest = tiles - full, units = full + rest * G.split;
   const int per = grid >> 3;
   const int stride = grid, first = (block & 7) * per + (block >> 3);
@@ -492,7 +534,7 @@ __device__ __forceinline__ void run_units(const FfnArgs& A, const TileGrid& G, i
       parts = G.split;
       id = full + slot - part * rest;
     }
-    return place<KIND, RELU2, BM, BN>(A, G, cum, tm, id);
+    return place<KIND, RELU2, BM, BN>(A, G, cum, rows, inv, id);
   };
   auto setup = [&](int u, Unit& U) {
     int slot, part, parts;
@@ -562,11 +604,11 @@ __device__ __forceinline__ void run_units(const FfnArgs& A, const TileGrid& G, i
   bool last = false;
   auto step_ahead = [&]() {
     const bool some = pu < units;
-    const int rows = P.rows < 64 ? P.rows : 64;
+    const int mem = P.rows < 64 ? P.rows : 64;  // memory rows of this step
     last = P.k == P.kt1 - 1 || P.k == P.kt1 * kPh - 1;
-    ra = make_rsrc(P.a, !some ? 0 : kAT ? rows * lda * 2 - P.na0 : P.na);
-    rb = make_rsrc(P.b, !some ? 0 : kBT ? rows * ldb * 2 - P.nb0 : P.nb);
-    if constexpr (kDual) rb1 = make_rsrc(P.b1, !some ? 0 : rows * ldb * 2 - P.nb0);
+    ra = make_rsrc(P.a, !some ? 0 : kAT ? mem * lda * 2 - P.na0 : P.na);
+    rb = make_rsrc(P.b, !some ? 0 : kBT ? mem * ldb * 2 - P.nb0 : P.nb);
+    if constexpr (kDual) rb1 = make_rsrc(P.b1, !some ? 0 : mem * ldb * 2 - P.nb0);
     if (!some) return;
     ++P.k;
     P.a += astep;
@@ -751,10 +793,10 @@ __global__ __launch_bounds__(64 * WM * WN) void k_ffn_join(const FfnArgs A, cons
   extern __shared__ __align__(16) int cum_[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int nout = KIND == K_UP || KIND == K_DH || KIND == K_DWI ? A.I : A.H;
-  const int tm = kDW ? G.row_tiles * (KIND == K_DWI && !RELU2 ? 2 : 1) * A.E : count_tiles(A, BM, cum_);
-  const int rest = tm * G.col_tiles - G.full, tile = blockIdx.x, i = blockIdx.y;
+  const int rows = kDW ? G.row_tiles : count_tiles(A, BM, cum_);
+  const int rest = rows * G.col_tiles * (kDW ? (KIND == K_DWI && !RELU2 ? 2 : 1) * A.E : 1) - G.full, tile = blockIdx.x, i = blockIdx.y;
   if (tile >= rest) return;
-  const Place P = place<KIND, RELU2, BM, BN>(A, G, cum_, tm, G.full + tile);
+  const Place P = place<KIND, RELU2, BM, BN>(A, G, cum_, rows, last_band(G, rows), G.full + tile);
   const int row16 = P.row + wave / WN * (BM / WM) + i * 16, wcol = P.n0 + wave % WN * (BC / WN);
   if (row16 >= P.end || wcol >= nout) return;
   typedef Emit<KIND, RELU2, NF> Out;
@@ -796,6 +838,12 @@ Launch plan(const FfnArgs& A, const FfnProduct& p, const FfnChoice& c, int cus) 
   Launch L;
   L.G.col_tiles = (p.cols + BC - 1) / BC;
   L.G.row_tiles = kDW ? (int)((p.rows + BM - 1) / BM) : 0;
+  // 8 row tiles (4 of both gradients): 12 tiles of operands for 32 products.
+  // Gradients of short sums are bound by their stores, which want whole output
+  // rows (6144 rows of 128 up-only experts: 647 us, in bands 844).
+  L.G.band_log = kDW && p.steps < 32 ? 0 : p.mats == 2 ? 2 : 3;
+  L.G.band = Divisor((int64_t)L.G.col_tiles << L.G.band_log);
+  L.G.group = Divisor(std::max<int64_t>(1, (int64_t)L.G.row_tiles * L.G.col_tiles * p.mats));
   // at most this many tiles (groups end inside tiles); the kernel counts them
   const int64_t tiles = ffn_tiles(p, kFfnTiles[c.tile]);
   L.rest = c.split > 1 ? tiles - c.full : 0;

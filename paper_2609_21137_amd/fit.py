@@ -513,8 +513,7 @@ def distill_step(student: TrainedLayer, x, head, teacher, ids, labels=None, temp
     logits = y.to(torch.bfloat16) @ head
     loss, dlogits = cardan.distill_loss(logits, teacher, ids, labels=labels, temperature=temperature,
                                         ce_weight=ce_weight, row_weight=row_weight, dlogits=logits)
-    dy = dlogits.float() @ head.float().t().contiguous()
-    return loss, student.backward(dy)
+    return loss, student.backward(dlogits @ head.t())
 
 
 def distill_layer(layer: dict, X, head, teacher, ids, k: int, d: int, act: str = "silu_glu", labels=None,
