@@ -24,25 +24,6 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr uint32_t kOob = 0x80000000u;     // an offset past every resource
 constexpr size_t kLdsBytes = 160 * 1024;   // of a CU
 
-// Division of 0 <= n < 2^31 by a constant of the launch: with l = ceil(log2 d)
-// and m = floor(2^(31 + l) / d) + 1, n m / 2^(31 + l) exceeds n / d by less than
-// 1 / d. (The compiler's division takes two dozen vector instructions.)
-struct Divisor {
-  uint32_t d, m, shift;
-  Divisor() : d(1), m(0), shift(0) {}
-  explicit Divisor(int64_t by) : d((uint32_t)by), m(0), shift(0) {
-    int l = 0;
-    while (((int64_t)1 << l) < by) ++l;
-    if (l > 0) {
-      m = (uint32_t)((((uint64_t)1 << (31 + l)) / d) + 1);
-      shift = l - 1;
-    }
-  }
-  __device__ __forceinline__ int quotient(int n) const {
-    return d == 1 ? n : (int)(__umulhi((uint32_t)n, m) >> shift);
-  }
-};
-
 struct TileGrid {
   Divisor band;       // tiles of a band of row tiles (below: place())
   Divisor group;      // tiles of one group's gradients
@@ -333,10 +314,10 @@ struct Place {
 // Tiles are numbered band by band of 2^band_log row tiles, all columns of a
 // band with the rows fastest: a run of neighbours shares its operands in the
 // XCD's L2. `rows` row tiles (of a group's gradient); the last band may be
-// lower: inv = ceil(2^32 / its height), 0 for a height of one.
+// lower: `inv` is inverse_of() its height.
 __device__ __forceinline__ uint32_t last_band(const TileGrid& G, int rows) {
   const uint32_t low = (uint32_t)rows & ((1u << G.band_log) - 1);
-  return (uint32_t)__builtin_amdgcn_readfirstlane(low > 1 ? (int)(0xffffffffu / low + 1) : 0);
+  return (uint32_t)__builtin_amdgcn_readfirstlane((int)inverse_of(low));
 }
 
 template <int KIND, bool RELU2, int BM, int BN>
@@ -360,7 +341,7 @@ __device__ __forceinline__ Place place(const FfnArgs& A, const TileGrid& G, cons
     col = in >> G.band_log;
     row = in & ((1 << G.band_log) - 1);
   } else {
-    col = inv ? (int)__umulhi((uint32_t)in, inv) : in;
+    col = small_quotient(in, inv);
     row = in - col * left;
   }
   row += band << G.band_log;

@@ -10,6 +10,35 @@
 
 namespace cardan {
 
+#ifdef __HIPCC__
+#define CARDAN_HD __host__ __device__
+#else
+#define CARDAN_HD
+#endif
+
+// Division of 0 <= n < 2^31 by a constant of the launch: with l = ceil(log2 d)
+// and m = floor(2^(31 + l) / d) + 1, n m / 2^(31 + l) exceeds n / d by less than
+// 1 / d. (The compiler's division takes two dozen vector instructions.)
+struct Divisor {
+  uint32_t d, m, shift;
+  Divisor() = default;
+  explicit Divisor(int64_t by) : d((uint32_t)by), m(0), shift(0) {
+    int l = 0;
+    while (((int64_t)1 << l) < by) ++l;
+    if (l > 0) {
+      m = (uint32_t)((((uint64_t)1 << (31 + l)) / d) + 1);
+      shift = l - 1;
+    }
+  }
+  CARDAN_HD int quotient(int n) const { return d == 1 ? n : (int)((uint32_t)((uint64_t)(uint32_t)n * m >> 32) >> shift); }
+};
+
+// Division of n by a small d of the kernel, n d < 2^32: inv = ceil(2^32 / d), 0 for 1.
+CARDAN_HD inline uint32_t inverse_of(uint32_t d) { return d > 1 ? 0xffffffffu / d + 1 : 0; }
+CARDAN_HD inline int small_quotient(int n, uint32_t inv) {
+  return inv ? (int)((uint64_t)(uint32_t)n * inv >> 32) : n;
+}
+
 // The products of the block. "rows" are the rows of a group (tokens).
 enum FfnKind {
   K_UP = 0,    // [rows, H] x [H, I] (gate and up): activation -> h, and g, u where kept

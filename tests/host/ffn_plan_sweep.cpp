@@ -44,6 +44,20 @@ int main(int argc, char** argv) {
           }
         }
   }
+  // quotients at and around multiples of the divisor, up to the largest dividend
+  for (int i = 0; i < 20 * n; ++i) {
+    const int64_t d = i < 300 ? i + 1 : log_uniform(1, 1.0e9);
+    const Divisor D(d);
+    const int64_t most = 0x7fffffff / d;
+    for (int64_t q : {(int64_t)0, most, most / 2, log_uniform(1, (double)most + 1.5) - 1})
+      for (int64_t off : {-1, 0, 1}) {
+        const int64_t v = q * d + off;
+        if (v < 0 || v > 0x7fffffff) continue;
+        if (D.quotient((int)v) != v / d && ++failures < 20) printf("%ld / %ld\n", (long)v, (long)d);
+        if (d < 8 && v * d < 0x100000000ll && small_quotient((int)v, inverse_of((uint32_t)d)) != v / d && ++failures < 20)
+          printf("small %ld / %ld\n", (long)v, (long)d);
+      }
+  }
   printf("%ld split products, %ld of them in a last round, %ld failures\n", splits, tails, failures);
   return failures != 0 || splits == 0 || tails == 0;
 }
