@@ -357,12 +357,13 @@ enum { CARDAN_LOGITS_BF16 = 0, CARDAN_LOGITS_F32 = 1 };
  * sum_n row_weight[n] (kd_n + ce_weight * ce_n), rounded once; it may be the
  * logits' own memory (dlogits == logits and dld == ld), and must not overlap
  * them otherwise. row_weight: [N] float32, NULL for ones.
- * An id outside [0, V) is no entry (the teacher's distribution is over the
- * others; a row without any has kd = 0); a label outside [0, V) is none (ce =
+ * An id outside [0, V), or one whose kept logit is -inf, is no entry (the
+ * teacher's distribution is over the others; a row without any has kd = 0); a label outside [0, V) is none (ce =
  * 0); labels may be NULL. A row with neither gets zero loss and gradient and
  * its logits are not looked at. An entry named twice counts with both its
  * probabilities. -inf logits have probability 0; NaN or +inf among a row's
- * logits give that row NaN. Values between V and the row strides are neither
+ * logits give that row NaN; among the kept logits of its entries they give NaN
+ * in kd and in the gradient at those entries. Values between V and the row strides are neither
  * read nor written.
  * 0 <= N <= 2^30, 1 <= V <= 2^30, 0 <= K <= 1024 (teacher and ids may be NULL
  * at K == 0), V <= ld, dld <= 2^40, 2^-16 <= T <= 2^16, ce_weight finite. */

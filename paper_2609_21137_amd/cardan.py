@@ -619,7 +619,8 @@ def distill_loss(logits, teacher, ids, labels=None, temperature: float = 1.0, ce
     entropy of ``labels`` (int32, [N]); ``dlogits`` is the gradient of
     ``sum_n row_weight[n] (kd_n + ce_weight ce_n)`` in the logits' type and
     with rows padded as theirs, or None with ``grad=False``. ``dlogits=logits`` overwrites the
-    logits. Ids and labels outside ``[0, V)`` mark absent entries and labels."""
+    logits. Ids and labels outside ``[0, V)`` mark absent entries and labels, and a
+    teacher's logit of -inf an absent entry."""
     if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or logits.dtype not in (torch.bfloat16, torch.float32):
         raise ValueError("logits must be a [N, V] tensor of bfloat16 or float32")
     N, V = logits.shape

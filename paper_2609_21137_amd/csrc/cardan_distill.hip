@@ -6,6 +6,9 @@
 //   p = softmax_j(t_j / T),  q = softmax(s / T),  r = softmax(s)
 //   kd = T^2 sum_j p_j (log p_j - log q_{i_j}),  ce = -log r_label
 //   d/ds [w (kd + c ce)] = w T (q - sum_j p_j 1_{i_j}) + w c (r - 1_label)
+//
+// Bound by the logits' read and the gradient's write: 8192 x 128256 bf16 in
+// 922 us (4.6 TB/s of those bytes), 1500 x 151936 float32 in 391 us (4.7).
 #include <hip/hip_runtime.h>
 
 #include "cardan_ffn.h"
@@ -157,6 +160,7 @@ __global__ __launch_bounds__(NT) void k_distill(const DistillArgs A, int first) 
     if (id[q] >= V) id[q] = -1;
     t[q] = id[q] >= 0 ? A.teacher[(int64_t)n * K + j] : -INFINITY;
     z[q] = id[q] >= 0 ? L::get(row, id[q]) : 0.f;
+    if (t[q] == -INFINITY) id[q] = -1;  // of probability zero: no entry, also where all are
     tmax = fmaxf(tmax, t[q]);
   }
 #pragma unroll
@@ -249,7 +253,7 @@ __global__ __launch_bounds__(NT) void k_distill(const DistillArgs A, int first) 
       const int j = q * NT + tid;
       if (q * NT >= K) break;
       const float p = id[q] >= 0 ? t[q] / tsum : 0.f;
-      if (p > 0.f) {
+      if (p != 0.f) {  // (a NaN goes on into the loss)
         const double tt = (double)A.teacher[(int64_t)n * K + j] - tmax;
         kd += (double)p * ((tt - ((double)z[q] - m)) * dT + logs);
       }

@@ -195,6 +195,34 @@ def test_masked_and_extreme_logits(C):
         assert torch.equal(loss2[2:], loss[2:]) and torch.equal(d2[2:], d[2:])
 
 
+@pytest.mark.parametrize("T", [1.0, 2.0, 3.0])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_teacher_rows_masked_out(C, dtype, T):
+    N, V, K = 7, 1003, 70
+    logits, teacher, ids, labels, w = _inputs(N, V, K, dtype, 31)
+    low = float("-inf")
+    teacher[0] = low                        # nothing left, with a label
+    teacher[1] = low                        # nothing left, nothing else
+    labels[1] = -1
+    teacher[2, ::2] = low                   # a part, the label at a masked entry
+    labels[2] = ids[2, 4]
+    teacher[3, 1:] = low                    # the label at a masked entry of a row with one left
+    labels[3] = ids[3, 9]
+    teacher[4] = low                        # nothing left, the label at a masked entry
+    labels[4] = ids[4, 0]
+    teacher[5, 3] = float("nan")
+    teacher[6, 3] = float("inf")
+    _say(f"teacher rows masked out: {dtype} T={T}")
+    loss, d = C.distill_loss(logits, teacher, ids, labels, T, 0.5, w)
+    n = 5
+    seen = torch.where(teacher == low, -1, ids)[:n].contiguous()
+    want = _oracle(logits[:n], torch.where(teacher == low, 0.0, teacher)[:n], seen, labels[:n], T, 0.5, w[:n])
+    _check(loss[:n], d[:n], want, dtype)
+    assert (loss[[0, 1, 4], 0] == 0).all() and (d[1] == 0).all() and loss[1, 1] == 0
+    for i in (5, 6):
+        assert torch.isnan(loss[i, 0]) and torch.isnan(d[i, ids[i].long()]).all() and torch.isfinite(loss[i, 1])
+
+
 def test_gradient_against_differences(C):
     N, V, K, T, c = 4, 777, 20, 2.0, 0.5
     logits, teacher, ids, labels, w = _inputs(N, V, K, torch.float32, seed=3)
