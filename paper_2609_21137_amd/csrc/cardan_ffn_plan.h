@@ -170,7 +170,7 @@ inline bool few_rows(int32_t N, int32_t H, int32_t I, bool grouped) {
 // rows: as many as the chip's CUs allow, up to 8, and at least a step for every
 // wave. Each of the second product's workgroups adds the parts of all of h and
 // holds it in LDS. (One row through 2048 x 1408: the two products take 4.7 and
-// 5.6 us with four parts, 9.4 and 5.8 without.)
+// 5.7 us with four parts, 9.4 and 5.8 without.)
 inline int few_split(int32_t N, int32_t H, int32_t I, int cus) {
   if (N > 16 || (int64_t)N * I > 32768) return 1;
   int s = 1;
