@@ -295,7 +295,7 @@ typedef struct {
 
 enum {
   CARDAN_FFN_SILU_GLU = 0, /* h = silu(x W_gate) * (x W_up)                  */
-  CARDAN_FFN_RELU2_UP = 1  /* h = max(x W_up, 0)^2; W_gate is not read       */
+  CARDAN_FFN_RELU2_UP = 1  /* h = max(x W_up, 0)^2 (NaN stays NaN); W_gate is not read */
 };
 
 /* Dense bf16 weights (device pointers), laid out as in cardan_dense_layer. */

@@ -236,6 +236,9 @@ __device__ __forceinline__ void wait_loads() {
   asm volatile("" ::: "memory");
 }
 
+// max(u, 0) that keeps a NaN (fmaxf returns its other operand).
+__device__ __forceinline__ float relu(float u) { return u < 0.f ? 0.f : u; }
+
 // Activation of four projections; g is not used by up-only experts.
 template <bool RELU2>
 __device__ __forceinline__ f32x4 activate(f32x4 g, f32x4 u) {
@@ -243,7 +246,7 @@ __device__ __forceinline__ f32x4 activate(f32x4 g, f32x4 u) {
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     if constexpr (RELU2) {
-      const float p = fmaxf(u[q], 0.f);
+      const float p = relu(u[q]);
       h[q] = p * p;
     } else {
       h[q] = g[q] * sigmoid(g[q]) * u[q];
@@ -258,7 +261,7 @@ __device__ __forceinline__ void activate_grad(f32x4 dh, f32x4 g, f32x4 u, f32x4&
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     if constexpr (RELU2) {
-      du[q] = dh[q] * 2.f * fmaxf(u[q], 0.f);
+      du[q] = dh[q] * 2.f * relu(u[q]);
     } else {
       const float s = sigmoid(g[q]);
       dg[q] = dh[q] * u[q] * s * (1.f + g[q] * (1.f - s));
