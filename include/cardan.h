@@ -343,7 +343,13 @@ int cardan_ffn_backward(const cardan_ffn_shape* shape, int32_t N, const cardan_b
                         cardan_bf16* dW_up, cardan_bf16* dW_down, void* ws, size_t ws_bytes,
                         hipStream_t stream);
 
-enum { CARDAN_LOGITS_BF16 = 0, CARDAN_LOGITS_F32 = 1 };
+enum {
+  CARDAN_LOGITS_BF16 = 0,
+  CARDAN_LOGITS_F32 = 1,
+  /* added to either: logits, teacher, ids, loss and dlogits need only start on
+   * a multiple of their own elements' size (a slice of rows of odd length) */
+  CARDAN_LOGITS_ANY_START = 16
+};
 
 /* Distillation loss of paper Sec. 3.3, Eq. (3), per row, with its gradient:
  * student logits s over V vocabulary entries (row n at logits + n * ld, type

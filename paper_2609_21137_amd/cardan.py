@@ -608,10 +608,13 @@ def _rows_ptr(t, dtype, name, shape, dev):
     return t.data_ptr(), ld
 
 
+_ANY_START = 16  # CARDAN_LOGITS_ANY_START
+
+
 def distill_loss(logits, teacher, ids, labels=None, temperature: float = 1.0, ce_weight: float = 0.0,
                  row_weight=None, grad: bool = True, out=None, dlogits=None):
     """Distillation loss of student ``logits [N, V]`` (bf16 or float32, rows
-    may be padded) against a teacher's kept logits ``teacher [N, K]`` (float32)
+    may be padded and start on any element) against a teacher's kept logits ``teacher [N, K]`` (float32)
     at the vocabulary entries ``ids [N, K]`` (int32), and its gradient.
 
     Returns ``(loss [N, 2], dlogits)``: per row ``kd = T^2 KL(softmax(teacher
@@ -632,14 +635,15 @@ def distill_loss(logits, teacher, ids, labels=None, temperature: float = 1.0, ce
     lp, ld = _rows_ptr(logits, dt, "logits", (N, V), dev)
     loss = out if out is not None else torch.empty((N, 2), dtype=f32, device=dev)
     if dlogits is None and grad:
-        # rows as far apart as the logits' (their alignment), where that is padding
-        dlogits = torch.empty((N, ld if ld <= 2 * V else V), dtype=dt, device=dev)[:, :V]
+        # rows that start as the logits' do (their alignment), as far apart where that is padding
+        width, skip = ld if ld <= 2 * V else V, lp % 16 // logits.element_size()
+        dlogits = torch.empty(skip + N * width, dtype=dt, device=dev)[skip:].view(N, width)[:, :V]
     gp, dld = _rows_ptr(dlogits, dt, "dlogits", (N, V), dev) if dlogits is not None else (None, 0)
     args = (_arg(teacher, f32, "teacher", (N, K), dev), _arg(ids, i32, "ids", (N, K), dev),
             _arg(labels, i32, "labels", (N,), dev, True), temperature, ce_weight,
             _arg(row_weight, f32, "row_weight", (N,), dev, True), _arg(loss, f32, "out", (N, 2), dev), gp, dld)
     with _Device(dev) as stream:
-        _check(_lib.cardan_distill_loss(N, V, K, 1 if dt is f32 else 0, lp, ld, *args, stream))
+        _check(_lib.cardan_distill_loss(N, V, K, _ANY_START + (1 if dt is f32 else 0), lp, ld, *args, stream))
     return loss, dlogits
 
 

@@ -848,7 +848,9 @@ int cardan_distill_loss(int32_t N, int32_t V, int32_t K, int32_t logits_type, co
   g_err[0] = 0;
   if (N < 0 || N > (1 << 30) || V < 1 || V > (1 << 30)) return fail(CARDAN_ERR_BAD_SHAPE, "N=%d, V=%d outside the valid range", N, V);
   if (K < 0 || K > 1024) return fail(CARDAN_ERR_UNSUPPORTED, "K=%d outside [0, 1024]", K);
-  if (logits_type != CARDAN_LOGITS_BF16 && logits_type != CARDAN_LOGITS_F32)
+  const bool any_start = (logits_type & CARDAN_LOGITS_ANY_START) != 0;
+  const int32_t type = logits_type & ~CARDAN_LOGITS_ANY_START;
+  if (type != CARDAN_LOGITS_BF16 && type != CARDAN_LOGITS_F32)
     return fail(CARDAN_ERR_UNSUPPORTED, "logits type %d is not known", logits_type);
   const int64_t most = (int64_t)1 << 40;
   if (ld < V || ld > most || (dlogits && (dld < V || dld > most)))
@@ -857,13 +859,18 @@ int cardan_distill_loss(int32_t N, int32_t V, int32_t K, int32_t logits_type, co
   if (!(temperature >= 1.0f / 65536.0f && temperature <= 65536.0f) || !isfinite(ce_weight))
     return fail(CARDAN_ERR_BAD_SHAPE, "temperature must lie within [2^-16, 2^16], and ce_weight be finite");
   if (N == 0) return CARDAN_OK;
-  REQ(logits, "logits");
-  REQ(loss, "loss");
-  if (K > 0) {
-    REQ(teacher, "teacher");
-    REQ(ids, "ids");
-  }
-  if (misaligned(dlogits)) return fail(CARDAN_ERR_ALIGN, "dlogits is not 16-byte aligned");
+  const auto start = [&](const void* p, const char* name, uintptr_t size) -> int {
+    if (!p) return fail(CARDAN_ERR_NULL_PTR, "%s is NULL", name);
+    const uintptr_t to = any_start ? size : 16;
+    return reinterpret_cast<uintptr_t>(p) % to ? fail(CARDAN_ERR_ALIGN, "%s is not %d-byte aligned", name, (int)to) : CARDAN_OK;
+  };
+  const uintptr_t element = type == CARDAN_LOGITS_F32 ? 4 : 2;
+  int rc = start(logits, "logits", element);
+  if (!rc) rc = start(loss, "loss", 4);
+  if (!rc && K > 0) rc = start(teacher, "teacher", 4);
+  if (!rc && K > 0) rc = start(ids, "ids", 4);
+  if (!rc && dlogits) rc = start(dlogits, "dlogits", element);
+  if (rc) return rc;
   if (dlogits == logits && dld != ld) return fail(CARDAN_ERR_BAD_SHAPE, "dlogits in place of the logits needs dld == ld");
   if ((reinterpret_cast<uintptr_t>(labels) | reinterpret_cast<uintptr_t>(row_weight)) & 3u)
     return fail(CARDAN_ERR_ALIGN, "labels or row_weight is not 4-byte aligned");
@@ -872,7 +879,7 @@ int cardan_distill_loss(int32_t N, int32_t V, int32_t K, int32_t logits_type, co
   A.N = N;
   A.V = V;
   A.K = K;
-  A.f32 = logits_type == CARDAN_LOGITS_F32;
+  A.f32 = type == CARDAN_LOGITS_F32;
   A.ld = ld;
   A.dld = dld;
   A.logits = logits;
