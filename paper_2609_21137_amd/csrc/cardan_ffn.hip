@@ -29,7 +29,6 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 #define LDS __attribute__((address_space(3)))
 
 constexpr uint32_t kOob = 0x80000000u;     // an offset past every resource
-constexpr size_t kLdsBytes = 160 * 1024;   // of a CU
 
 struct TileGrid {
   Divisor band;       // tiles of a band of row tiles (below: place())
@@ -827,8 +826,10 @@ struct Launch {
   size_t list, lds;  // of the groups' list, and of all
 };
 
-template <int KIND, bool RELU2, int BM, int BN, int WM, int WN, int NS>
+template <int KIND, bool RELU2, int TILE>
 Launch plan(const FfnArgs& A, const FfnProduct& p, const FfnChoice& c, int cus) {
+  constexpr FfnTile T = kFfnTiles[TILE];
+  constexpr int BM = T.bm, BN = T.bn;
   constexpr bool kDW = KIND == K_DWI || KIND == K_DWD;
   constexpr int BC = KIND == K_UP && !RELU2 ? BN / 2 : BN;
   Launch L;
@@ -841,28 +842,29 @@ Launch plan(const FfnArgs& A, const FfnProduct& p, const FfnChoice& c, int cus) 
   L.G.band = Divisor((int64_t)L.G.col_tiles << L.G.band_log);
   L.G.group = Divisor(std::max<int64_t>(1, (int64_t)L.G.row_tiles * L.G.col_tiles * p.mats));
   // at most this many tiles (groups end inside tiles); the kernel counts them
-  const int64_t tiles = ffn_tiles(p, kFfnTiles[c.tile]);
+  const int64_t tiles = ffn_tiles(p, T);
   L.rest = c.split > 1 ? tiles - c.full : 0;
   L.units = tiles + L.rest * (c.split - 1);
   L.G.full = (int)c.full;
   L.G.split = c.split;
-  L.list = A.off && !kDW ? (size_t)A.E * 12 : 0;
-  L.lds = (size_t)NS * (BM + BN) * 128 + L.list;
-  const int fit = (int)(kLdsBytes / L.lds), wave_fit = 8 / (WM * WN);  // workgroups a CU holds at once
-  const int64_t most = (int64_t)cus * (fit < wave_fit ? fit : wave_fit);
+  L.list = p.list;
+  L.lds = ffn_lds(T, L.list);
+  const int64_t most = (int64_t)cus * ffn_resident(T, L.list);
   L.grid = (int)((std::min(L.units, most) + 7) / 8 * 8);
   return L;
 }
 
-template <int KIND, bool RELU2, int BM, int BN, int WM, int WN, int NS>
+template <int KIND, bool RELU2, int TILE>
 hipError_t run(const FfnArgs& A, const FfnProduct& p, const FfnChoice& c, int cus, hipStream_t s) {
-  const Launch L = plan<KIND, RELU2, BM, BN, WM, WN, NS>(A, p, c, cus);
+  constexpr FfnTile T = kFfnTiles[TILE];
+  constexpr int kThreads = 64 * T.wm * T.wn;
+  const Launch L = plan<KIND, RELU2, TILE>(A, p, c, cus);
   if (L.units == 0) return hipSuccess;
   if (L.units > 0x40000000) return hipErrorInvalidValue;
-  k_ffn<KIND, RELU2, BM, BN, WM, WN, NS><<<dim3(L.grid), dim3(64 * WM * WN), L.lds, s>>>(A, L.G);
+  k_ffn<KIND, RELU2, T.bm, T.bn, T.wm, T.wn, T.stages><<<dim3(L.grid), dim3(kThreads), L.lds, s>>>(A, L.G);
   hipError_t e = hipGetLastError();
   if (L.rest == 0 || e != hipSuccess) return e;
-  k_ffn_join<KIND, RELU2, BM, BN, WM, WN><<<dim3((unsigned)L.rest, BM / WM / 16), dim3(64 * WM * WN), L.list, s>>>(A, L.G);
+  k_ffn_join<KIND, RELU2, T.bm, T.bn, T.wm, T.wn><<<dim3((unsigned)L.rest, T.bm / T.wm / 16), dim3(kThreads), L.list, s>>>(A, L.G);
   return hipGetLastError();
 }
 
@@ -871,12 +873,12 @@ hipError_t run_kind(const FfnArgs& A, int cus, hipStream_t s) {
   const FfnProduct p = ffn_product((FfnKind)KIND, A.N, A.E, A.H, A.I, !RELU2, A.off != nullptr);
   const FfnChoice c = choose_ffn(p, cus);
   switch (c.tile) {
-    case 0: return run<KIND, RELU2, 256, 256, 2, 4, 2>(A, p, c, cus, s);
-    case 1: return run<KIND, RELU2, 128, 256, 2, 4, 3>(A, p, c, cus, s);
-    case 2: return run<KIND, RELU2, 64, 256, 1, 8, 3>(A, p, c, cus, s);
-    case 3: return run<KIND, RELU2, 128, 128, 2, 2, 2>(A, p, c, cus, s);
-    case 4: return run<KIND, RELU2, 64, 128, 1, 4, 3>(A, p, c, cus, s);
-    default: return run<KIND, RELU2, 32, 128, 1, 4, 4>(A, p, c, cus, s);
+    case 0: return run<KIND, RELU2, 0>(A, p, c, cus, s);
+    case 1: return run<KIND, RELU2, 1>(A, p, c, cus, s);
+    case 2: return run<KIND, RELU2, 2>(A, p, c, cus, s);
+    case 3: return run<KIND, RELU2, 3>(A, p, c, cus, s);
+    case 4: return run<KIND, RELU2, 4>(A, p, c, cus, s);
+    default: return run<KIND, RELU2, 5>(A, p, c, cus, s);
   }
 }
 
@@ -894,9 +896,10 @@ hipError_t run_grads(const FfnArgs& A, int cus, hipStream_t s) {
     one = one && c[i].tile == kFfnTileCount - 1 && c[i].split == 1;
   }
   if (one) {
-    const Launch L[3] = {plan<K_DX, RELU2, 32, 128, 1, 4, 4>(A, p[0], c[0], cus),
-                         plan<K_DWI, RELU2, 32, 128, 1, 4, 4>(A, p[1], c[1], cus),
-                         plan<K_DWD, RELU2, 32, 128, 1, 4, 4>(A, p[2], c[2], cus)};
+    constexpr int kLast = kFfnTileCount - 1;
+    constexpr FfnTile T = kFfnTiles[kLast];
+    const Launch L[3] = {plan<K_DX, RELU2, kLast>(A, p[0], c[0], cus), plan<K_DWI, RELU2, kLast>(A, p[1], c[1], cus),
+                         plan<K_DWD, RELU2, kLast>(A, p[2], c[2], cus)};
     GradGrids S;
     int at = 0;
     for (int i = 0; i < 3; ++i) {
@@ -904,7 +907,7 @@ hipError_t run_grads(const FfnArgs& A, int cus, hipStream_t s) {
       S.g[i] = L[i].G;
       S.at[i] = at += L[i].grid;
     }
-    k_ffn_grads<RELU2, 32, 128, 1, 4, 4><<<dim3(at), dim3(256), L[0].lds, s>>>(A, S);
+    k_ffn_grads<RELU2, T.bm, T.bn, T.wm, T.wn, T.stages><<<dim3(at), dim3(64 * T.wm * T.wn), L[0].lds, s>>>(A, S);
     return hipGetLastError();
   }
   hipError_t e = A.N > 0 && A.dx ? run_kind<K_DX, RELU2>(A, cus, s) : hipSuccess;

@@ -60,16 +60,28 @@ inline size_t ffn_partial_bytes(int32_t N, int32_t H, int32_t I, bool gated) {
   return std::min(kPartialMax, (size_t)kMaxSplit * 4 * std::max(up(N) * wide, (gated ? 2 : 1) * up(H) * up(I)));
 }
 
-// Tiles (output rows x columns), the workgroups that a CU holds of them, and
-// the time of one step of 64 of the sum, measured with every CU busy (y = h Wd
-// of 8192 rows, 4096 x 11008: 1.31, 1.07, 0.85, 0.99, 0.70 and 0.44 PFLOP/s).
+// Tiles (output rows x columns), their waves and stages of LDS, and the time of
+// one step of 64 of the sum, measured with every CU busy: with as many workgroups
+// on a CU as fit (y = h Wd of 8192 rows, 4096 x 11008: 1.31, 1.07, 0.85, 0.99,
+// 0.70 and 0.44 PFLOP/s), and with one, where that differs (two tiles of 32 x 128
+// on a CU take 0.61 us a step, one alone 0.27; 64 x 128 0.78 and 0.35).
 struct FfnTile {
-  int bm, bn, per_cu;
-  double step_us;
+  int bm, bn, wm, wn, stages;
+  double step_us, alone_us;
 };
-constexpr FfnTile kFfnTiles[] = {{256, 256, 1, 1.60}, {128, 256, 1, 0.98}, {64, 256, 1, 0.62},
-                                 {128, 128, 2, 1.06}, {64, 128, 2, 0.78},  {32, 128, 2, 0.61}};
+constexpr FfnTile kFfnTiles[] = {{256, 256, 2, 4, 2, 1.60, 1.60}, {128, 256, 2, 4, 3, 0.98, 0.98}, {64, 256, 1, 8, 3, 0.62, 0.62},
+                                 {128, 128, 2, 2, 2, 1.06, 1.06}, {64, 128, 1, 4, 3, 0.78, 0.35}, {32, 128, 1, 4, 4, 0.61, 0.27}};
 constexpr int kFfnTileCount = sizeof kFfnTiles / sizeof kFfnTiles[0];
+
+// LDS of a workgroup, with the list of the row groups (of E > 0 of them) behind
+// the stages, and the workgroups that a CU holds at once.
+constexpr size_t kLdsBytes = 160 * 1024;
+inline size_t ffn_list_bytes(int32_t E) { return (size_t)E * 12; }
+inline size_t ffn_lds(const FfnTile& t, size_t list) { return (size_t)t.stages * (t.bm + t.bn) * 128 + list; }
+inline int ffn_resident(const FfnTile& t, size_t list) {
+  return (int)std::min<size_t>(kLdsBytes / ffn_lds(t, list), 8 / (t.wm * t.wn));
+}
+
 constexpr double kUnitUs = 3.8;         // a unit's setup and epilogue ...
 constexpr double kUnitAreaUs = 4.0;     // ... plus this for 256 x 256 outputs
 constexpr double kJoinUs = 3.5;         // a joining kernel
@@ -84,6 +96,7 @@ struct FfnProduct {
   bool dual;   // two products side by side in a tile (gate and up)
   bool grad;   // a weight gradient: every group has `rows` rows of its own
   bool known;  // the number of tiles is known on the host
+  size_t list; // bytes of LDS that the list of the row groups takes
   int64_t steps;
   int max_split;
   size_t partial_bytes;
@@ -98,6 +111,7 @@ inline FfnProduct ffn_product(FfnKind kind, int32_t N, int32_t E, int32_t H, int
   p.dual = kind == K_UP && gated;
   p.grad = grad;
   p.known = grad || !grouped;
+  p.list = p.known ? 0 : ffn_list_bytes(E);
   p.cols = over_h || kind == K_DWI ? I : H;
   p.groups = grad ? E : active;
   p.rows = kind == K_DWI ? H : kind == K_DWD ? I : N;
@@ -135,7 +149,9 @@ inline FfnChoice choose_ffn(const FfnProduct& p, int cus) {
   for (int t = 0; t < kFfnTileCount; ++t) {
     const FfnTile& T = kFfnTiles[t];
     const int bc = p.dual ? T.bn / 2 : T.bn;
-    const int64_t most = ffn_tiles(p, T), slots = (int64_t)cus * T.per_cu;
+    const int resident = ffn_resident(T, p.list);
+    const double step_us = resident > 1 ? T.step_us : T.alone_us;
+    const int64_t most = ffn_tiles(p, T), slots = (int64_t)cus * resident;
     const int64_t tiles = p.known ? most
                                   : (int64_t)(std::max((double)std::min(p.groups, p.rows), (double)p.rows / T.bm + 0.5 * p.groups) *
                                               ((p.cols + bc - 1) / bc));
@@ -147,8 +163,8 @@ inline FfnChoice choose_ffn(const FfnProduct& p, int cus) {
       if (s > 1 && (most == full || bytes > (double)p.partial_bytes)) continue;
       const int64_t rest = tiles - full;
       const double rounds = (double)(full / slots), last = (double)((rest * s + slots - 1) / slots);
-      const double work = rounds * (T.step_us * (double)p.steps + unit_us) +
-                          last * (T.step_us * (double)((p.steps + s - 1) / s) + unit_us);
+      const double work = rounds * (step_us * (double)p.steps + unit_us) +
+                          last * (step_us * (double)((p.steps + s - 1) / s) + unit_us);
       const double join = s == 1 ? 0.0 : kJoinUs + (double)rest * s * T.bm * T.bn * 4.0 / 4.0e6;
       const double us = std::max(work, stream_us) + 0.1 * std::min(work, stream_us) + join;
       if (us < best_us) {
