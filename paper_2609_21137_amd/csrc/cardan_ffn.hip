@@ -52,10 +52,16 @@ __device__ __forceinline__ u32x4 make_rsrc(const void* base, int bytes) {
 // `lds`. Written as asm because the compiler, which cannot tell the stages of
 // LDS apart, waits for every such load before the next transposing read; the
 // wait that is needed is wait_loads(). It has no output register. (M0 holds
-// the LDS address and must be a wait state old.)
+// the LDS address and must be a wait state old.) It writes LDS and M0: no other
+// memory access moves across it, which the counts of wait_loads() rely on. The
+// compiler takes M0 for reserved and warns that it is not kept, as it need not be.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_to_lds(u32x4 rs, uint32_t lds, uint32_t voff) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(rs));
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(rs)
+               : "m0", "memory");
 }
+#pragma clang diagnostic pop
 
 // float32 -> bf16, nearest even (NaN stays NaN)
 __device__ __forceinline__ uint32_t bf16_bits(float f) {
