@@ -462,7 +462,7 @@ class TrainedLayer:
         if self._kept is None:
             raise RuntimeError("backward needs a forward pass")
         xe, rows, a, offsets, W, saved = self._kept
-        dye = (dy.float()[rows] * a[:, None]).to(torch.bfloat16)
+        dye = (dy.float()[rows] * a[:, None]).to(torch.bfloat16)  # (what the block takes)
         _, dg, du, dd = cardan.ffn_backward(dye, xe, W.get("gate"), W["up"], W["down"], saved, offsets=offsets,
                                             act=self.act, need_dx=False)
         grads = {}
@@ -513,7 +513,8 @@ def distill_step(student: TrainedLayer, x, head, teacher, ids, labels=None, temp
     logits = y.to(torch.bfloat16) @ head
     loss, dlogits = cardan.distill_loss(logits, teacher, ids, labels=labels, temperature=temperature,
                                         ce_weight=ce_weight, row_weight=row_weight, dlogits=logits)
-    return loss, student.backward(dlogits @ head.t())
+    # in float32: the rows of the experts are rounded to bf16 once, weighted, in backward()
+    return loss, student.backward(torch.mm(dlogits, head.t(), out_dtype=torch.float32))
 
 
 def distill_layer(layer: dict, X, head, teacher, ids, k: int, d: int, act: str = "silu_glu", labels=None,
