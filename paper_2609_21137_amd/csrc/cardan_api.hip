@@ -24,11 +24,15 @@ hipError_t launch_expert(const Plan&, const Args&, const Chain&, int, size_t, hi
 hipError_t launch_route_reset(const Plan&, const Args&, hipStream_t);
 hipError_t launch_zero(void* p, size_t bytes, hipStream_t);
 hipError_t launch_rmsnorm(hipStream_t, int, int, const float*, float, uint16_t*, hipEvent_t, hipEvent_t);
-// The training kernels' launchers are weak: a build of the host code without
-// them (the sanitizer tests') links, and reports a HIP error if one is reached.
-__attribute__((weak)) hipError_t launch_ffn_forward(const FfnArgs&, hipStream_t);
-__attribute__((weak)) hipError_t launch_ffn_backward(const FfnArgs&, hipStream_t);
-__attribute__((weak)) hipError_t launch_distill(const DistillArgs&, hipStream_t);
+// Host code built for a sanitizer links without the training kernels: there
+// their launchers report a HIP error unless the kernels are linked too.
+#if defined(__has_feature)
+#if __has_feature(address_sanitizer)
+__attribute__((weak)) hipError_t launch_ffn_forward(const FfnArgs&, hipStream_t) { return hipErrorInvalidDeviceFunction; }
+__attribute__((weak)) hipError_t launch_ffn_backward(const FfnArgs&, hipStream_t) { return hipErrorInvalidDeviceFunction; }
+__attribute__((weak)) hipError_t launch_distill(const DistillArgs&, hipStream_t) { return hipErrorInvalidDeviceFunction; }
+#endif
+#endif
 }  // namespace cardan
 
 using namespace cardan;
@@ -802,7 +806,7 @@ int cardan_ffn_forward(const cardan_ffn_shape* shape, int32_t N, const cardan_bf
   A.g = gate;
   A.u = up;
   A.h = hidden ? hidden : A.dg;
-  const hipError_t e = launch_ffn_forward ? launch_ffn_forward(A, stream) : hipErrorInvalidDeviceFunction;
+  const hipError_t e = launch_ffn_forward(A, stream);
   return e == hipSuccess ? CARDAN_OK : hip_fail(e, "ffn forward launch");
 }
 
@@ -837,7 +841,7 @@ int cardan_ffn_backward(const cardan_ffn_shape* shape, int32_t N, const cardan_b
   A.dWg = dW_gate;
   A.dWu = dW_up;
   A.dWd = dW_down;
-  const hipError_t e = launch_ffn_backward ? launch_ffn_backward(A, stream) : hipErrorInvalidDeviceFunction;
+  const hipError_t e = launch_ffn_backward(A, stream);
   return e == hipSuccess ? CARDAN_OK : hip_fail(e, "ffn backward launch");
 }
 
@@ -891,7 +895,7 @@ int cardan_distill_loss(int32_t N, int32_t V, int32_t K, int32_t logits_type, co
   A.ce_weight = ce_weight;
   A.loss = loss;
   A.dlogits = dlogits;
-  const hipError_t e = launch_distill ? launch_distill(A, stream) : hipErrorInvalidDeviceFunction;
+  const hipError_t e = launch_distill(A, stream);
   return e == hipSuccess ? CARDAN_OK : hip_fail(e, "distillation launch");
 }
 
