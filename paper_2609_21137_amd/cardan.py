@@ -541,7 +541,10 @@ def ffn_forward(x, W_gate, W_up, W_down, offsets=None, act: str = "silu_glu", sa
     (bf16; rows in no group are not written), and with ``save=True`` also the
     activations ``(gate, up, hidden)`` that ``ffn_backward`` reads (float32,
     float32, bf16, ``[N, I]``; ``gate`` is None for up-only experts).
-    ``out`` and ``saved`` give the tensors to write."""
+    ``out`` and ``saved`` give the tensors to write.
+
+    The outputs carry no autograd graph, also where an input requires a
+    gradient: gradients come from ``ffn_backward``."""
     shape, N, weights, off, ws = _ffn_call(x, W_gate, W_up, W_down, offsets, act, ws)
     H, I, dev = shape.H, shape.I, x.device
     bf, f32 = torch.bfloat16, torch.float32
@@ -569,7 +572,8 @@ def ffn_backward(dy, x, W_gate, W_up, W_down, saved, offsets=None, act: str = "s
     (bf16), from the activations ``saved`` by it. Returns ``(dx, dW_gate,
     dW_up, dW_down)`` in bf16, laid out as their inputs (rows in no group of
     dx are not written; weight gradients of a group without rows are zero);
-    None where not asked for. ``out`` gives the four tensors to write."""
+    None where not asked for. ``out`` gives the four tensors to write; nothing
+    is added to an input's ``.grad``."""
     shape, N, weights, off, ws = _ffn_call(x, W_gate, W_up, W_down, offsets, act, ws)
     H, I, dev = shape.H, shape.I, x.device
     bf, f32 = torch.bfloat16, torch.float32
@@ -623,7 +627,8 @@ def distill_loss(logits, teacher, ids, labels=None, temperature: float = 1.0, ce
     ``sum_n row_weight[n] (kd_n + ce_weight ce_n)`` in the logits' type and
     with rows padded as theirs, or None with ``grad=False``. ``dlogits=logits`` overwrites the
     logits. Ids and labels outside ``[0, V)`` mark absent entries and labels, and a
-    teacher's logit of -inf an absent entry."""
+    teacher's logit of -inf an absent entry. The losses carry no autograd graph,
+    also where the logits require a gradient: ``dlogits`` is it."""
     if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or logits.dtype not in (torch.bfloat16, torch.float32):
         raise ValueError("logits must be a [N, V] tensor of bfloat16 or float32")
     N, V = logits.shape
