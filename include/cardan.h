@@ -367,7 +367,8 @@ enum {
  * teacher's distribution is over the others; a row without any has kd = 0); a label outside [0, V) is none (ce =
  * 0); labels may be NULL. A row with neither gets zero loss and gradient and
  * its logits are not looked at. An entry named twice counts with both its
- * probabilities. -inf logits have probability 0; NaN or +inf among a row's
+ * probabilities. -inf logits have probability 0 (a row of nothing else has no
+ * softmax and gives NaN); NaN or +inf among a row's
  * logits give that row NaN; among the kept logits of its entries they give NaN
  * in kd and in the gradient at those entries. Values between V and the row strides are neither
  * read nor written.
