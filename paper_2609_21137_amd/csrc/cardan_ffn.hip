@@ -841,10 +841,13 @@ Launch plan(const FfnArgs& A, const FfnProduct& p, const FfnChoice& c, int cus) 
   Launch L;
   L.G.col_tiles = (p.cols + BC - 1) / BC;
   L.G.row_tiles = kDW ? (int)((p.rows + BM - 1) / BM) : 0;
-  // 8 row tiles (4 of both gradients): 12 tiles of operands for 32 products.
-  // Gradients of short sums are bound by their stores, which want whole output
-  // rows (6144 rows of 128 up-only experts: 647 us, in bands 844).
-  L.G.band_log = kDW && p.steps < 32 ? 0 : p.mats == 2 ? 2 : 3;
+  // 8 row tiles (4 of both gradients): 12 tiles of operands for 32 products. Against
+  // bands of one row tile, dW of gate/up and of down, us: 48 experts of 2688 x 1856,
+  // sums of 1 step 257 and 134 -> 235 and 131, of 8 steps 631 and 325 -> 570 and 330;
+  // 64 of 2048 x 1024, 8 steps 342 and 170 -> 339 and 169; 4096 x 11008, 128 steps
+  // 1175 and 624 -> 1076 and 584. Only one group of few rows is slower (33 rows of
+  // 4096 x 11008: 42 -> 45).
+  L.G.band_log = p.mats == 2 ? 2 : 3;
   L.G.band = Divisor((int64_t)L.G.col_tiles << L.G.band_log);
   L.G.group = Divisor(std::max<int64_t>(1, (int64_t)L.G.row_tiles * L.G.col_tiles * p.mats));
   // at most this many tiles (groups end inside tiles); the kernel counts them
