@@ -8,7 +8,8 @@
 //   d/ds [w (kd + c ce)] = w T (q - sum_j p_j 1_{i_j}) + w c (r - 1_label)
 //
 // Bound by the logits' read and the gradient's write: 8192 x 128256 bf16 in
-// 922 us (4.6 TB/s of those bytes), 1500 x 151936 float32 in 391 us (4.7).
+// 922 us (4.6 TB/s of those bytes; T = 2, 896 at T = 1 and 1005 at others, with two
+// exponentials a value), 1500 x 151936 float32 in 391 us (4.7).
 #include <hip/hip_runtime.h>
 
 #include "cardan_ffn.h"
@@ -350,9 +351,9 @@ hipError_t run(const DistillArgs& A, hipStream_t s) {
 // that several rows share a CU; 16 vectors a thread fit beside the kernel's
 // other registers. bf16 rows of more than 128 KiB keep half: two rows a CU,
 // one of which computes while the other loads or stores, beat the second read
-// of the rest (8192 x 128256: 945 us, all of one row in 1024 threads' registers
-// 1066); float32 rows, with half the exponentials a byte, keep 256 KiB (1500 x
-// 151936: 393 us against 444).
+// of the rest (8192 x 128256: 922 us, all of one row in 1024 threads' registers
+// 1058); float32 rows, with half the exponentials a byte, keep 256 KiB (1500 x
+// 151936: 391 us against 443).
 template <bool F32, int MODE>
 hipError_t run_rows(const DistillArgs& A, hipStream_t s) {
   const int64_t vecs = ((int64_t)A.V * (F32 ? 4 : 2) + 15) / 16;

@@ -7,11 +7,15 @@
 //
 // Every product runs on v_mfma_f32_16x16x32_bf16 with float32 accumulators. g
 // and u are kept in float32, so that h, dg and du, which enter the second
-// products in bf16, are rounded once.
+// products in bf16, are rounded once (pack4() below): half a step, 2^-8, of their
+// values. Outputs are then off by 2.3e-3 of their norm, two roundings' root of
+// squares, where one that is rounded at the end alone is off by 1.7e-3. More bits
+// of h, dg and du would be a second product of their low halves: six of a training
+// step's nine products twice.
 //
-// Measured at 8192 rows, 4096 x 11008: gate/up 1.11 PFLOP/s (0.9 GB of kept
-// projections and h beside it), down 1.33, dh 0.97 (1.1 GB in its epilogues),
-// dx 1.30, weight gradients 1.25; MFMA busy 65 to 77 % of the cycles (57 % in dh).
+// Measured at 8192 rows, 4096 x 11008: gate/up 1.15 PFLOP/s (0.9 GB of kept
+// projections and h beside it), down 1.38, dh 0.99 (1.1 GB in its epilogues),
+// dx 1.34, weight gradients 1.33; MFMA busy 63 to 75 % of the cycles (52 % in dh).
 // 6144 rows of 128 experts, 2688 x 1856: weights at 5 TB/s.
 #include <hip/hip_runtime.h>
 

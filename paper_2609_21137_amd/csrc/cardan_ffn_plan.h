@@ -62,9 +62,10 @@ inline size_t ffn_partial_bytes(int32_t N, int32_t H, int32_t I, bool gated) {
 
 // Tiles (output rows x columns), their waves and stages of LDS, and the time of
 // one step of 64 of the sum, measured with every CU busy: with as many workgroups
-// on a CU as fit (y = h Wd of 8192 rows, 4096 x 11008: 1.31, 1.07, 0.85, 0.99,
-// 0.70 and 0.44 PFLOP/s), and with one, where that differs (two tiles of 32 x 128
-// on a CU take 0.61 us a step, one alone 0.27; 64 x 128 0.78 and 0.35).
+// on a CU as fit, and with one, where that differs. y = h Wd of 8192 rows, 4096 x
+// 11008, runs at 1.32, 1.18, 0.89, 1.05, 0.69 and 0.36 PFLOP/s; over the four row
+// products two tiles of 32 x 128 on a CU take 0.47 to 0.71 us a step and one alone
+// 0.25 to 0.32, of 64 x 128 0.65 to 0.81 and 0.30 to 0.42.
 struct FfnTile {
   int bm, bn, wm, wn, stages;
   double step_us, alone_us;
@@ -177,7 +178,8 @@ inline FfnChoice choose_ffn(const FfnProduct& p, int cus) {
 }
 
 // Whether a forward pass takes the kernels for few rows: one launch a product,
-// no join, but 3 TB/s of weights against the tiles' 4.8.
+// no join, but 2.5 TB/s of weights and less (one row, 2048 x 1408: 2.5 in the
+// first product, 1.0 in the second) against the tiles' 4.8.
 inline bool few_rows(int32_t N, int32_t H, int32_t I, bool grouped) {
   return !grouped && N <= 64 && (int64_t)H * I * ((N + 15) / 16) <= (6 << 20);
 }
