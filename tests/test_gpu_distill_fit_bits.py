@@ -43,3 +43,12 @@ def test_gradient_behind_the_head_is_float32(C, act, monkeypatch):
     assert seen["dy"].dtype == torch.float32
     err = (seen["dy"].double() - g @ h).abs()
     assert (err <= (head.shape[1] + 2) * 2.0 ** -24 * (g.abs() @ h.abs())).all()
+
+
+@pytest.mark.parametrize("act", ["silu_glu", "relu2_up"])
+def test_a_batch_without_rows(C, act):
+    L, k, d, x, head, teacher, ids, labels = _setup(act, 8, False)
+    student = fit.TrainedLayer(L, k, d, act)
+    loss, grads = fit.distill_step(student, x[:0], head, teacher[:0], ids[:0], labels=labels[:0])
+    assert loss.shape == (0, 2) and set(grads) == set(student.factors)
+    assert all((g == 0).all() and g.shape == student.factors[n].shape for n, g in grads.items())
