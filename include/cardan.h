@@ -346,6 +346,7 @@ int cardan_ffn_backward(const cardan_ffn_shape* shape, int32_t N, const cardan_b
 enum {
   CARDAN_LOGITS_BF16 = 0,
   CARDAN_LOGITS_F32 = 1,
+  CARDAN_LOGITS_F64 = 2, /* routing calls alone */
   /* added to either: logits, teacher, ids, loss and dlogits need only start on
    * a multiple of their own elements' size (a slice of rows of odd length) */
   CARDAN_LOGITS_ANY_START = 16
@@ -379,6 +380,135 @@ int cardan_distill_loss(int32_t N, int32_t V, int32_t K, int32_t logits_type, co
                         const int32_t* labels, float temperature, float ce_weight,
                         const float* row_weight, float* loss, void* dlogits, int64_t dld,
                         hipStream_t stream);
+
+/* ---- training: the router, rows to their experts and back, the optimizer ---
+ * What a routed layer of any number of rows has around its feed-forward block
+ * (paper Sec. 2.1, Sec. 3.3): the routing whose places and offsets
+ * cardan_ffn_forward's rows follow, with its gradient; the copies of the rows
+ * and their weighted sums, with theirs; and the step that the gradients go
+ * into. Conventions as for the training calls above, except that every pointer
+ * need only start on a multiple of its own elements' size. */
+
+enum { CARDAN_SCORE_SOFTMAX = 0, CARDAN_SCORE_SIGMOID = 1 };
+
+/* How rows choose among E experts. 1 <= E <= 1024, 1 <= top_k <= min(E, 32),
+ * 1 <= groups <= 64 dividing E, top_groups * (E / groups) >= top_k, group_best
+ * 1 or 2 and at most E / groups, scale finite. groups = top_groups = group_best
+ * = 1: no groups. */
+typedef struct {
+  int32_t E, top_k;
+  int32_t score;      /* CARDAN_SCORE_SOFTMAX or CARDAN_SCORE_SIGMOID         */
+  int32_t renorm;     /* 1: weights are divided by the sum of the kept scores */
+  int32_t groups;     /* groups of E / groups consecutive experts             */
+  int32_t top_groups; /* groups that a row may choose from                    */
+  int32_t group_best; /* a group counts by its best (1) or best two (2)       */
+  float scale;        /* factor of every weight                               */
+} cardan_routing;
+
+/* Workspace bytes of cardan_route_rows with places for up to N rows (0 for
+ * few rows). No zero fill is needed, nothing is kept between calls. Host-only. */
+int cardan_route_rows_workspace_bytes(const cardan_routing* routing, int32_t N, size_t* out);
+
+/* Routing of N rows of logits z (row n at logits + n * ld; bf16, float32 or
+ * float64). Scores s_e = softmax(z)_e over all E or sigmoid(z_e). The selection
+ * goes by v_e = s_e + bias_e in float64 (bias: [E] float32, or NULL) where there
+ * is a bias or group_best is 2 with groups; else by z_e, in the scores' order. A
+ * group counts by its best v or the sum of its best two; of the top_groups best
+ * groups (ties to the lower index) the top_k largest v are kept, descending,
+ * exact ties to the lower index. weight_j = scale * s_j, divided by the sum of
+ * the kept s with renorm; the bias is in no weight. With softmax, renorm, no
+ * bias and no groups this is cardan_route_topk's routing.
+ * idx [N][top_k] int32, weight [N][top_k] float32.
+ * A logit of -inf (or a v of -inf) is an expert that is not there; where fewer
+ * than top_k are left (a padding row is one of -inf alone) the rest of idx is
+ * -1 with weight 0. A NaN among a row's logits or v is never selected and makes
+ * the row's weights NaN; +inf makes a softmax row's weights NaN.
+ * place [N][top_k] and offsets [E + 1] (both or neither NULL): the (row,
+ * selection) pairs of an expert e are rows offsets[e] <= p < offsets[e + 1] of
+ * the array grouped by expert, in their order, place their p; -1 where idx is.
+ * ws is read with places alone. N * top_k below 2^31; N may be 0 (offsets are
+ * zero then). Rows up to 2^40 elements apart. */
+int cardan_route_rows(const cardan_routing* routing, int32_t N, int32_t logits_type, const void* logits, int64_t ld,
+                      const float* bias, int32_t* idx, float* weight, int32_t* place, int32_t* offsets, void* ws,
+                      size_t ws_bytes, hipStream_t stream);
+
+/* Gradient of the logits for the gradient dweight [N][top_k] of
+ * cardan_route_rows's weights at the experts idx that it chose (the selection
+ * itself has none): with w the weights before scale and d = scale * dweight,
+ *   renorm:  dz_j = w_j (d_j - sum_i w_i d_i), times (1 - s_j) with sigmoid
+ *   sigmoid: dz_j = s_j (1 - s_j) d_j
+ *   softmax: dz_e = s_e (d_e [e chosen] - sum_i s_i d_i) for every expert
+ * in the logits' type, rounded once, written whole (zero at other experts).
+ * dlogits may be the logits' own memory (dld == ld), and must not overlap them
+ * otherwise. idx outside [0, E): no expert, its dweight is not looked at. An
+ * expert named twice in a row gets one of its gradients. */
+int cardan_route_rows_backward(const cardan_routing* routing, int32_t N, int32_t logits_type, const void* logits,
+                               int64_t ld, const int32_t* idx, const float* dweight, void* dlogits, int64_t dld,
+                               hipStream_t stream);
+
+/* xe[place[n][j]] = x[n] for the k places of every row: x [N][H] bf16, place
+ * [N][k] int32, xe [M][H] bf16. Places outside [0, M) are none; rows of xe that
+ * no place names are left as they were; a row named twice gets one of the two.
+ * 1 <= k <= 32, 1 <= H <= 2^20. The gradient is cardan_combine_rows without
+ * weights. */
+int cardan_dispatch_rows(int32_t N, int32_t k, int32_t H, int32_t M, const cardan_bf16* x, const int32_t* place,
+                         cardan_bf16* xe, hipStream_t stream);
+
+/* y[n] = sum_j weight[n][j] * ye[place[n][j]] in float32 in the order of j,
+ * rounded once to y's type (CARDAN_LOGITS_BF16 or _F32): ye [M][H] bf16, weight
+ * [N][k] float32 or NULL for ones, y [N][H]. Places outside [0, M) add nothing
+ * (their weights are not looked at); a row without any is zero. */
+int cardan_combine_rows(int32_t N, int32_t k, int32_t H, int32_t M, const cardan_bf16* ye, const int32_t* place,
+                        const float* weight, int32_t y_type, void* y, hipStream_t stream);
+
+/* Gradients of cardan_combine_rows for dy [N][H] (bf16 or float32):
+ *   dye[place[n][j]] = weight[n][j] * dy[n]   (bf16; rows without a place stay)
+ *   dweight[n][j] = <dy[n], ye[place[n][j]]>  (float32; 0 without a place)
+ * dye or dweight may be NULL (not computed; ye is read for dweight alone). */
+int cardan_combine_rows_backward(int32_t N, int32_t k, int32_t H, int32_t M, int32_t dy_type, const void* dy,
+                                 const cardan_bf16* ye, const int32_t* place, const float* weight, cardan_bf16* dye,
+                                 float* dweight, hipStream_t stream);
+
+/* One tensor of an optimizer step (device pointers). n values each; with
+ * 8-bit moments m holds e4m3 and v e5m2 values, and each has a float32 scale
+ * for every 256 consecutive values ([ceil(n / 256)]). Zeros are the state
+ * before the first step. */
+typedef struct {
+  void* param;        /* weights, updated                                     */
+  const void* grad;
+  void* m;            /* first moment, updated                                */
+  void* v;            /* second moment, updated                               */
+  float* m_scale;     /* 8-bit moments alone                                  */
+  float* v_scale;
+  cardan_bf16* copy;  /* receives float32 weights rounded to bf16, or NULL    */
+  int64_t n;          /* values, 0 allowed                                    */
+} cardan_adamw_tensor;
+
+typedef struct {
+  int32_t param_type;          /* CARDAN_LOGITS_BF16 or _F32, of all tensors  */
+  int32_t grad_type;           /* likewise                                    */
+  int32_t state_bits;          /* 32 (float32 moments) or 8                   */
+  int32_t step;                /* t >= 1, unless step_device                  */
+  double lr, beta1, beta2, eps, weight_decay;
+  const int32_t* step_device;  /* t on the device (below 1 counts as 1), or NULL */
+  const float* lr_device;      /* lr on the device, or NULL                   */
+  const float* grad_scale;     /* factor of every gradient, on the device, or NULL (1) */
+} cardan_adamw;
+
+/* AdamW over `count` tensors (`tensors` is a host array; up to 40 share a
+ * launch), for value p with gradient g (times grad_scale) at step t:
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
+ *   p = p - lr weight_decay p - lr m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps)
+ * in float32. 8-bit moments enter the update as computed and are stored
+ * rounded, with a scale of the largest size of their 256 over 448 (m) or
+ * 57344 (v); these roundings, and those of bf16 weights, are dithered by a mix
+ * of a value's place in its tensor and t (right in the mean; the same arguments
+ * give the same result). Copies are rounded to nearest. A gradient that is not
+ * finite goes on into its weight and moments; with 8-bit moments into those of
+ * its 256 values. With step_device and lr_device a captured call follows both.
+ * Tensors must not overlap one another. */
+int cardan_adamw_step(const cardan_adamw* config, int32_t count, const cardan_adamw_tensor* tensors,
+                      hipStream_t stream);
 
 /* Kernel timing for measurement. cardan_profile_begin(n) makes the next n
  * calls launch each kernel with a HIP start/stop event pair recorded by the

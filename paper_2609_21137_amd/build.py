@@ -17,7 +17,8 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libcardan.so")
 SOURCES = ["cardan_kernels.hip", "cardan_api.hip", "cardan_planner.cpp",
-           "cardan_ffn.hip", "cardan_distill.hip"]
+           "cardan_ffn.hip", "cardan_distill.hip", "cardan_route.hip", "cardan_rows.hip",
+           "cardan_adamw.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

@@ -56,6 +56,22 @@ class FfnWeightsStruct(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("W_gate", "W_up", "W_down")]
 
 
+class Routing(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("E", "top_k", "score", "renorm", "groups", "top_groups",
+                                              "group_best")] + [("scale", ctypes.c_float)]
+
+
+class AdamwTensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("param", "grad", "m", "v", "m_scale", "v_scale", "copy")]
+    _fields_ += [("n", ctypes.c_int64)]
+
+
+class Adamw(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("param_type", "grad_type", "state_bits", "step")]
+    _fields_ += [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")]
+    _fields_ += [(n, ctypes.c_void_p) for n in ("step_device", "lr_device", "grad_scale")]
+
+
 class LayerStruct(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in LAYER_FIELDS]
 
@@ -75,6 +91,7 @@ def _load():
     dp = ctypes.POINTER(DenseLayerStruct)
     fp = ctypes.POINTER(FfnShape)
     wp = ctypes.POINTER(FfnWeightsStruct)
+    rp = ctypes.POINTER(Routing)
     i64, f32 = ctypes.c_int64, ctypes.c_float
     sig = {
         "cardan_abi_version": ([], ctypes.c_int),
@@ -97,6 +114,13 @@ def _load():
         "cardan_ffn_backward": ([fp, i32, vp, vp, vp, wp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp], ctypes.c_int),
         "cardan_distill_loss": ([i32, i32, i32, i32, vp, i64, vp, vp, vp, f32, f32, vp, vp, vp, i64, vp],
                                 ctypes.c_int),
+        "cardan_route_rows_workspace_bytes": ([rp, i32, ctypes.POINTER(sz)], ctypes.c_int),
+        "cardan_route_rows": ([rp, i32, i32, vp, i64, vp, vp, vp, vp, vp, vp, sz, vp], ctypes.c_int),
+        "cardan_route_rows_backward": ([rp, i32, i32, vp, i64, vp, vp, vp, i64, vp], ctypes.c_int),
+        "cardan_dispatch_rows": ([i32, i32, i32, i32, vp, vp, vp, vp], ctypes.c_int),
+        "cardan_combine_rows": ([i32, i32, i32, i32, vp, vp, vp, i32, vp, vp], ctypes.c_int),
+        "cardan_combine_rows_backward": ([i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp], ctypes.c_int),
+        "cardan_adamw_step": ([ctypes.POINTER(Adamw), i32, ctypes.POINTER(AdamwTensor), vp], ctypes.c_int),
         "cardan_profile_begin": ([i32], ctypes.c_int),
         "cardan_profile_end": ([ctypes.POINTER(ctypes.c_float), ctypes.POINTER(i32)], ctypes.c_int),
     }
@@ -117,6 +141,9 @@ EXPORTED = (
     "cardan_rmsnorm_bf16",
     "cardan_ffn_workspace_bytes", "cardan_ffn_forward", "cardan_ffn_backward",
     "cardan_distill_loss",
+    "cardan_route_rows_workspace_bytes", "cardan_route_rows", "cardan_route_rows_backward",
+    "cardan_dispatch_rows", "cardan_combine_rows", "cardan_combine_rows_backward",
+    "cardan_adamw_step",
     "cardan_profile_begin", "cardan_profile_end",
 )
 
@@ -650,6 +677,262 @@ def distill_loss(logits, teacher, ids, labels=None, temperature: float = 1.0, ce
     with _Device(dev) as stream:
         _check(_lib.cardan_distill_loss(N, V, K, _ANY_START + (1 if dt is f32 else 0), lp, ld, *args, stream))
     return loss, dlogits
+
+
+# ---------------------------------------------------------------------------
+# training: the router, rows to their experts and back, the optimizer
+# ---------------------------------------------------------------------------
+SCORES = {"softmax": 0, "sigmoid": 1}
+_TYPES = {torch.bfloat16: 0, torch.float32: 1, torch.float64: 2}
+
+
+@functools.lru_cache(maxsize=256)
+def _routing(E, top_k, score, renorm, scale, groups, top_groups, group_best) -> Routing:
+    if score not in SCORES:
+        raise ValueError(f"unknown score {score!r}")
+    return Routing(E, top_k, SCORES[score], int(bool(renorm)), groups, top_groups, group_best, scale)
+
+
+def route_rows_workspace_bytes(N: int, E: int, top_k: int, score: str = "softmax", renorm: bool = True,
+                               scale: float = 1.0, groups: int = 1, top_groups: int = 1, group_best: int = 1) -> int:
+    """Bytes of workspace of ``route_rows`` over up to N rows (no zero fill
+    needed; nothing is kept in it between calls)."""
+    out = ctypes.c_size_t(0)
+    r = _routing(E, top_k, score, renorm, scale, groups, top_groups, group_best)
+    _check(_lib.cardan_route_rows_workspace_bytes(ctypes.byref(r), N, ctypes.byref(out)))
+    return out.value
+
+
+@functools.lru_cache(maxsize=256)
+def _route_bytes(E, top_k, N):
+    return route_rows_workspace_bytes(N, E, top_k)
+
+
+def _logit_rows(logits):
+    if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or logits.dtype not in _TYPES:
+        raise ValueError("logits must be a [N, E] tensor of bfloat16, float32 or float64")
+    lp, ld = _rows_ptr(logits, logits.dtype, "logits", logits.shape, logits.device)
+    return lp, ld, _TYPES[logits.dtype]
+
+
+def route_rows(logits, top_k: int, bias=None, score: str = "softmax", renorm: bool = True, scale: float = 1.0,
+               groups: int = 1, top_groups: int = 1, group_best: int = 1, places: bool = True, ws=None, out=None):
+    """Routing of rows of any number by their ``logits [N, E]`` (bf16, float32
+    or float64; rows may be padded): the ``top_k`` experts of each row and
+    their weights.
+
+    ``score``: ``"softmax"`` over all experts or ``"sigmoid"``; ``bias``
+    (float32 ``[E]``) takes part in the selection alone; with ``groups`` a row
+    chooses among the experts of its ``top_groups`` best groups, which count by
+    their best expert or by their best two (``group_best``). The weights are the
+    scores, divided by their sum with ``renorm``, times ``scale``. Ties go to
+    the lower index; selections of equal scores are decided in float64.
+
+    Returns ``(idx, weight, place, offsets)``: int32 and float32 ``[N, top_k]``,
+    and the rows' places in an array grouped by expert (int32 ``[N, top_k]``)
+    with its ``offsets`` (int32 ``[E + 1]``), as ``dispatch_rows``,
+    ``ffn_forward`` and ``combine_rows`` take them (None, None with
+    ``places=False``). An expert whose logit is -inf is never chosen; where a
+    row has fewer than ``top_k`` others (a padding row has none) ``idx`` and
+    ``place`` are -1 and the weight is 0. ``out`` gives the four tensors to
+    write. The weights carry no autograd graph: their gradient goes through
+    ``route_rows_backward``."""
+    lp, ld, kind = _logit_rows(logits)
+    N, E = logits.shape
+    dev, i32, f32 = logits.device, torch.int32, torch.float32
+    r = _routing(E, top_k, score, renorm, scale, groups, top_groups, group_best)
+    if out is not None:
+        idx, weight, place, offsets = out
+    else:
+        idx, weight = torch.empty((N, top_k), dtype=i32, device=dev), torch.empty((N, top_k), dtype=f32, device=dev)
+        place, offsets = (torch.empty((N, top_k), dtype=i32, device=dev),
+                          torch.empty((E + 1,), dtype=i32, device=dev)) if places else (None, None)
+    need = _route_bytes(E, top_k, N) if offsets is not None else 0
+    if ws is None:
+        ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    elif ws.dtype is not torch.uint8 or ws.device != dev or not ws.is_contiguous():
+        raise ValueError(f"ws must be a contiguous uint8 tensor on {dev}")
+    args = (_arg(bias, f32, "bias", (E,), dev, True), _arg(idx, i32, "idx", (N, top_k), dev),
+            _arg(weight, f32, "weight", (N, top_k), dev), _arg(place, i32, "place", (N, top_k), dev, offsets is None),
+            _arg(offsets, i32, "offsets", (E + 1,), dev, place is None))
+    with _Device(dev) as stream:
+        _check(_lib.cardan_route_rows(ctypes.byref(r), N, kind, lp, ld, *args, ws.data_ptr() if ws is not None else None,
+                                      ws.numel() if ws is not None else 0, stream))
+    return idx, weight, place, offsets
+
+
+def route_rows_backward(logits, idx, dweight, top_k: int | None = None, score: str = "softmax", renorm: bool = True,
+                        scale: float = 1.0, groups: int = 1, top_groups: int = 1, group_best: int = 1, out=None):
+    """Gradient of ``route_rows``'s ``logits`` for the gradient ``dweight [N,
+    top_k]`` (float32) of its weights, at the experts ``idx`` that it chose; the
+    other arguments as there. In the logits' type, whole rows (zero at experts
+    that the weights do not depend on); ``out=logits`` overwrites the logits.
+    Where ``idx`` is -1 ``dweight`` is not looked at."""
+    lp, ld, kind = _logit_rows(logits)
+    N, E = logits.shape
+    dev = logits.device
+    if not isinstance(idx, torch.Tensor) or idx.dim() != 2 or (top_k is not None and idx.shape[1] != top_k):
+        raise ValueError("idx must be a [N, top_k] tensor")
+    k = idx.shape[1]
+    r = _routing(E, k, score, renorm, scale, groups, top_groups, group_best)
+    d = out if out is not None else torch.empty((N, E), dtype=logits.dtype, device=dev)
+    dp, dld = _rows_ptr(d, logits.dtype, "out", (N, E), dev)
+    args = (_arg(idx, torch.int32, "idx", (N, k), dev), _arg(dweight, torch.float32, "dweight", (N, k), dev))
+    with _Device(dev) as stream:
+        _check(_lib.cardan_route_rows_backward(ctypes.byref(r), N, kind, lp, ld, *args, dp, dld, stream))
+    return d
+
+
+def _row_types(t, name):
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise ValueError(f"{name} must be a two-dimensional tensor")
+    return t.shape
+
+
+def dispatch_rows(x, place, rows: int | None = None, out=None):
+    """Copies of the rows ``x [N, H]`` (bf16) at the places ``place [N, k]``
+    (int32, as ``route_rows`` gives them): ``xe[place[n, j]] = x[n]`` in an
+    array of ``rows`` rows (default N k). Places outside it are none; rows that
+    no place names are not written. The gradient of x is ``combine_rows`` of
+    xe's, without weights."""
+    N, H = _row_types(x, "x")
+    k = _row_types(place, "place")[1]
+    dev, bf = x.device, torch.bfloat16
+    xe = out if out is not None else torch.empty((N * k if rows is None else rows, H), dtype=bf, device=dev)
+    M = _row_types(xe, "out")[0]
+    args = (_arg(x, bf, "x", (N, H), dev), _arg(place, torch.int32, "place", (N, k), dev), _arg(xe, bf, "out", (M, H), dev))
+    with _Device(dev) as stream:
+        _check(_lib.cardan_dispatch_rows(N, k, H, M, *args, stream))
+    return xe
+
+
+def combine_rows(ye, place, weight=None, dtype=torch.bfloat16, out=None):
+    """Sums of the rows ``ye [M, H]`` (bf16) that ``place [N, k]`` names,
+    weighted by ``weight [N, k]`` (float32; None: ones): ``y[n] = sum_j weight[n,
+    j] ye[place[n, j]]``, in float32 in the order of j, as bf16 or float32
+    (``dtype``) ``[N, H]``. Places outside ``[0, M)`` add nothing. The result
+    carries no autograd graph: ``combine_rows_backward``."""
+    M, H = _row_types(ye, "ye")
+    N, k = _row_types(place, "place")
+    dev = ye.device
+    y = out if out is not None else torch.empty((N, H), dtype=dtype, device=dev)
+    if not isinstance(y, torch.Tensor) or y.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("y is bfloat16 or float32")
+    args = (_arg(ye, torch.bfloat16, "ye", (M, H), dev), _arg(place, torch.int32, "place", (N, k), dev),
+            _arg(weight, torch.float32, "weight", (N, k), dev, True), _TYPES[y.dtype], _arg(y, y.dtype, "out", (N, H), dev))
+    with _Device(dev) as stream:
+        _check(_lib.cardan_combine_rows(N, k, H, M, *args, stream))
+    return y
+
+
+def combine_rows_backward(dy, ye, place, weight=None, need_dye: bool = True, need_dweight: bool = True, dye=None,
+                          dweight=None):
+    """Gradients of ``combine_rows`` for ``dy [N, H]`` (bf16 or float32):
+    ``dye[place[n, j]] = weight[n, j] dy[n]`` (bf16, laid out as ye; rows that no
+    place names are not written) and ``dweight[n, j] = <dy[n], ye[place[n, j]]>``
+    (float32, 0 without a place). Returns ``(dye, dweight)``, None where not
+    asked for; ``dye`` and ``dweight`` give the tensors to write."""
+    M, H = _row_types(ye, "ye")
+    N, k = _row_types(place, "place")
+    dev = ye.device
+    if not isinstance(dy, torch.Tensor) or dy.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("dy must be a [N, H] tensor of bfloat16 or float32")
+    if dye is None and need_dye:
+        dye = torch.empty_like(ye)
+    if dweight is None and need_dweight:
+        dweight = torch.empty((N, k), dtype=torch.float32, device=dev)
+    args = (_TYPES[dy.dtype], _arg(dy, dy.dtype, "dy", (N, H), dev), _arg(ye, torch.bfloat16, "ye", (M, H), dev),
+            _arg(place, torch.int32, "place", (N, k), dev), _arg(weight, torch.float32, "weight", (N, k), dev, True),
+            _arg(dye, torch.bfloat16, "dye", (M, H), dev, True), _arg(dweight, torch.float32, "dweight", (N, k), dev, True))
+    with _Device(dev) as stream:
+        _check(_lib.cardan_combine_rows_backward(N, k, H, M, *args, stream))
+    return dye, dweight
+
+
+ADAMW_BLOCK = 256  # values of a tensor that share a scale of 8-bit moments
+
+
+def adamw_state(param, bits: int = 32):
+    """Moments of ``param`` before its first ``adamw_step``: ``(m, v)`` in
+    float32, or with ``bits=8`` ``(m, v, m_scale, v_scale)``: float8_e4m3fn and
+    float8_e5m2 values with a float32 scale for every 256 of them (in the order
+    of the tensor's elements), so that m is ``m.float() * its scale``."""
+    dev, n = param.device, param.numel()
+    if bits == 32:
+        return tuple(torch.zeros(param.shape, dtype=torch.float32, device=dev) for _ in range(2))
+    if bits != 8:
+        raise ValueError("bits is 8 or 32")
+    blocks = -(-n // ADAMW_BLOCK)
+    return (torch.zeros(param.shape, dtype=torch.uint8, device=dev).view(torch.float8_e4m3fn),
+            torch.zeros(param.shape, dtype=torch.uint8, device=dev).view(torch.float8_e5m2),
+            torch.zeros(blocks, dtype=torch.float32, device=dev), torch.zeros(blocks, dtype=torch.float32, device=dev))
+
+
+def _scalar(t, dtype, name, dev):
+    if t.dim() > 1 or t.numel() != 1:
+        raise ValueError(f"{name} must hold one value")
+    return _arg(t, dtype, name, t.shape, dev)
+
+
+def adamw_step(params, grads, states, step, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0,
+               grad_scale=None, copies=None):
+    """One AdamW step over many tensors, in place: ``params`` (all float32 or
+    all bf16), their ``grads`` (all float32 or all bf16; a parameter whose
+    gradient is None is left out) and their ``states`` (``adamw_state``, all of one
+    kind), at ``step`` (1 for the first).
+
+    ``m = b1 m + (1 - b1) g``, ``v = b2 v + (1 - b2) g^2``, ``p -= lr
+    (weight_decay p + m / (1 - b1^t) / (sqrt(v / (1 - b2^t)) + eps))`` in float32.
+    8-bit moments and bf16 weights are stored with dithered rounding (right in
+    the mean, a function of step and place). ``step`` (int32) and ``lr`` (float32)
+    may be one-element tensors on the device, which a captured call then follows;
+    ``grad_scale`` (float32, one element on the device) multiplies every
+    gradient. ``copies``: bf16 tensors (or None) that receive float32 weights
+    rounded to bf16, as ``ffn_forward`` takes them."""
+    params, grads, states = list(params), list(grads), list(states)
+    copies = [None] * len(params) if copies is None else list(copies)
+    if not len(params) == len(grads) == len(states) == len(copies):
+        raise ValueError("params, grads, states and copies must have one entry for each tensor")
+    todo = [t for t in zip(params, grads, states, copies) if t[1] is not None]
+    if not todo:
+        return
+    p, g, s, _ = todo[0]
+    if not isinstance(p, torch.Tensor) or not isinstance(g, torch.Tensor):
+        raise TypeError("params and grads must be torch tensors")
+    dev, pt, gt, kinds = p.device, p.dtype, g.dtype, len(s)
+    for t, name in ((pt, "params"), (gt, "grads")):
+        if t not in (torch.float32, torch.bfloat16):
+            raise ValueError(f"{name} must be float32 or bfloat16")
+    if kinds not in (2, 4):
+        raise ValueError("a state is (m, v) or (m, v, m_scale, v_scale)")
+    f32 = torch.float32
+    mt, vt = (f32, f32) if kinds == 2 else (torch.float8_e4m3fn, torch.float8_e5m2)
+    table = (AdamwTensor * len(todo))()
+    for e, (p, g, s, c) in zip(table, todo):
+        if len(s) != kinds:
+            raise ValueError("states must be of one kind")
+        shape = getattr(p, "shape", None)
+        e.param, e.grad = _arg(p, pt, "params", shape, dev), _arg(g, gt, "grads", shape, dev)
+        e.m, e.v = _arg(s[0], mt, "m", shape, dev), _arg(s[1], vt, "v", shape, dev)
+        e.n = n = p.numel()
+        if kinds == 4:
+            blocks = (-(-n // ADAMW_BLOCK),)
+            e.m_scale, e.v_scale = _arg(s[2], f32, "m_scale", blocks, dev), _arg(s[3], f32, "v_scale", blocks, dev)
+        if c is not None:
+            e.copy = _arg(c, torch.bfloat16, "copies", shape, dev)
+    conf = Adamw(_TYPES[pt], _TYPES[gt], 32 if kinds == 2 else 8, 0, 0.0, betas[0], betas[1], eps, weight_decay)
+    if isinstance(step, torch.Tensor):
+        conf.step_device = _scalar(step, torch.int32, "step", dev)
+    else:
+        conf.step = step
+    if isinstance(lr, torch.Tensor):
+        conf.lr_device = _scalar(lr, f32, "lr", dev)
+    else:
+        conf.lr = lr
+    if grad_scale is not None:
+        conf.grad_scale = _scalar(grad_scale, f32, "grad_scale", dev)
+    with _Device(dev) as stream:
+        _check(_lib.cardan_adamw_step(ctypes.byref(conf), len(todo), table, stream))
 
 
 def profile_begin(max_calls: int):

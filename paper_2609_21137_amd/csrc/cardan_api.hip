@@ -14,6 +14,7 @@
 
 #include "../../include/cardan.h"
 #include "cardan_ffn.h"
+#include "cardan_rows.h"
 #include "cardan_plan.h"
 
 namespace cardan {
@@ -31,6 +32,12 @@ hipError_t launch_rmsnorm(hipStream_t, int, int, const float*, float, uint16_t*,
 __attribute__((weak)) hipError_t launch_ffn_forward(const FfnArgs&, hipStream_t) { return hipErrorInvalidDeviceFunction; }
 __attribute__((weak)) hipError_t launch_ffn_backward(const FfnArgs&, hipStream_t) { return hipErrorInvalidDeviceFunction; }
 __attribute__((weak)) hipError_t launch_distill(const DistillArgs&, hipStream_t) { return hipErrorInvalidDeviceFunction; }
+__attribute__((weak)) hipError_t launch_route(const RouteArgs&, hipStream_t) { return hipErrorInvalidDeviceFunction; }
+__attribute__((weak)) hipError_t launch_route_backward(const RouteArgs&, hipStream_t) { return hipErrorInvalidDeviceFunction; }
+__attribute__((weak)) hipError_t launch_dispatch(const RowsArgs&, hipStream_t) { return hipErrorInvalidDeviceFunction; }
+__attribute__((weak)) hipError_t launch_combine(const RowsArgs&, hipStream_t) { return hipErrorInvalidDeviceFunction; }
+__attribute__((weak)) hipError_t launch_combine_backward(const RowsArgs&, hipStream_t) { return hipErrorInvalidDeviceFunction; }
+__attribute__((weak)) hipError_t launch_adamw(const AdamwArgs&, bool, bool, bool, hipStream_t) { return hipErrorInvalidDeviceFunction; }
 #endif
 #endif
 }  // namespace cardan
@@ -897,6 +904,291 @@ int cardan_distill_loss(int32_t N, int32_t V, int32_t K, int32_t logits_type, co
   A.dlogits = dlogits;
   const hipError_t e = launch_distill(A, stream);
   return e == hipSuccess ? CARDAN_OK : hip_fail(e, "distillation launch");
+}
+
+}  // extern "C"
+
+namespace {
+
+// A required pointer that starts on its own elements' size.
+int check_start(const void* p, const char* name, uintptr_t size) {
+  if (!p) return fail(CARDAN_ERR_NULL_PTR, "%s is NULL", name);
+  if (reinterpret_cast<uintptr_t>(p) % size) return fail(CARDAN_ERR_ALIGN, "%s is not %d-byte aligned", name, (int)size);
+  return CARDAN_OK;
+}
+#define START(p, name, size)                                  \
+  do {                                                        \
+    if (int rc_ = check_start(p, name, size)) return rc_;     \
+  } while (0)
+
+int check_routing(const cardan_routing* r, int32_t N) {
+  if (!r) return fail(CARDAN_ERR_NULL_PTR, "routing is NULL");
+  if (N < 0 || N > (1 << 30)) return fail(CARDAN_ERR_BAD_SHAPE, "N=%d outside [0, 2^30]", N);
+  if (r->E < 1 || r->E > kMaxE) return fail(CARDAN_ERR_UNSUPPORTED, "E=%d outside [1, %d]", r->E, kMaxE);
+  if (r->top_k < 1 || r->top_k > r->E) return fail(CARDAN_ERR_BAD_SHAPE, "top_k=%d outside [1, E=%d]", r->top_k, r->E);
+  if (r->top_k > 32) return fail(CARDAN_ERR_UNSUPPORTED, "top_k=%d exceeds 32", r->top_k);
+  if ((int64_t)N * r->top_k >= 0x7fffffff) return fail(CARDAN_ERR_UNSUPPORTED, "N=%d times top_k=%d exceeds 2^31", N, r->top_k);
+  if (r->score != CARDAN_SCORE_SOFTMAX && r->score != CARDAN_SCORE_SIGMOID)
+    return fail(CARDAN_ERR_UNSUPPORTED, "score %d is not known", r->score);
+  if (r->renorm != 0 && r->renorm != 1) return fail(CARDAN_ERR_BAD_SHAPE, "renorm is 0 or 1");
+  if (r->groups < 1 || r->groups > 64) return fail(CARDAN_ERR_UNSUPPORTED, "groups=%d outside [1, 64]", r->groups);
+  if (r->E % r->groups) return fail(CARDAN_ERR_BAD_SHAPE, "E=%d is not a multiple of groups=%d", r->E, r->groups);
+  if (r->top_groups < 1 || r->top_groups > r->groups)
+    return fail(CARDAN_ERR_BAD_SHAPE, "top_groups=%d outside [1, groups=%d]", r->top_groups, r->groups);
+  if (r->top_groups * (r->E / r->groups) < r->top_k)
+    return fail(CARDAN_ERR_BAD_SHAPE, "%d groups of %d hold fewer than top_k=%d experts", r->top_groups,
+                r->E / r->groups, r->top_k);
+  if (r->group_best != 1 && r->group_best != 2) return fail(CARDAN_ERR_UNSUPPORTED, "group_best is 1 or 2");
+  if (r->group_best > r->E / r->groups) return fail(CARDAN_ERR_BAD_SHAPE, "groups of one expert have no second best");
+  if (!isfinite(r->scale)) return fail(CARDAN_ERR_BAD_SHAPE, "scale must be finite");
+  return CARDAN_OK;
+}
+
+// What the routing's forward and backward calls share.
+int route_args(const cardan_routing* r, int32_t N, int32_t type, const void* logits, int64_t ld, RouteArgs* A) {
+  int rc = check_routing(r, N);
+  if (rc) return rc;
+  if (type != CARDAN_LOGITS_BF16 && type != CARDAN_LOGITS_F32 && type != CARDAN_LOGITS_F64)
+    return fail(CARDAN_ERR_UNSUPPORTED, "logits type %d is not known", type);
+  if (ld < r->E || ld > (int64_t)1 << 40)
+    return fail(CARDAN_ERR_BAD_SHAPE, "row stride %lld is below E=%d or too large", (long long)ld, r->E);
+  const uintptr_t size = type == CARDAN_LOGITS_F64 ? 8 : type == CARDAN_LOGITS_F32 ? 4 : 2;
+  if (N > 0) START(logits, "logits", size);
+  memset(A, 0, sizeof *A);
+  A->N = N;
+  A->E = r->E;
+  A->k = r->top_k;
+  A->sigmoid = r->score == CARDAN_SCORE_SIGMOID;
+  A->renorm = r->renorm;
+  A->groups = r->groups;
+  A->top_groups = r->top_groups;
+  A->best = r->group_best;
+  A->each = r->E / r->groups;
+  A->type = type;
+  A->scale = r->scale;
+  A->ld = ld;
+  A->logits = logits;
+  // 16 experts at most are one access: whole ones on their own alignment
+  A->wide = r->E % 16 == 0 && reinterpret_cast<uintptr_t>(logits) % 16 == 0 && ld * size % 16 == 0;
+  return CARDAN_OK;
+}
+
+int check_rows(int32_t N, int32_t k, int32_t H, int32_t M, const int32_t* place, RowsArgs* A) {
+  if (N < 0 || N > (1 << 30) || M < 0) return fail(CARDAN_ERR_BAD_SHAPE, "N=%d or M=%d outside the valid range", N, M);
+  if (k < 1 || k > 32) return fail(CARDAN_ERR_UNSUPPORTED, "k=%d outside [1, 32]", k);
+  if (H < 1 || H > (1 << 20)) return fail(CARDAN_ERR_UNSUPPORTED, "H=%d outside [1, 2^20]", H);
+  if (N > 0) START(place, "place", 4);
+  memset(A, 0, sizeof *A);
+  A->N = N;
+  A->k = k;
+  A->H = H;
+  A->M = M;
+  A->place = place;
+  A->wide = H % 8 == 0;
+  return CARDAN_OK;
+}
+
+bool on16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+}  // namespace
+
+extern "C" {
+
+int cardan_route_rows_workspace_bytes(const cardan_routing* routing, int32_t N, size_t* out) {
+  g_err[0] = 0;
+  int rc = check_routing(routing, N);
+  if (rc) return rc;
+  if (!out) return fail(CARDAN_ERR_NULL_PTR, "out is NULL");
+  // counts of every block of rows, and their totals
+  const int64_t blocks = std::min<int64_t>(kRouteBlocks, ((int64_t)N + 3) / 4);
+  *out = N <= kRouteSmall ? 0 : align256((size_t)(blocks + 1) * routing->E * 4);
+  return CARDAN_OK;
+}
+
+int cardan_route_rows(const cardan_routing* routing, int32_t N, int32_t logits_type, const void* logits, int64_t ld,
+                      const float* bias, int32_t* idx, float* weight, int32_t* place, int32_t* offsets, void* ws,
+                      size_t ws_bytes, hipStream_t stream) {
+  g_err[0] = 0;
+  RouteArgs A;
+  int rc = route_args(routing, N, logits_type, logits, ld, &A);
+  if (rc) return rc;
+  if (bias) START(bias, "bias", 4);
+  if (N > 0) {
+    START(idx, "idx", 4);
+    START(weight, "weight", 4);
+    if (offsets || place) START(place, "place", 4);
+  }
+  if (offsets || place) START(offsets, "offsets", 4);
+  size_t need = 0;
+  if ((rc = cardan_route_rows_workspace_bytes(routing, N, &need))) return rc;
+  if (offsets && need > 0 && (rc = check_ws(need, ws, ws_bytes))) return rc;
+  A.by_score = bias != nullptr || (A.groups > 1 && A.best == 2);
+  A.bias = bias;
+  A.idx = idx;
+  A.weight = weight;
+  A.place = place;
+  A.offsets = offsets;
+  A.count = static_cast<int32_t*>(ws);
+  const hipError_t e = launch_route(A, stream);
+  return e == hipSuccess ? CARDAN_OK : hip_fail(e, "routing launch");
+}
+
+int cardan_route_rows_backward(const cardan_routing* routing, int32_t N, int32_t logits_type, const void* logits,
+                               int64_t ld, const int32_t* idx, const float* dweight, void* dlogits, int64_t dld,
+                               hipStream_t stream) {
+  g_err[0] = 0;
+  RouteArgs A;
+  int rc = route_args(routing, N, logits_type, logits, ld, &A);
+  if (rc) return rc;
+  if (dld < A.E || dld > (int64_t)1 << 40)
+    return fail(CARDAN_ERR_BAD_SHAPE, "row stride %lld is below E=%d or too large", (long long)dld, A.E);
+  if (dlogits == logits && dld != ld) return fail(CARDAN_ERR_BAD_SHAPE, "dlogits in place of the logits needs dld == ld");
+  if (N == 0) return CARDAN_OK;
+  const uintptr_t size = logits_type == CARDAN_LOGITS_F64 ? 8 : logits_type == CARDAN_LOGITS_F32 ? 4 : 2;
+  START(idx, "idx", 4);
+  START(dweight, "dweight", 4);
+  START(dlogits, "dlogits", size);
+  A.wide = A.wide && on16(dlogits) && dld * size % 16 == 0;
+  A.idx = const_cast<int32_t*>(idx);
+  A.dweight = dweight;
+  A.dlogits = dlogits;
+  A.dld = dld;
+  const hipError_t e = launch_route_backward(A, stream);
+  return e == hipSuccess ? CARDAN_OK : hip_fail(e, "routing backward launch");
+}
+
+int cardan_dispatch_rows(int32_t N, int32_t k, int32_t H, int32_t M, const cardan_bf16* x, const int32_t* place,
+                         cardan_bf16* xe, hipStream_t stream) {
+  g_err[0] = 0;
+  RowsArgs A;
+  int rc = check_rows(N, k, H, M, place, &A);
+  if (rc) return rc;
+  if (N == 0 || M == 0) return CARDAN_OK;
+  START(x, "x", 2);
+  START(xe, "xe", 2);
+  A.wide = A.wide && on16(x) && on16(xe);
+  A.x = x;
+  A.xe = xe;
+  const hipError_t e = launch_dispatch(A, stream);
+  return e == hipSuccess ? CARDAN_OK : hip_fail(e, "dispatch launch");
+}
+
+int cardan_combine_rows(int32_t N, int32_t k, int32_t H, int32_t M, const cardan_bf16* ye, const int32_t* place,
+                        const float* weight, int32_t y_type, void* y, hipStream_t stream) {
+  g_err[0] = 0;
+  RowsArgs A;
+  int rc = check_rows(N, k, H, M, place, &A);
+  if (rc) return rc;
+  if (y_type != CARDAN_LOGITS_BF16 && y_type != CARDAN_LOGITS_F32)
+    return fail(CARDAN_ERR_UNSUPPORTED, "type %d of y is not known", y_type);
+  if (N == 0) return CARDAN_OK;
+  if (M > 0) START(ye, "ye", 2);
+  if (weight) START(weight, "weight", 4);
+  A.f32 = y_type == CARDAN_LOGITS_F32;
+  START(y, "y", A.f32 ? 4 : 2);
+  A.wide = A.wide && on16(ye) && on16(y);
+  A.ye = ye;
+  A.weight = weight;
+  A.y = y;
+  const hipError_t e = launch_combine(A, stream);
+  return e == hipSuccess ? CARDAN_OK : hip_fail(e, "combine launch");
+}
+
+int cardan_combine_rows_backward(int32_t N, int32_t k, int32_t H, int32_t M, int32_t dy_type, const void* dy,
+                                 const cardan_bf16* ye, const int32_t* place, const float* weight, cardan_bf16* dye,
+                                 float* dweight, hipStream_t stream) {
+  g_err[0] = 0;
+  RowsArgs A;
+  int rc = check_rows(N, k, H, M, place, &A);
+  if (rc) return rc;
+  if (dy_type != CARDAN_LOGITS_BF16 && dy_type != CARDAN_LOGITS_F32)
+    return fail(CARDAN_ERR_UNSUPPORTED, "type %d of dy is not known", dy_type);
+  if (N == 0) return CARDAN_OK;
+  if (!dye && !dweight) {  // (an array without rows has no address)
+    if (M == 0) return CARDAN_OK;
+    return fail(CARDAN_ERR_NULL_PTR, "no gradient is asked for");
+  }
+  A.f32 = dy_type == CARDAN_LOGITS_F32;
+  START(dy, "dy", A.f32 ? 4 : 2);
+  if (weight) START(weight, "weight", 4);
+  if (M > 0 && dweight) START(ye, "ye", 2);
+  if (dweight) START(dweight, "dweight", 4);
+  if (dye) START(dye, "dye", 2);
+  A.wide = A.wide && on16(dy) && on16(ye) && on16(dye);
+  A.dy = dy;
+  A.ye = ye;
+  A.weight = weight;
+  A.dye = dye;
+  A.dweight = dweight;
+  const hipError_t e = launch_combine_backward(A, stream);
+  return e == hipSuccess ? CARDAN_OK : hip_fail(e, "combine backward launch");
+}
+
+int cardan_adamw_step(const cardan_adamw* config, int32_t count, const cardan_adamw_tensor* tensors,
+                      hipStream_t stream) {
+  g_err[0] = 0;
+  if (!config) return fail(CARDAN_ERR_NULL_PTR, "config is NULL");
+  const cardan_adamw& c = *config;
+  if (count < 0) return fail(CARDAN_ERR_BAD_SHAPE, "count=%d is negative", count);
+  for (const int32_t type : {c.param_type, c.grad_type})
+    if (type != CARDAN_LOGITS_BF16 && type != CARDAN_LOGITS_F32)
+      return fail(CARDAN_ERR_UNSUPPORTED, "type %d of weights or gradients is not known", type);
+  if (c.state_bits != 8 && c.state_bits != 32) return fail(CARDAN_ERR_UNSUPPORTED, "state_bits is 8 or 32, not %d", c.state_bits);
+  if (!(c.beta1 >= 0.0 && c.beta1 < 1.0 && c.beta2 >= 0.0 && c.beta2 < 1.0))
+    return fail(CARDAN_ERR_BAD_SHAPE, "beta1 and beta2 must lie within [0, 1)");
+  if (!(c.eps >= 0.0) || !isfinite(c.eps) || !isfinite(c.lr) || !isfinite(c.weight_decay))
+    return fail(CARDAN_ERR_BAD_SHAPE, "eps must be finite and not negative, lr and weight_decay finite");
+  if (!c.step_device && c.step < 1) return fail(CARDAN_ERR_BAD_SHAPE, "step=%d must be positive", c.step);
+  if (c.step_device) START(c.step_device, "step_device", 4);
+  if (c.lr_device) START(c.lr_device, "lr_device", 4);
+  if (c.grad_scale) START(c.grad_scale, "grad_scale", 4);
+  if (count > 0 && !tensors) return fail(CARDAN_ERR_NULL_PTR, "tensors is NULL");
+  const bool pbf = c.param_type == CARDAN_LOGITS_BF16, gbf = c.grad_type == CARDAN_LOGITS_BF16, s8 = c.state_bits == 8;
+  const uintptr_t ss = s8 ? 1 : 4;
+  for (int32_t i = 0; i < count; ++i) {
+    const cardan_adamw_tensor& T = tensors[i];
+    if (T.n < 0 || T.n > (int64_t)1 << 36) return fail(CARDAN_ERR_BAD_SHAPE, "tensor %d has %lld values", i, (long long)T.n);
+    if (T.n == 0) continue;
+    START(T.param, "param", pbf ? 2 : 4);
+    START(T.grad, "grad", gbf ? 2 : 4);
+    START(T.m, "m", ss);
+    START(T.v, "v", ss);
+    if (s8) {
+      START(T.m_scale, "m_scale", 4);
+      START(T.v_scale, "v_scale", 4);
+    }
+    if (T.copy) {
+      if (pbf) return fail(CARDAN_ERR_UNSUPPORTED, "bf16 weights have no bf16 copy");
+      START(T.copy, "copy", 2);
+    }
+  }
+  AdamwArgs A;
+  memset(&A, 0, sizeof A);
+  A.step = c.step_device ? 1 : c.step;
+  A.beta1 = c.beta1;
+  A.beta2 = c.beta2;
+  A.lr = c.lr;
+  A.decay = c.weight_decay;
+  A.b1 = (float)c.beta1;
+  A.a1 = (float)(1.0 - c.beta1);
+  A.b2 = (float)c.beta2;
+  A.a2 = (float)(1.0 - c.beta2);
+  A.eps = (float)c.eps;
+  A.lr_decay = (float)(c.lr * c.weight_decay);
+  A.lr_c1 = (float)(c.lr / (1.0 - pow(c.beta1, (double)A.step)));
+  A.inv_c2 = (float)(1.0 / (1.0 - pow(c.beta2, (double)A.step)));
+  A.lr_device = c.lr_device;
+  A.step_device = c.step_device;
+  A.grad_scale = c.grad_scale;
+  for (int32_t i = 0; i < count;) {
+    for (A.count = 0; i < count && A.count < kAdamwTensors; ++i) {
+      const cardan_adamw_tensor& T = tensors[i];
+      if (T.n > 0) A.t[A.count++] = AdamwTensor{T.param, T.grad, T.m, T.v, T.m_scale, T.v_scale, T.copy, T.n};
+    }
+    const hipError_t e = A.count ? launch_adamw(A, pbf, gbf, s8, stream) : hipSuccess;
+    if (e != hipSuccess) return hip_fail(e, "AdamW launch");
+  }
+  return CARDAN_OK;
 }
 
 int cardan_profile_begin(int32_t max_calls) {

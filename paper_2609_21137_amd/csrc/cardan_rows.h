@@ -1,0 +1,92 @@
+// Arguments and launchers of the routing of many rows, of rows to their
+// experts and back (cardan_route.hip, cardan_rows.hip) and of the AdamW step
+// (cardan_adamw.hip), shared with the C ABI.
+#ifndef CARDAN_ROWS_H
+#define CARDAN_ROWS_H
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+
+namespace cardan {
+
+enum LogitType { LOGIT_BF16 = 0, LOGIT_F32 = 1, LOGIT_F64 = 2 };
+
+// The blocks of rows that count their experts' selections before the rows'
+// places are known: at most this many, so that their prefix sums stay short.
+constexpr int kRouteBlocks = 1024;
+// Rows of one call that a single workgroup routes and places by itself.
+constexpr int kRouteSmall = 64;
+
+// One call of the routing of N rows (the backward pass reads idx and dweight).
+struct RouteArgs {
+  int32_t N, E, k;
+  int32_t sigmoid, renorm;
+  int32_t groups, top_groups, best, each;  // each = E / groups experts a group
+  int32_t by_score;                        // selection by float64 scores (plus bias), else by logits
+  int32_t type;                            // LogitType
+  int32_t wide;                            // rows and strides allow 16-byte accesses
+  float scale;
+  int64_t ld, dld;                         // row strides in elements
+  const void* logits;
+  const float* bias;                       // [E] or nullptr
+  int32_t* idx;                            // [N][k], -1: no expert
+  float* weight;                           // [N][k]
+  int32_t* place;                          // [N][k] or nullptr, -1: none
+  int32_t* offsets;                        // [E + 1] with place
+  int32_t* count;                          // [blocks][E] (workspace), then totals [E]
+  int32_t block_rows, blocks;
+  const float* dweight;                    // [N][k]
+  void* dlogits;                           // [N][dld]
+};
+
+// Rows of N tokens and their k copies in an array of M rows grouped by expert.
+struct RowsArgs {
+  int32_t N, k, H, M;
+  int32_t f32;               // y or dy is float32 (else bf16)
+  int32_t wide;              // every row starts on 16 bytes and H % 8 == 0
+  const int32_t* place;      // [N][k]; outside [0, M): none
+  const float* weight;       // [N][k] or nullptr (1)
+  const uint16_t *x, *ye;    // [N][H], [M][H]
+  const void* dy;            // [N][H]
+  uint16_t *xe, *dye;        // [M][H]
+  void* y;                   // [N][H]
+  float* dweight;            // [N][k] or nullptr
+};
+
+constexpr int kAdamwBlock = 256;  // values that share a scale
+constexpr int kAdamwTensors = 40; // tensors of one launch (their table is a kernel argument)
+
+struct AdamwTensor {
+  void* p;
+  const void* g;
+  void *m, *v;
+  float *ms, *vs;
+  uint16_t* copy;
+  int64_t n;
+};
+
+struct AdamwArgs {
+  AdamwTensor t[kAdamwTensors];
+  int32_t first[kAdamwTensors + 1];  // first workgroup of every tensor
+  int32_t count;
+  int32_t step;
+  double beta1, beta2, lr, decay;    // for a step or a rate on the device
+  float b1, a1, b2, a2, eps;         // beta and 1 - beta
+  float lr_decay, lr_c1, inv_c2;     // lr decay, lr / (1 - beta1^t), 1 / (1 - beta2^t)
+  const float* lr_device;
+  const int32_t* step_device;
+  const float* grad_scale;
+};
+
+hipError_t launch_route(const RouteArgs&, hipStream_t);
+hipError_t launch_route_backward(const RouteArgs&, hipStream_t);
+hipError_t launch_dispatch(const RowsArgs&, hipStream_t);
+hipError_t launch_combine(const RowsArgs&, hipStream_t);
+hipError_t launch_combine_backward(const RowsArgs&, hipStream_t);
+hipError_t launch_adamw(const AdamwArgs&, bool param_bf16, bool grad_bf16, bool state8, hipStream_t);
+
+}  // namespace cardan
+
+#endif  // CARDAN_ROWS_H

@@ -1,0 +1,331 @@
+"""AdamW steps against float64.
+
+With h = 2^-24: a moment is two or three products and a sum, off by at most 3 h
+of the sum of their sizes; an update m / (sqrt(v / c2) + eps) lr / c1 has the
+relative errors of m (times its sizes over |m|), half of v's, and those of its
+constants, root, sum, quotient and products (10 h); the weight's two differences
+and its decay add 3 h of its size. bf16 weights are one of the two neighbours of
+the float32 result, stored 8-bit moments one of the two neighbours of theirs.
+"""
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+H = 2.0 ** -24
+BF, F32, F64 = torch.bfloat16, torch.float32, torch.float64
+E4, E5 = torch.float8_e4m3fn, torch.float8_e5m2
+
+
+@pytest.fixture(scope="module")
+def C():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2609_21137_amd import cardan
+    return cardan
+
+
+def _tensors(sizes, param, grad, seed=0, skip=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+
+    def make(n, std, dtype):
+        full = torch.zeros(n + skip, dtype=dtype, device="cuda")
+        full[skip:] = torch.randn((n,), generator=g, device="cuda", dtype=F64).mul_(std).to(dtype)
+        return full[skip:]
+
+    return [make(n, 0.05, param) for n in sizes], [make(n, 0.01, grad) for n in sizes]
+
+
+def _values(state, n):
+    """Moments of a state in float64."""
+    if len(state) == 2:
+        return state[0].double().reshape(-1), state[1].double().reshape(-1)
+    at = torch.arange(n, device="cuda") // 256
+    return (state[0].float().double().reshape(-1) * state[2].double()[at],
+            state[1].float().double().reshape(-1) * state[3].double()[at])
+
+
+def _step(p, g, m, v, t, lr=1e-2, betas=(0.9, 0.999), eps=1e-8, wd=0.1, gs=1.0):
+    """(p, m, v) in float64 and their bounds."""
+    p, g = p.double().reshape(-1), g.double().reshape(-1) * gs
+    b1, b2 = betas
+    m1, sm = b1 * m + (1 - b1) * g, b1 * m.abs() + (1 - b1) * g.abs()
+    v1 = b2 * v + (1 - b2) * g * g
+    c1, c2 = 1 - b1 ** t, 1 - b2 ** t
+    root = (v1 / c2).sqrt() + eps
+    up = lr / c1 * m1 / root
+    new = p - lr * wd * p - up
+    em, ev = 4 * H * sm, 5 * H * v1 + 2.0 ** -148
+    ep = lr / c1 / root * em + up.abs() * 13 * H + 4 * H * (p.abs() + up.abs()) + lr * wd * p.abs() * 3 * H
+    return new, m1, v1, ep, em + 2.0 ** -148, ev
+
+
+def _grid(dtype):
+    v = torch.arange(128, dtype=torch.uint8, device="cuda").view(dtype).float().double()
+    return v[torch.isfinite(v)]
+
+
+def _neighbours(got, x, err, dtype):
+    """Every stored value is one of the grid's two around x (within err)."""
+    grid = _grid(dtype)
+    lo = grid[(torch.bucketize((x.abs() - err).clamp(min=0), grid, right=True) - 1).clamp(max=grid.numel() - 1)]
+    hi = grid[torch.bucketize(x.abs() + err, grid).clamp(max=grid.numel() - 1)]
+    a = got.float().double().abs()
+    return ((a >= lo) & (a <= hi) & ((got.float() == 0) | (torch.sign(got.float()).double() == torch.sign(x)))).all()
+
+
+def _check(C, params, grads, states, t, copies=None, **kw):
+    old = [(p.clone(), *_values(s, p.numel())) for p, s in zip(params, states)]
+    args = dict(lr=1e-2, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.1)
+    args.update(kw)
+    C.adamw_step(params, grads, states, t, copies=copies, **args)
+    torch.cuda.synchronize()
+    for i, (p, g, s, (p0, m0, v0)) in enumerate(zip(params, grads, states, old)):
+        n = p.numel()
+        if n == 0:
+            continue
+        new, m, v, ep, em, ev = _step(p0, g, m0, v0, t, args["lr"], args["betas"], args["eps"], args["weight_decay"],
+                                      float(kw["grad_scale"]) if "grad_scale" in kw else 1.0)
+        got = p.double().reshape(-1)
+        if p.dtype is F32:
+            assert ((got - new).abs() <= ep).all()
+            if copies is not None and copies[i] is not None:
+                assert torch.equal(copies[i], p.bfloat16())
+        else:
+            step = torch.exp2(torch.floor(torch.log2(new.abs() + ep)) - 7)
+            assert ((got - new).abs() <= step + ep).all()
+        if len(s) == 2:
+            assert ((s[0].double().reshape(-1) - m).abs() <= em).all()
+            assert ((s[1].double().reshape(-1) - v).abs() <= ev).all()
+            continue
+        at = torch.arange(n, device="cuda") // 256
+        for q, scale, x, err, dtype in ((s[0], s[2], m, em, E4), (s[1], s[3], v, ev, E5)):
+            top = torch.zeros(scale.shape, dtype=F64, device="cuda").index_reduce_(0, at, x.abs(), "amax")
+            most = torch.zeros(scale.shape, dtype=F64, device="cuda").index_reduce_(0, at, err, "amax")
+            want = top / float(_grid(dtype)[-1])
+            assert ((scale.double() - want).abs() <= 2 * H * want + most).all()
+            unit = scale.double()[at].clamp(min=2.0 ** -140)
+            # (x / scale: the error of x, of the reciprocal and the product)
+            xs = x / unit
+            assert _neighbours(q.reshape(-1), xs, err / unit + 4 * H * xs.abs(), dtype)
+
+
+SIZES = [1, 2, 7, 8, 9, 255, 256, 257, 511, 4096, 4097, 5000, 0, 70001]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("param,grad", [(F32, F32), (F32, BF), (BF, BF), (BF, F32)])
+@pytest.mark.parametrize("skip", [0, 1])
+def test_steps(C, param, grad, bits, skip):
+    params, grads = _tensors(SIZES, param, grad, 1, skip)
+    states = [C.adamw_state(p, bits) for p in params]
+    copies = [torch.zeros(p.shape, dtype=BF, device="cuda") for p in params] if param is F32 else None
+    for t in (1, 2, 3):
+        _check(C, params, grads, states, t, copies)
+        grads = _tensors(SIZES, param, grad, 10 + t, skip)[1]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_arguments(C, bits):
+    for kw in (dict(weight_decay=0.0), dict(betas=(0.0, 0.0), eps=1e-3), dict(lr=0.0), dict(eps=0.0),
+               dict(grad_scale=torch.tensor([0.125], device="cuda")), dict(betas=(0.8, 0.99), lr=1.0)):
+        params, grads = _tensors([300, 4096], F32, F32, 2)
+        states = [C.adamw_state(p, bits) for p in params]
+        _check(C, params, grads, states, 1, **kw)
+        _check(C, params, grads, states, 1000, **kw)
+
+
+def test_is_torchs_step(C):
+    """Ten steps of float32 tensors as torch's AdamW takes them, in float64 there."""
+    params, _ = _tensors([1000, 33], F32, F32, 3)
+    ref = [p.double().clone().requires_grad_(True) for p in params]
+    opt = torch.optim.AdamW(ref, lr=1e-2, betas=(0.9, 0.99), eps=1e-6, weight_decay=0.05)
+    states = [C.adamw_state(p) for p in params]
+    for t in range(1, 11):
+        _, grads = _tensors([1000, 33], F32, F32, 50 + t)
+        for r, g in zip(ref, grads):
+            r.grad = g.double()
+        opt.step()
+        C.adamw_step(params, grads, states, t, 1e-2, (0.9, 0.99), 1e-6, 0.05)
+    # ten steps of at most 1e-2 each, every one off by 20 h of itself and 8 h of the weight
+    assert all(((p.double() - r).abs() <= 10 * (20 * H * 1e-1 + 8 * H * r.abs())).all() for p, r in zip(params, ref))
+
+
+def test_shapes_and_gradients_that_are_missing(C):
+    g = torch.Generator(device="cuda").manual_seed(4)
+    params = [torch.randn(s, generator=g, device="cuda") for s in ((3, 5, 7), (2, 300), ())]
+    grads = [torch.randn(s.shape, generator=g, device="cuda") for s in params]
+    states = [C.adamw_state(p, 8) for p in params]
+    grads[1] = None
+    kept = params[1].clone()
+    C.adamw_step(params, grads, states, 1, 1e-2)
+    assert torch.equal(params[1], kept) and not states[1][2].any()
+    assert states[0][0].shape == (3, 5, 7) and states[0][0].dtype is E4 and states[0][1].dtype is E5
+    C.adamw_step(params, [None] * 3, states, 2, 1e-2)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_many_tensors(C, bits):
+    """More tensors than a launch's table holds, each as if it were alone."""
+    sizes = [(i * 37) % 700 for i in range(95)]
+    params, grads = _tensors(sizes, F32, F32, 5)
+    states = [C.adamw_state(p, bits) for p in params]
+    alone = [(p.clone(), tuple(t.clone() for t in s)) for p, s in zip(params, states)]
+    C.adamw_step(params, grads, states, 3, 1e-2, weight_decay=0.1)
+    for (p, s), g, q, r in zip(alone, grads, params, states):
+        C.adamw_step([p], [g], [s], 3, 1e-2, weight_decay=0.1)
+        assert torch.equal(p, q) and all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(s, r))
+
+
+def test_the_same_arguments_give_the_same_result(C):
+    for param in (F32, BF):
+        a = _tensors([9000], param, F32, 6)
+        b = [[t.clone() for t in x] for x in a]
+        sa, sb = [C.adamw_state(a[0][0], 8)], [C.adamw_state(b[0][0], 8)]
+        for t in (1, 2):
+            C.adamw_step(*a, sa, t, 1e-2)
+            C.adamw_step(*b, sb, t, 1e-2)
+        assert torch.equal(a[0][0], b[0][0])
+        assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(sa[0], sb[0]))
+
+
+def test_small_moments_move_in_the_mean(C):
+    """Values a hundredth of their block's largest, whose v has to fall by a thousandth a
+    step: the mean over 255 x 400 values follows the float64 recursion. A stored v is off
+    by less than a step (a quarter of it) each time, independently: after t steps its
+    variance is below t (2^-2 v)^2 0.001 / 0.18, that is 0.06 v (one deviation) a value at
+    300 steps, and the mean's six deviations 6 * 0.06 * sqrt(300) / sqrt(102000)... bounded
+    here by one percent. Rounded to nearest it would not have moved (26 percent off)."""
+    n = 256 * 400
+    p = torch.zeros(n, device="cuda")
+    big = torch.arange(n, device="cuda") % 256 == 0
+    g = torch.where(big, 1.0, 0.01)
+    s = C.adamw_state(p, 8)
+    C.adamw_step([p], [g * 2], [s], 1, 0.0, betas=(0.9, 0.0))          # v starts four times too large
+    v = 4e-4
+    for t in range(2, 302):
+        C.adamw_step([p], [g], [s], t, 0.0)
+        v = 0.999 * v + 0.001 * 1e-4
+    got = _values(s, n)[1][~big].mean().item()
+    assert abs(got / v - 1) < 0.01, (got, v)
+    m = _values(s, n)[0][~big].mean().item()
+    assert abs(m / 0.01 - 1) < 0.01
+
+
+def test_bf16_weights_move_in_the_mean(C):
+    """Updates of 2^-6 of a step of the weight, 64 times: one step in the mean over 2^18 values.
+    A value's sum of 64 roundings has a deviation of 64^(1/2) / 8 steps, the mean's six are below
+    6 / 512: 1.2 percent."""
+    n = 1 << 18
+    p = torch.ones(n, dtype=BF, device="cuda")
+    g = torch.full((n,), -1.0, device="cuda")
+    s = C.adamw_state(p)
+    lr = 2.0 ** -7 / 64
+    for t in range(1, 65):
+        C.adamw_step([p], [g], [s], t, lr, eps=0.0)
+    assert abs((p.double().mean().item() - 1) / 2.0 ** -7 - 1) < 0.012
+
+
+def test_dither_bits_are_even(C):
+    """A constant between two grid points goes up as often as its fraction says, at every
+    place of the fraction and at several steps."""
+    n = 1 << 20
+    for t in (1, 2, 77, 123456):
+        for part in (0.03125, 0.3, 0.5, 0.9):
+            g = torch.full((n,), 1.0 + part * 0.125, device="cuda")
+            g[::256] = 448.0 / 256                       # the block's largest: a scale of 2^-8
+            p, s = torch.zeros(n, device="cuda"), C.adamw_state(torch.zeros(n, device="cuda"), 8)
+            C.adamw_step([p], [g], [s], t, 0.0, betas=(0.0, 0.0))
+            up = (s[0].float() > 256.5).double().reshape(-1, 256)[:, 1:].mean().item()
+            # six deviations of a count of 2^20, and the 16 bits
+            want = (1.0 + part * 0.125) * 256
+            lo = 2.0 ** 8
+            frac = (want - lo) / 32
+            assert abs(up - frac) < 6 * 0.5 / 1020 + 2.0 ** -16, (t, part, up, frac)
+
+
+def test_gradients_that_are_not_finite(C):
+    for bits in (32, 8):
+        for bad in (float("nan"), float("inf")):
+            params, grads = _tensors([1000], F32, F32, 8)
+            grads[0][300] = bad
+            s = [C.adamw_state(params[0], bits)]
+            C.adamw_step(params, grads, s, 1, 1e-2)
+            m, v = _values(s[0], 1000)
+            assert not torch.isfinite(params[0][300]) and not torch.isfinite(m[300]) and not torch.isfinite(v[300])
+            fine = torch.ones(1000, dtype=torch.bool, device="cuda")
+            fine[300] = False
+            assert torch.isfinite(params[0][fine]).all()
+            if bits == 8:
+                fine[256:512] = False
+            assert torch.isfinite(m[fine]).all() and torch.isfinite(v[fine]).all()
+
+
+def test_tiny_and_zero_gradients(C):
+    """Blocks of zeros, and of sizes whose squares and scales are subnormal: nothing but finite values."""
+    for size in (0.0, 1e-30, 1e-22, 1e-18, 1e18):
+        p, g = torch.ones(600, device="cuda"), torch.full((600,), size, device="cuda")
+        g[::3] = 0
+        s = C.adamw_state(p, 8)
+        for t in (1, 2, 3):
+            C.adamw_step([p], [g], [s], t, 1e-2)
+        assert all(torch.isfinite(x).all() for x in (p, *_values(s, 600)))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("param", [F32, BF])
+def test_captured_step_follows_step_and_rate_on_the_device(C, bits, param):
+    sizes = [700, 5000]
+    params, grads = _tensors(sizes, param, F32, 9)
+    other = [p.clone() for p in params]
+    states, theirs = ([C.adamw_state(p, bits) for p in params] for _ in range(2))
+    step = torch.zeros(1, dtype=torch.int32, device="cuda")
+    lr, gs = torch.zeros(1, device="cuda"), torch.ones(1, device="cuda")
+
+    def call():
+        step.add_(1)
+        C.adamw_step(params, grads, states, step, lr, weight_decay=0.1, grad_scale=gs)
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for t in range(1, 6):
+        for g, new in zip(grads, _tensors(sizes, param, F32, 30 + t)[1]):
+            g.copy_(new)
+        lr.fill_(0.01 / t)
+        gs.fill_(0.5 * t)
+        graph.replay()
+        torch.cuda.synchronize()
+        C.adamw_step(other, grads, theirs, t, float(lr), weight_decay=0.1, grad_scale=gs)
+        torch.cuda.synchronize()
+        for p, q in zip(params, other):
+            if param is F32:
+                # the constants in float64 on either side, rounded once: the same to a step of theirs
+                assert ((p - q).abs() <= 8 * 2 * H * (0.01 + q.abs())).all()
+            else:
+                assert ((p.float() - q.float()).abs() <= 2.0 ** -7 * q.float().abs() + 1e-3).all()
+    assert int(step) == 5
+
+
+def test_tensors_past_31_bits(C):
+    """The last values of a tensor of more than 2^31, as the first of ... their own places say."""
+    n = (1 << 31) + 5000
+    p = torch.zeros(n, dtype=BF, device="cuda")
+    g = torch.zeros(n, dtype=BF, device="cuda")
+    tail = slice(n - 4000, n)
+    g[tail] = torch.randn(4000, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).bfloat16()
+    p[tail] = 1.0
+    s = C.adamw_state(p, 8)
+    C.adamw_step([p], [g], [s], 1, 0.25, eps=1e-6)
+    torch.cuda.synchronize()
+    new, m, v, ep, em, ev = _step(torch.ones(4000, device="cuda"), g[tail], torch.zeros(4000, device="cuda", dtype=F64),
+                                  torch.zeros(4000, device="cuda", dtype=F64), 1, 0.25, eps=1e-6, wd=0.0)
+    got = p[tail].double()
+    step = torch.exp2(torch.floor(torch.log2(new.abs() + ep)) - 7)
+    assert ((got - new).abs() <= step + ep).all()
+    at = (torch.arange(n - 4000, n, device="cuda")) // 256
+    assert ((s[0][tail].float().double() * s[2].double()[at] - m).abs() <= 2.0 ** -3 * m.abs() + s[2].double()[at] * 2.0 ** -9).all()
+    assert not p[:n - 4000].any()
+    del p, g, s
+    torch.cuda.empty_cache()

@@ -1,0 +1,390 @@
+"""Routing of many rows and its gradient against the definition in float64.
+
+Selections have to be equal, places too. Bounds of the weights, with h = 2^-24
+(half a step of float32) and D the largest distance of a row's finite logits:
+a difference of logits is off by h times its size, which is the relative error
+of its exponential (D h), the exponential's own is below 4 h, a sum of up to
+1024 terms goes through at most 15 + 6 additions and a quotient and two products
+add 3 h: (2 D + 32) h of the weight. The gradient w (d - sum w d) has the
+relative error of w twice, of its own sums and products: (4 D + 96) h of w (|d| +
+sum |w d|), and half a step of its own type. float64 logits: float32 weights are
+rounded once (2 h), the gradient holds 1e-12.
+"""
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+H = 2.0 ** -24
+BF, F32, F64 = torch.bfloat16, torch.float32, torch.float64
+
+
+@pytest.fixture(scope="module")
+def C():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2609_21137_amd import cardan
+    return cardan
+
+
+def _opts(top_k, score="softmax", renorm=True, scale=1.0, groups=1, top_groups=1, group_best=1):
+    return dict(top_k=top_k, score=score, renorm=renorm, scale=scale, groups=groups, top_groups=top_groups,
+                group_best=group_best)
+
+
+def _oracle(logits, bias, o):
+    """Row by row in float64 numpy: (idx, weight, scores)."""
+    z = logits.double().cpu().numpy()
+    b = None if bias is None else bias.double().cpu().numpy()
+    N, E = z.shape
+    k, G = o["top_k"], o["groups"]
+    idx, w = np.full((N, k), -1), np.zeros((N, k))
+    scores = np.zeros((N, E))
+    by_score = b is not None or (G > 1 and o["group_best"] == 2)
+    for n in range(N):
+        live = z[n] != -np.inf
+        with np.errstate(over="ignore", under="ignore", invalid="ignore"):
+            if o["score"] == "sigmoid":
+                s = np.where(live, 1.0 / (1.0 + np.exp(-z[n])), 0.0)
+            else:
+                top = np.fmax.reduce(z[n]) if live.any() else 0.0
+                e = np.exp(z[n] - top)
+                s = e / e.sum() if live.any() else e
+        scores[n] = s
+        v = (s if by_score else z[n]).copy()
+        if b is not None:
+            v = v + b
+        v[~live] = -np.inf
+        bad = np.isnan(v).any()
+        v[np.isnan(v)] = -np.inf
+        if G > 1:
+            of = v.reshape(G, E // G)
+            tops = -np.sort(-of, 1)[:, :o["group_best"]]
+            count = np.where(tops[:, 0] == -np.inf, -np.inf, np.where(tops == -np.inf, 0.0, tops).sum(1))
+            kept = np.argsort(-count, kind="stable")[:o["top_groups"]]
+            out = np.ones(G, bool)
+            out[kept] = False
+            of[out] = -np.inf
+        order = np.argsort(-v, kind="stable")[:k]
+        idx[n] = np.where(v[order] == -np.inf, -1, order)
+        has = idx[n] >= 0
+        if o["renorm"] and has.any():
+            zk = z[n][idx[n][has]]
+            with np.errstate(over="ignore", under="ignore", invalid="ignore"):
+                if o["score"] == "softmax":
+                    r = np.exp(zk - zk.max())
+                else:
+                    m = min(zk.max(), 0.0)
+                    r = np.where(zk > 0, 1.0 / (1.0 + np.exp(-zk)), np.exp(zk - m) / (1.0 + np.exp(zk)))
+                w[n][has] = r / r.sum()
+        else:
+            w[n][has] = s[idx[n][has]]
+        w[n] *= o["scale"]
+        if bad:
+            w[n] = np.nan
+    return idx, w, scores
+
+
+def _spread(logits):
+    z = logits.double().cpu().numpy()
+    z = np.where(np.isfinite(z), z, np.nan)
+    some = ~np.isnan(z).all(1)
+    d = np.zeros(z.shape[0])
+    d[some] = np.nanmax(np.abs(z[some]), 1) + np.nanmax(z[some], 1) - np.nanmin(z[some], 1)
+    return d[:, None]
+
+
+def _check(C, logits, bias, o, **kw):
+    idx, w, place, offsets = C.route_rows(logits, bias=bias, **o, **kw)
+    torch.cuda.synchronize()
+    ri, rw, _ = _oracle(logits, bias, o)
+    i = idx.cpu().numpy()
+    assert np.array_equal(i, ri), np.nonzero((i != ri).any(1))[0][:5]
+    got = w.double().cpu().numpy()
+    tol = (2 * H + 1e-13) if logits.dtype is F64 else (2 * _spread(logits) + 32) * H
+    with np.errstate(invalid="ignore"):
+        ok = (np.abs(got - rw) <= tol * np.abs(rw) + 2.0 ** -149) | (np.isnan(got) & np.isnan(rw))
+    assert ok.all(), (got[~ok][:4], rw[~ok][:4])
+    _check_places(idx, place, offsets, logits.shape[1])
+    return idx, w, place, offsets
+
+
+def _check_places(idx, place, offsets, E):
+    i, p, off = idx.cpu().numpy().reshape(-1), place.cpu().numpy().reshape(-1), offsets.cpu().numpy()
+    assert np.array_equal(off, np.concatenate([[0], np.bincount(i[i >= 0], minlength=E).cumsum()]))
+    order = np.argsort(np.where(i < 0, E, i), kind="stable")
+    want = np.empty_like(p)
+    want[order] = np.arange(p.size)
+    want[i < 0] = -1
+    assert np.array_equal(p, want)
+
+
+def _logits(N, E, dtype, seed=0, std=1.5):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return (torch.randn((N, E), generator=g, device="cuda", dtype=F64) * std).to(dtype)
+
+
+def _bias(E, seed=1):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randn((E,), generator=g, device="cuda") * 0.1
+
+
+FORMS = [
+    (8, _opts(2)), (64, _opts(6, renorm=False)), (128, _opts(8)), (1, _opts(1)), (5, _opts(5, "sigmoid")),
+    (256, _opts(8, "sigmoid", True, 2.5, 8, 4, 2)), (160, _opts(6, "softmax", False, 16.0, 8, 3, 1)),
+    (38 * 4, _opts(9, "softmax", True, 1.0, 4, 2, 2)), (300, _opts(32, "sigmoid", False)), (1000, _opts(7, "softmax", False)),
+    (1024, _opts(32, "sigmoid", True, 1.0, 64, 5, 2)), (17, _opts(16)), (512, _opts(3, "softmax", True, 1.0, 2, 1, 1)),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32, F64])
+@pytest.mark.parametrize("biased", [False, True])
+@pytest.mark.parametrize("E,o", FORMS)
+def test_forms(C, E, o, biased, dtype):
+    for N in (1, 3, 64, 65, 300):
+        _check(C, _logits(N, E, dtype, N), _bias(E) if biased else None, o)
+
+
+@pytest.mark.parametrize("N", [1, 16, 63, 1024, 1025, 16385, 70001])
+def test_rows(C, N):
+    """Rows of one workgroup, of a block, and of blocks of more rows than one pass."""
+    E, o = 96, _opts(4)
+    logits = _logits(N, E, F32, N)
+    idx, w, place, offsets = C.route_rows(logits, **o)
+    val, want = torch.sort(logits.double(), dim=1, descending=True, stable=True)
+    assert torch.equal(idx.long(), want[:, :4])
+    ref = torch.softmax(val[:, :4], 1)
+    assert ((w.double() - ref).abs() <= (2 * 16 + 32) * H * ref).all()
+    _check_places(idx, place, offsets, E)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("groups,top,best", [(1, 1, 1), (4, 2, 1), (4, 2, 2)])
+def test_ties_go_to_the_lower_index(C, score, groups, top, best):
+    o = _opts(6, score, True, 1.0, groups, top, best)
+    z = torch.zeros((70, 32), device="cuda")
+    z[1, 7] = z[1, 30] = 1.0
+    z[2] = -z[2].abs()                     # -0 among zeros: equal to them
+    z[2, ::2] = 0.0
+    z[3:] = torch.randint(-2, 3, (67, 32), generator=torch.Generator().manual_seed(1)).float().cuda()
+    for dtype in (BF, F32, F64):
+        _check(C, z.to(dtype), None, o)
+        _check(C, z.to(dtype), torch.zeros(32, device="cuda"), o)
+
+
+@pytest.mark.parametrize("N", [40, 200])
+@pytest.mark.parametrize("o", [_opts(4), _opts(4, "softmax", False), _opts(4, "sigmoid"), _opts(4, "sigmoid", False),
+                               _opts(4, "sigmoid", True, 1.0, 4, 2, 2), _opts(4, "softmax", False, 2.0, 4, 2, 1)])
+@pytest.mark.parametrize("biased", [False, True])
+def test_masked_experts_and_rows(C, o, N, biased):
+    """-inf: not there; a row of nothing else has no experts. The lowest finite value is a logit like others."""
+    z = _logits(N, 16, F32, 3)
+    inf = float("inf")
+    z[0] = -inf
+    z[1, 3:] = -inf
+    z[2, :] = torch.finfo(F32).min
+    z[3, 1:] = torch.finfo(F32).min
+    z[4, :15] = -inf
+    z[5, 4:8] = -inf
+    z[N // 2] = -inf
+    z[N - 1] = -inf
+    bias = _bias(16) if biased else None
+    if biased:
+        bias[9] = -inf
+    idx, w, place, offsets = _check(C, z, bias, o)
+    assert (idx[0] == -1).all() and (w[0] == 0).all() and (place[N - 1] == -1).all()
+    assert int(offsets[-1]) == int((idx >= 0).sum())
+    d = torch.full((N, 4), float("nan"), device="cuda")
+    d[idx >= 0] = 1.0
+    g = C.route_rows_backward(z, idx, d, **o)
+    assert torch.isfinite(g).all() and (g[0] == 0).all()
+
+
+@pytest.mark.parametrize("o", [_opts(4), _opts(4, "softmax", False), _opts(4, "sigmoid"), _opts(4, "sigmoid", False, 1.0, 4, 2, 2)])
+def test_values_that_are_not_finite(C, o):
+    """A NaN is not selected and shows in all of its row's weights, and in no other row."""
+    z = _logits(70, 16, F32, 4)
+    z[1, 5] = float("nan")
+    z[2] = float("nan")
+    z[3, 2] = float("inf")
+    idx, w, place, offsets = C.route_rows(z, **o)
+    assert torch.isnan(w[1]).all() and torch.isnan(w[2]).all()
+    assert not (idx[1] == 5).any() and (idx[2] == -1).all()
+    assert ((idx >= -1) & (idx < 16)).all()
+    if o["score"] == "softmax":
+        assert torch.isnan(w[3]).any() or torch.isnan(w[3]).all()
+    else:
+        assert torch.isfinite(w[3]).all() and (idx[3] == 2).any()
+    rest = torch.cat([z[:1], z[4:]])
+    again = C.route_rows(rest, **o)
+    keep = torch.cat([torch.arange(1), torch.arange(4, 70)]).cuda()
+    assert torch.equal(again[0], idx[keep]) and torch.equal(again[1], w[keep])
+    _check_places(idx, place, offsets, 16)
+
+
+def test_far_logits(C):
+    """Sigmoid scores far below 1/2 keep their shares, large logits of either sign are no overflow."""
+    for o in (_opts(4, "sigmoid"), _opts(4, "softmax"), _opts(4, "softmax", False), _opts(4, "sigmoid", False)):
+        for shift in (-300.0, -80.0, 0.0, 80.0, 300.0):
+            _check(C, _logits(66, 24, F32, 5) + shift, None, o)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32, F64])
+@pytest.mark.parametrize("E,pad,skip", [(64, 0, 0), (64, 8, 0), (64, 3, 1), (50, 1, 1), (256, 16, 2)])
+def test_rows_that_are_padded_or_start_anywhere(C, dtype, E, pad, skip):
+    N = 130
+    full = torch.full((N * (E + pad) + skip,), float("nan"), dtype=dtype, device="cuda")
+    z = full[skip:].view(N, E + pad)[:, :E]
+    z.copy_(_logits(N, E, dtype, 6))
+    for o in (_opts(5, "softmax", False), _opts(5, "sigmoid")):
+        idx, w, _, _ = _check(C, z, None, o)
+        d = torch.randn(w.shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+        assert torch.equal(C.route_rows_backward(z, idx, d, **o), C.route_rows_backward(z.contiguous(), idx, d, **o))
+
+
+def test_no_rows(C):
+    idx, w, place, offsets = C.route_rows(torch.empty((0, 8), device="cuda"), 2)
+    assert idx.shape == w.shape == place.shape == (0, 2) and (offsets == 0).all() and offsets.shape == (9,)
+    assert C.route_rows_backward(torch.empty((0, 8), device="cuda"), idx, w).shape == (0, 8)
+
+
+def test_without_places(C):
+    z = _logits(500, 64, F32, 7)
+    a, b = C.route_rows(z, 4), C.route_rows(z, 4, places=False)
+    assert b[2] is None and b[3] is None and torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_is_the_decode_layers_routing(C):
+    """The routing of a layer of up to 64 tokens (logits of exact bf16 products in float64)."""
+    Hd, E, k, B = 256, 128, 8, 64
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.randn((B, Hd), generator=g, device="cuda").bfloat16()
+    W = (torch.randn((Hd, E), generator=g, device="cuda") * Hd ** -0.5).bfloat16()
+    shape = C.make_shape(Hd, 128, E, k, 4, 16, 8)
+    idx, w = C.route_topk(shape, x, W)
+    mine = C.route_rows(x.double() @ W.double(), k)
+    assert torch.equal(mine[0], idx) and ((mine[1] - w).abs() <= 1e-6).all()
+
+
+def _gradient(logits, idx, d, o):
+    """By differentiation of the weights in float64, and the bound's scale."""
+    z = logits.double().clone().requires_grad_(True)
+    has, at = idx >= 0, idx.clamp(min=0).long()
+    live = torch.where(z == -float("inf"), torch.full_like(z, -1e300), z)
+    s = torch.sigmoid(live) if o["score"] == "sigmoid" else torch.softmax(live, 1)
+    w = s.gather(1, at) * has
+    if o["renorm"] and o["score"] == "softmax":
+        # over the chosen logits alone: the others' gradients are zeros, not float64 residues
+        w = torch.softmax(torch.where(has, live.gather(1, at), -1e300), 1) * has
+    elif o["renorm"]:
+        w = w / w.sum(1, keepdim=True).clamp(min=1e-300)
+    dd = torch.where(has, d.double(), 0.0)
+    (w * o["scale"] * dd).sum().backward()
+    sd = o["scale"] * dd.abs()
+    total = (w.detach() * sd).sum(1, keepdim=True)
+    size = torch.zeros_like(z).detach()
+    size.scatter_add_(1, at, (w.detach() * (sd + total)) * has)
+    if o["score"] == "softmax" and not o["renorm"]:
+        size += s.detach() * total
+    return z.grad, size
+
+
+@pytest.mark.parametrize("dtype", [BF, F32, F64])
+@pytest.mark.parametrize("E,o", FORMS)
+def test_gradients(C, E, o, dtype):
+    for N in (1, 70, 515):
+        z = _logits(N, E, dtype, N)
+        bias = _bias(E)
+        idx, w, _, _ = C.route_rows(z, bias=bias, **o)
+        d = torch.randn(w.shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(N))
+        got = C.route_rows_backward(z, idx, d, **o)
+        assert got.dtype is dtype
+        ref, size = _gradient(z, idx, d, o)
+        D = torch.from_numpy(_spread(z)).cuda()
+        tol = 1e-12 * size if dtype is F64 else (4 * D + 96) * H * size
+        if dtype is BF:
+            tol = tol + 2.0 ** -8 * ref.abs()
+        assert ((got.double() - ref).abs() <= tol + 2.0 ** -133).all()
+
+
+@pytest.mark.parametrize("o", [_opts(3), _opts(3, "softmax", False, 2.0), _opts(3, "sigmoid", True, 2.5), _opts(3, "sigmoid", False)])
+def test_gradients_against_differences(C, o):
+    """Float64 logits, central differences of float32 weights: a step of 2^-8 leaves
+    (2^-16 / 6) of a third derivative (below 8) and 2^-24 * 2 / 2^-7 of a rounding."""
+    z = _logits(40, 12, F64, 9)
+    idx, w, _, _ = C.route_rows(z, **o)
+    d = torch.randn(w.shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(3))
+    got = C.route_rows_backward(z, idx, d, **o)
+    h = 2.0 ** -8
+
+    def loss(v):
+        """At the experts that were chosen, in the same order."""
+        i, ww, _, _ = C.route_rows(v, **o)
+        out = torch.zeros((40, 12), dtype=F64, device="cuda").scatter_(1, i.long(), ww.double())
+        return i, (out.gather(1, idx.long()) * d.double()).sum(1)
+
+    for e in range(12):
+        step = torch.zeros_like(z)
+        step[:, e] = h
+        (iu, up), (il, lo) = loss(z + step), loss(z - step)
+        same = (iu.sort(1).values == idx.sort(1).values).all(1) & (il.sort(1).values == idx.sort(1).values).all(1)
+        err = ((up - lo) / (2 * h) - got[:, e]).abs()
+        bound = (h * h / 6 * 8 + 2 * H / h) * o["scale"] * d.abs().sum(1).double()
+        assert same.sum() > 20 and (err[same] <= bound[same]).all()
+
+
+def test_gradient_in_place_of_the_logits(C):
+    for o in (_opts(4, "softmax", False), _opts(4)):
+        z = _logits(300, 64, BF, 2)
+        idx, w, _, _ = C.route_rows(z, **o)
+        want = C.route_rows_backward(z, idx, w, **o)
+        assert C.route_rows_backward(z, idx, w, out=z, **o).data_ptr() == z.data_ptr() and torch.equal(z, want)
+
+
+def test_experts_outside_the_range_have_no_gradient(C):
+    z = _logits(20, 8, F32, 2)
+    idx = torch.tensor([[0, 8], [-1, 3], [1 << 30, -(1 << 31)]] + [[1, 2]] * 17, dtype=torch.int32, device="cuda")
+    d = torch.ones((20, 2), device="cuda")
+    g = C.route_rows_backward(z, idx, d, score="sigmoid", renorm=False)
+    assert (g[2] == 0).all() and (g[0, 1:] == 0).all() and g[0, 0] != 0 and g[1, 3] != 0
+
+
+@pytest.mark.parametrize("N", [33, 3000])
+def test_captured_and_replayed(C, N):
+    """Replays follow their inputs; two graphs with workspaces of their own."""
+    o, E = _opts(6, "sigmoid", True, 1.0, 4, 2, 2), 64
+    z, bias = _logits(N, E, F32, 1), _bias(E)
+    runs = []
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        C.route_rows(z, bias=bias, **o)
+    torch.cuda.current_stream().wait_stream(side)
+    for _ in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = C.route_rows(z, bias=bias, **o)
+            g = C.route_rows_backward(z, out[0], out[1], **o)
+        runs.append((graph, out, g))
+    for step in range(4):
+        z.copy_(_logits(N, E, F32, 10 + step))
+        want = C.route_rows(z, bias=bias, **o)
+        dw = C.route_rows_backward(z, want[0], want[1], **o)
+        for graph, out, g in runs:
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(out, want)) and torch.equal(g, dw)
+
+
+def test_other_streams_and_shared_workspaces_in_turn(C):
+    z = [_logits(2000, 128, F32, s) for s in range(3)]
+    ws = torch.empty(C.route_rows_workspace_bytes(2000, 128, 8), dtype=torch.uint8, device="cuda").fill_(0xff)
+    want = [C.route_rows(v, 8) for v in z]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        got = [C.route_rows(v, 8, ws=ws) for v in z]
+    torch.cuda.current_stream().wait_stream(s)
+    assert all(torch.equal(a, b) for x, y in zip(got, want) for a, b in zip(x, y))
