@@ -120,7 +120,7 @@ def _load():
         "cardan_dispatch_rows": ([i32, i32, i32, i32, vp, vp, vp, vp], ctypes.c_int),
         "cardan_combine_rows": ([i32, i32, i32, i32, vp, vp, vp, i32, vp, vp], ctypes.c_int),
         "cardan_combine_rows_backward": ([i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp], ctypes.c_int),
-        "cardan_adamw_step": ([ctypes.POINTER(Adamw), i32, ctypes.POINTER(AdamwTensor), vp], ctypes.c_int),
+        "cardan_adamw_step": ([ctypes.POINTER(Adamw), i32, vp, vp], ctypes.c_int),
         "cardan_profile_begin": ([i32], ctypes.c_int),
         "cardan_profile_end": ([ctypes.POINTER(ctypes.c_float), ctypes.POINTER(i32)], ctypes.c_int),
     }
@@ -745,8 +745,7 @@ def route_rows(logits, top_k: int, bias=None, score: str = "softmax", renorm: bo
         idx, weight, place, offsets = out
     else:
         idx, weight = torch.empty((N, top_k), dtype=i32, device=dev), torch.empty((N, top_k), dtype=f32, device=dev)
-        place, offsets = (torch.empty((N, top_k), dtype=i32, device=dev),
-                          torch.empty((E + 1,), dtype=i32, device=dev)) if places else (None, None)
+        place, offsets = (torch.empty_like(idx), torch.empty((E + 1,), dtype=i32, device=dev)) if places else (None, None)
     need = _route_bytes(E, top_k, N) if offsets is not None else 0
     if ws is None:
         ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
@@ -907,19 +906,31 @@ def adamw_step(params, grads, states, step, lr, betas=(0.9, 0.999), eps: float =
         raise ValueError("a state is (m, v) or (m, v, m_scale, v_scale)")
     f32 = torch.float32
     mt, vt = (f32, f32) if kinds == 2 else (torch.float8_e4m3fn, torch.float8_e5m2)
-    table = (AdamwTensor * len(todo))()
-    for e, (p, g, s, c) in zip(table, todo):
+    index, kept, rows = dev.index, torch.bfloat16, []  # of AdamwTensor
+    for p, g, s, c in todo:
         if len(s) != kinds:
             raise ValueError("states must be of one kind")
-        shape = getattr(p, "shape", None)
-        e.param, e.grad = _arg(p, pt, "params", shape, dev), _arg(g, gt, "grads", shape, dev)
-        e.m, e.v = _arg(s[0], mt, "m", shape, dev), _arg(s[1], vt, "v", shape, dev)
-        e.n = n = p.numel()
+        m, v = s[0], s[1]
+        # (a pass over what _arg looks at, which gives the message where one does not fit)
+        try:
+            shape, n = p.shape, p.numel()
+            fits = (p.dtype is pt and g.dtype is gt and m.dtype is mt and v.dtype is vt and p.get_device() == index == g.get_device()
+                    and m.get_device() == index == v.get_device() and g.shape == shape and m.shape == shape and v.shape == shape
+                    and p.is_contiguous() and g.is_contiguous() and m.is_contiguous() and v.is_contiguous())
+        except AttributeError:
+            shape, fits = getattr(p, "shape", None), False
+        if fits and index is not None:
+            rows += (p.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr())
+        else:
+            rows += (_arg(p, pt, "params", shape, dev), _arg(g, gt, "grads", shape, dev), _arg(m, mt, "m", shape, dev),
+                     _arg(v, vt, "v", shape, dev))
         if kinds == 4:
             blocks = (-(-n // ADAMW_BLOCK),)
-            e.m_scale, e.v_scale = _arg(s[2], f32, "m_scale", blocks, dev), _arg(s[3], f32, "v_scale", blocks, dev)
-        if c is not None:
-            e.copy = _arg(c, torch.bfloat16, "copies", shape, dev)
+            rows += (_arg(s[2], f32, "m_scale", blocks, dev), _arg(s[3], f32, "v_scale", blocks, dev))
+        else:
+            rows += (0, 0)
+        rows += (0 if c is None else _arg(c, kept, "copies", shape, dev), n)
+    table = (ctypes.c_int64 * len(rows))(*rows)
     conf = Adamw(_TYPES[pt], _TYPES[gt], 32 if kinds == 2 else 8, 0, 0.0, betas[0], betas[1], eps, weight_decay)
     if isinstance(step, torch.Tensor):
         conf.step_device = _scalar(step, torch.int32, "step", dev)

@@ -22,6 +22,8 @@ namespace cardan {
 namespace {
 
 constexpr int kMostK = 32;
+constexpr int kSumBlocks = 64;  // blocks whose counts are summed without a launch of their own
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ float widen(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
 __device__ __forceinline__ float widen(float v) { return v; }
@@ -36,7 +38,11 @@ template <> struct Wide<double> { typedef double type; };
 
 template <int CTRL>
 __device__ __forceinline__ int lane_move(int v) {
-  return __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false);
+  return __builtin_amdgcn_mov_dpp(v, CTRL, 0xf, 0xf, true);
+}
+template <int CTRL>
+__device__ __forceinline__ uint32_t lane_move(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xf, 0xf, true);
 }
 template <int CTRL>
 __device__ __forceinline__ float lane_move(float v) {
@@ -54,7 +60,7 @@ __device__ __forceinline__ V over_row(V v, F f) {
   v = f(v, lane_move<0xB1>(v));   // lane ^ 1
   v = f(v, lane_move<0x4E>(v));   // lane ^ 2
   v = f(v, lane_move<0x141>(v));  // the other half of 8
-  v = f(v, lane_move<0x140>(v));  // the other half of 16
+  if constexpr (LPR >= 16) v = f(v, lane_move<0x140>(v));  // the other half of 16
   if constexpr (LPR == 64) {
     v = f(v, __shfl_xor(v, 16));
     v = f(v, __shfl_xor(v, 32));
@@ -125,7 +131,6 @@ template <class T> __device__ __forceinline__ T exp_of(T v);
 template <> __device__ __forceinline__ float exp_of(float v) { return expf(v); }
 template <> __device__ __forceinline__ double exp_of(double v) { return exp(v); }
 
-// The largest of a lane's values and its removal.
 template <int EPL, class V>
 __device__ __forceinline__ V local_max(const V (&v)[EPL]) {
   V m = v[0];
@@ -134,168 +139,438 @@ __device__ __forceinline__ V local_max(const V (&v)[EPL]) {
   return m;
 }
 
-// Selects the experts of one row into sel[k] (LDS of this row), -1 where none
-// is left; v is used up.
-template <int LPR, int EPL, class V>
-__device__ __forceinline__ void select_top(V (&v)[EPL], int k, int lane, int* sel) {
-  const int at = lane & (LPR - 1);
-  V b = local_max(v);
-  for (int j = 0; j < k; ++j) {
-    const V m = row_max<LPR>(b);
-    const uint64_t have = row_ballot<LPR>(b == m, lane);
-    if (at == __ffsll((unsigned long long)have) - 1) {
-      int hit = 0;
-      bool found = false;
+// Exponentials of a row's sum and of float32 scores: exp2 of one product is off
+// by |v| 2^-24 of the result, as the difference v to the row's top is itself.
+__device__ __forceinline__ float quick_exp(float v) { return __builtin_amdgcn_exp2f(v * 1.44269504088896340736f); }
+__device__ __forceinline__ double quick_exp(double v) { return exp(v); }
+
+// Descending order of N = 4, 8 or 16 keys (odd-even merge).
+template <int N>
+__device__ __forceinline__ void sort_keys(uint32_t (&v)[N]) {
 #pragma unroll
-      for (int i = 0; i < EPL; ++i) {
-        const bool here = !found && v[i] == b;
-        hit = here ? i : hit;
-        v[i] = here ? (V)-INFINITY : v[i];
-        found |= here;
-      }
-      sel[j] = m == (V)-INFINITY ? -1 : at * EPL + hit;
-      b = local_max(v);
+  for (int p = 1; p < N; p *= 2)
+#pragma unroll
+    for (int k = p; k >= 1; k /= 2)
+#pragma unroll
+      for (int j = k % p; j <= N - 1 - k; j += 2 * k)
+#pragma unroll
+        for (int i = 0; i <= (k - 1 < N - j - k - 1 ? k - 1 : N - j - k - 1); ++i)
+          if ((i + j) / (2 * p) == (i + j + k) / (2 * p)) {
+            const uint32_t a = v[i + j], b = v[i + j + k];
+            v[i + j] = a > b ? a : b;
+            v[i + j + k] = a > b ? b : a;
+          }
+}
+
+// Order of float32 values as unsigned numbers; -infinity is below kNone, also
+// with other low bits.
+constexpr uint32_t kNone = 0x00800000u;
+__device__ __forceinline__ uint32_t ordered(float v) {
+  const uint32_t u = __float_as_uint(v + 0.0f);  // (-0 is 0)
+  return u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float from_ordered(uint32_t u) {
+  return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
+}
+
+// A row's part of LDS: the candidates' experts and keys, with groups their
+// values and whether they are kept, and an area for one thing after another:
+// staged values of the groups, the lanes' sorted keys, the values of the
+// candidates or of all experts, the weights.
+constexpr int kSpare = 2;  // candidates behind the selection
+constexpr int kGroupBytes = 64 * (8 + 4);
+struct RowLds {
+  int* e;
+  uint32_t* key;
+  unsigned char *group, *area;
+  __device__ __forceinline__ RowLds(unsigned char* lds, const RouteArgs& A) {
+    e = reinterpret_cast<int*>(lds);
+    key = reinterpret_cast<uint32_t*>(e + A.slots);
+    group = lds + A.slots * 8;
+    area = group + (A.groups > 1 ? kGroupBytes : 0);
+  }
+};
+// A lane's sorted keys, apart from the next lane's by an odd number of 16 bytes.
+template <int EPL>
+constexpr int kListStep = EPL % 8 ? EPL : EPL + 4;
+template <class V, int LPR, int EPL>
+int row_bytes(const RouteArgs& A) {
+  const int list = LPR * kListStep<EPL> * 4, values = LPR * EPL * (int)sizeof(V), more = A.slots * 8;
+  return A.slots * 8 + (A.groups > 1 ? kGroupBytes : 0) + std::max(std::max(list, values), more);
+}
+
+// value[g], g < groups (LDS): which are kept, and the least of these and the
+// largest of the others over this lane's groups.
+template <int LPR, class V>
+__device__ __forceinline__ void rank_groups(const RouteArgs& A, int at, const V* value, int* keep, V& least, V& most) {
+  for (int grp = at; grp < A.groups; grp += LPR) {
+    const V x = value[grp];
+    int before = 0;
+    for (int h = 0; h < A.groups; ++h) {
+      const V o = value[h];
+      before += o > x || (o == x && h < grp);
     }
+    const bool in = before < A.top_groups && x != (V)-INFINITY;
+    keep[grp] = in;
+    if (in) least = x < least ? x : least;
+    else most = x > most ? x : most;
+  }
+}
+// Values of this lane's groups from all[E] (LDS).
+template <int LPR, class V>
+__device__ __forceinline__ void value_groups(const RouteArgs& A, int at, const V* all, V* value) {
+  for (int grp = at; grp < A.groups; grp += LPR) {
+    V b1 = (V)-INFINITY, b2 = (V)-INFINITY;
+#pragma unroll 4
+    for (int i = 0; i < A.each; ++i) {
+      const V x = all[grp * A.each + i], lo = x < b1 ? x : b1;
+      b1 = x > b1 ? x : b1;
+      b2 = lo > b2 ? lo : b2;
+    }
+    value[grp] = A.best == 2 && b2 != (V)-INFINITY ? b1 + b2 : b1;
   }
 }
 
-// Experts outside the kept groups leave the selection. `all` [E] and `of`
-// [groups] are LDS of this row.
-template <int LPR, int EPL, class V>
-__device__ __forceinline__ void keep_groups(V (&v)[EPL], const RouteArgs& A, int lane, V* all) {
-  const int at = lane & (LPR - 1);
-#pragma unroll
-  for (int i = 0; i < EPL; ++i)
-    if (at * EPL + i < A.E) all[at * EPL + i] = v[i];
-  wave_sync();
-  constexpr int GPL = 64 / LPR;  // groups a lane: at most 64 in all
-  V g[GPL];
-#pragma unroll
-  for (int q = 0; q < GPL; ++q) {
-    const int grp = at * GPL + q;
-    V b1 = (V)-INFINITY, b2 = (V)-INFINITY;
-    if (grp < A.groups)
-      for (int i = 0; i < A.each; ++i) {
-        const V x = all[grp * A.each + i], lo = x < b1 ? x : b1;
-        b1 = x > b1 ? x : b1;
-        b2 = lo > b2 ? lo : b2;
-      }
-    g[q] = A.best == 2 && b2 != (V)-INFINITY ? b1 + b2 : b1;
-  }
-  wave_sync();
-  uint64_t kept = 0;
-  V b = local_max(g);
-  for (int j = 0; j < A.top_groups; ++j) {
-    const V m = row_max<LPR>(b);
-    const uint64_t have = row_ballot<LPR>(b == m, lane);
-    const int first = __ffsll((unsigned long long)have) - 1;
-    int hit = 0;
-    if (at == first) {
-      bool found = false;
-#pragma unroll
-      for (int q = 0; q < GPL; ++q) {
-        const bool here = !found && g[q] == b;
-        hit = here ? q : hit;
-        g[q] = here ? (V)-INFINITY : g[q];
-        found |= here;
-      }
-      b = local_max(g);
+// The values that define the selection, logits or float64 scores with their
+// bias, -infinity for NaN and what is not there, into all[E] (X.area).
+template <class L, class V, int LPR, int EPL>
+__device__ __forceinline__ void exact_values(const RouteArgs& A, int at, const L* row, const RowLds& X) {
+  const int lo = at * EPL;
+  V* all = reinterpret_cast<V*>(X.area);
+  V x[EPL], top = (V)-INFINITY, sum = 0;
+  load_row<EPL>(row, lo, A.E, A.wide, x);
+  if (sizeof(V) == 8 && (sizeof(L) < 8 || A.by_score)) {
+    if (!A.sigmoid) {
+      top = row_max<LPR>(local_max(x));
+      if (top == (V)-INFINITY) top = 0;
     }
-    hit = __shfl(hit, (lane & ~(LPR - 1)) + first);
-    if (m != (V)-INFINITY) kept |= 1ull << (first * GPL + hit);
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) all[lo + i] = A.sigmoid ? -x[i] : x[i] - top;
+    // (loops of few exponentials: the code of all of them at once would push the rest out of the caches)
+#pragma unroll 4
+    for (int i = 0; i < EPL; ++i) {
+      const V e = exp_of(all[lo + i]);
+      all[lo + i] = A.sigmoid ? (V)1 / ((V)1 + e) : e;
+      sum += e;
+    }
+    sum = A.sigmoid ? (V)1 : row_sum<LPR>(sum);
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+      const V s = all[lo + i] / sum + (A.bias && lo + i < A.E ? (V)A.bias[lo + i] : (V)0);
+      all[lo + i] = x[i] == (V)-INFINITY || s != s ? (V)-INFINITY : s;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) all[lo + i] = x[i] == x[i] ? x[i] : (V)-INFINITY;
   }
+  wave_sync();
+}
+
+// Experts outside the kept groups leave the selection, by float32 values v
+// that are at most `margin` / 4 off; by the exact ones where that does not
+// decide.
+template <class L, class V, int LPR, int EPL>
+__device__ __forceinline__ void keep_groups(float (&v)[EPL], const RouteArgs& A, int at, const L* row, float margin,
+                                            const RowLds& X) {
+  float* value = reinterpret_cast<float*>(X.group);
+  int* keep = reinterpret_cast<int*>(X.group + 64 * 8);
+  const int lg = A.group_lanes;  // log2 of a group's lanes where it is made of whole ones, else -1
+  if (lg >= 0) {
+    float b1 = -INFINITY, b2 = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+      b2 = fmaxf(b2, fminf(b1, v[i]));
+      b1 = fmaxf(b1, v[i]);
+    }
+    const auto join = [&](float o1, float o2) {
+      b2 = fmaxf(fminf(b1, o1), fmaxf(b2, o2));
+      b1 = fmaxf(b1, o1);
+    };
+    if (lg > 0) join(lane_move<0xB1>(b1), lane_move<0xB1>(b2));
+    if (lg > 1) join(lane_move<0x4E>(b1), lane_move<0x4E>(b2));
+    if (lg > 2) join(lane_move<0x141>(b1), lane_move<0x141>(b2));
+    if (lg > 3) join(lane_move<0x140>(b1), lane_move<0x140>(b2));
+    if ((at & ((1 << lg) - 1)) == 0 && at >> lg < A.groups) value[at >> lg] = A.best == 2 && b2 != -INFINITY ? b1 + b2 : b1;
+  } else {
+    float* all = reinterpret_cast<float*>(X.area);
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) all[at * EPL + i] = v[i];
+    wave_sync();
+    value_groups<LPR>(A, at, all, value);
+  }
+  wave_sync();
+  float least = INFINITY, most = -INFINITY;
+  rank_groups<LPR>(A, at, value, keep, least, most);
+  wave_sync();
+  if (margin != 0.f) {
+    least = -row_max<LPR>(-least);
+    most = row_max<LPR>(most);
+    if (!(most == -INFINITY || least - most > margin + 0x1p-23f * (fabsf(least) + fabsf(most)))) {
+      V a = 0, b = 0, *exact = reinterpret_cast<V*>(X.group);
+      exact_values<L, V, LPR, EPL>(A, at, row, X);
+      value_groups<LPR>(A, at, reinterpret_cast<V*>(X.area), exact);
+      wave_sync();
+      rank_groups<LPR>(A, at, exact, keep, a, b);
+      wave_sync();
+    }
+  }
+  if (lg >= 0) {
+    const bool in = at >> lg < A.groups && keep[at >> lg];
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) v[i] = in ? v[i] : -INFINITY;
+  } else {
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) v[i] = at * EPL + i < A.E && keep[A.by_each.quotient(at * EPL + i)] ? v[i] : -INFINITY;
+  }
+}
+
+// The experts of a row in 32-bit keys: the upper bits of the value's order,
+// below them the expert's place (LOGITS: of the row, so that all keys differ;
+// else of the lane). The lanes' keys are sorted, each step takes the largest
+// of the lanes' first ones: the selection and one or two behind it. Where
+// neighbours among these are closer than what the keys tell apart (the bits
+// cut off, `margin` for values that are themselves rounded), the row is not
+// decided and false returned; logits whose keys are the same are put in their
+// order if the last candidate's key is another. (A lane's keys come out of LDS
+// one by one: shifted in registers they took a third of the kernel's
+// instructions.)
+template <class L, int LPR, int EPL, bool LOGITS>
+__device__ __forceinline__ bool select_keys(const float (&v)[EPL], const RouteArgs& A, int lane, const L* row, float margin,
+                                            const RowLds& X) {
+  constexpr uint32_t kMask = (LOGITS ? LPR * EPL : EPL) - 1;
+  constexpr int kMore = kSpare;
+  const int at = lane & (LPR - 1);
+  uint32_t key[EPL], low = 0;
 #pragma unroll
   for (int i = 0; i < EPL; ++i) {
-    const int e = at * EPL + i;
-    if (e < A.E && !(kept >> (e / A.each) & 1)) v[i] = (V)-INFINITY;
+    if constexpr (LOGITS) low |= __float_as_uint(v[i]);
+    key[i] = (ordered(v[i]) & ~kMask) | (kMask - (LOGITS ? at * EPL + i : i));
   }
+  // logits whose low bits are all zero (bf16 ones) lose nothing in the keys
+  bool whole = LOGITS && sizeof(L) == 2;
+  if constexpr (LOGITS && sizeof(L) == 4) whole = row_ballot<LPR>((low & kMask) != 0, lane) == 0;
+  sort_keys(key);
+  // The keys behind the first one wait in LDS until the lane has had that. (All
+  // lanes' keys are at least 64, those of what is not there among them: the
+  // zero behind a lane's last one never is the largest.)
+  uint32_t* list = reinterpret_cast<uint32_t*>(X.area) + at * kListStep<EPL>;
+#pragma unroll
+  for (int i = 0; i < EPL; i += 4)
+    *reinterpret_cast<u32x4*>(list + i) = u32x4{key[i + 1], key[i + 2], key[i + 3], i + 4 < EPL ? key[i + 4 < EPL ? i + 4 : 0] : 0u};
+  uint32_t head = key[0];
+  const int total = LOGITS && sizeof(L) == 2 ? A.k : A.k + kMore;
+  for (int j = 0; j < total; ++j) {
+    const uint32_t mine = LOGITS ? head : head & ~kMask;
+    const uint32_t m = over_row<LPR>(mine, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+    bool win = mine == m;
+    if constexpr (!LOGITS) win = at == __ffsll((unsigned long long)row_ballot<LPR>(win, lane)) - 1;
+    if (win) {
+      X.key[j] = head;
+      if constexpr (!LOGITS) X.e[j] = at;
+      head = *list++;
+    }
+  }
+  wave_sync();
+  for (int j = at; j < total; j += LPR) {
+    const uint32_t m = X.key[j];
+    X.e[j] = m < kNone ? -1 : (LOGITS ? 0 : X.e[j] * EPL) + (int)(kMask - (m & kMask));
+    X.key[j] = m & ~kMask;
+  }
+  wave_sync();
+  if (whole) return true;
+  const auto near = [&](uint32_t a, uint32_t b) {  // a >= b
+    if (b < kNone) return false;
+    if constexpr (LOGITS) return a == b;
+    const float hi = from_ordered(a), lo = from_ordered(b);
+    return !(hi - lo > margin + fabsf(lo) * (0x1p-22f * (float)(kMask + 1)) + 0x1p-120f);
+  };
+  bool close = false;
+  for (int j = at; j < A.k; j += LPR) close |= near(X.key[j], X.key[j + 1]);
+  if (row_ballot<LPR>(close, lane) == 0) return true;
+  if (near(X.key[A.k - 1], X.key[total - 1])) return false;
+  // the candidates' ranks: by logit and expert, or by float64 score and expert
+  if constexpr (LOGITS) {
+    uint64_t* value = reinterpret_cast<uint64_t*>(X.area);
+    for (int j = at; j < total; j += LPR) {
+      const int e = X.e[j];
+      value[j] = e < 0 ? (uint64_t)(total - j) : (uint64_t)ordered((float)widen(row[e])) << 32 | (uint32_t)~e;
+    }
+    wave_sync();
+    for (int j = at; j < total; j += LPR) {
+      const uint64_t x = value[j];
+      int before = 0;
+#pragma unroll 4
+      for (int i = 0; i < total; ++i) before += value[i] > x;
+      X.key[before] = (uint32_t)X.e[j];
+    }
+  } else {
+    double *value = reinterpret_cast<double*>(X.area), top = 0, sum = 1;
+    const bool by_score = sizeof(L) < 8 || A.by_score;
+    if (by_score && !A.sigmoid) {
+      double z[EPL];
+      load_row<EPL>(row, at * EPL, A.E, A.wide, z);
+      top = row_max<LPR>(local_max(z));
+      sum = 0;
+      for (int e = at * EPL; e < at * EPL + EPL && e < A.E; ++e) sum += exp_of((double)widen(row[e]) - top);
+      sum = row_sum<LPR>(sum);
+    }
+    for (int j = at; j < total; j += LPR) {
+      const int e = X.e[j];
+      double x = e >= 0 ? (double)widen(row[e]) : -INFINITY;
+      if (by_score && e >= 0) {
+        const double y = exp_of(A.sigmoid ? -x : x - top);
+        x = (A.sigmoid ? 1.0 / (1.0 + y) : y / sum) + (A.bias ? (double)A.bias[e] : 0.0);
+      }
+      value[j] = x;
+    }
+    wave_sync();
+    for (int j = at; j < total; j += LPR) {
+      const double x = value[j];
+      const int e = X.e[j];
+      int before = 0;
+#pragma unroll 4
+      for (int i = 0; i < total; ++i) before += value[i] > x || (value[i] == x && (X.e[i] < e || (X.e[i] == e && i < j)));
+      X.key[before] = (uint32_t)e;
+    }
+  }
+  wave_sync();
+  for (int j = at; j < A.k; j += LPR) X.e[j] = (int)X.key[j];
+  wave_sync();
+  return true;
 }
 
-// The selection and the weights of row n; sel[k] (LDS of this row) receives the experts.
+// The selection in the exact values, for rows that neither keys nor their
+// candidates decide (several equal or nearly equal values at its end): loops
+// over LDS, as it is rare. V is float for float32 logits alone.
 template <class L, class V, int LPR, int EPL>
-__device__ __forceinline__ void route_row(const RouteArgs& A, int n, int lane, int* sel, V* all) {
+__device__ __forceinline__ void select_values(const RouteArgs& A, int lane, const L* row, const RowLds& X) {
+  const int at = lane & (LPR - 1), lo = at * EPL, hi = lo + EPL < A.E ? lo + EPL : A.E;
+  V* all = reinterpret_cast<V*>(X.area);
+  exact_values<L, V, LPR, EPL>(A, at, row, X);
+  if (A.groups > 1) {
+    const int* keep = reinterpret_cast<const int*>(X.group + 64 * 8);
+    for (int e = lo; e < hi; ++e)
+      if (!keep[A.by_each.quotient(e)]) all[e] = (V)-INFINITY;
+  }
+  V last = (V)INFINITY;
+  int last_e = -1;
+  for (int j = 0; j < A.k; ++j) {
+    V best = (V)-INFINITY;
+    int be = -1;
+#pragma unroll 4
+    for (int e = lo; e < hi; ++e) {
+      const V x = all[e];
+      const bool left = x < last || (x == last && e > last_e);
+      if (left && x > best) {
+        best = x;
+        be = e;
+      }
+    }
+    last = row_max<LPR>(best);
+    const int first = __ffsll((unsigned long long)row_ballot<LPR>(best == last, lane)) - 1;
+    last_e = __shfl(be, (lane & ~(LPR - 1)) + first);
+    if (at == first) X.e[j] = be;
+  }
+  wave_sync();
+}
+
+// The selection and the weights of row n, whose logits are z; X.e receives the experts.
+template <class L, class V, int LPR, int EPL>
+__device__ __forceinline__ void route_row(const RouteArgs& A, int n, int lane, const RowLds& X,
+                                          const typename Wide<L>::type (&z)[EPL]) {
   typedef typename Wide<L>::type T;
   const int at = lane & (LPR - 1), e0 = at * EPL;
   const L* row = static_cast<const L*>(A.logits) + (int64_t)n * A.ld;
-  V v[EPL];
-  load_row<EPL>(row, e0, A.E, A.wide, v);
-  // largest logit and sum of the softmax over all experts, where they are needed
-  V top = 0, sum = 1;
-  const bool whole = !A.sigmoid && (A.by_score || !A.renorm);
-  if (whole) {
-    V b = (V)-INFINITY;
-#pragma unroll
-    for (int i = 0; i < EPL; ++i) b = v[i] > b ? v[i] : b;
-    top = row_max<LPR>(b);
-    if (top == (V)-INFINITY) top = 0;
-    sum = 0;
-#pragma unroll
-    for (int i = 0; i < EPL; ++i) sum += exp_of(v[i] - top);
-    sum = row_sum<LPR>(sum);
-  }
+  // (float32 values: logits; float64 values of narrower logits: scores)
+  const bool by_score = sizeof(V) == 8 && (sizeof(L) < 8 || A.by_score);
+  T top = 0, sum = 1;
   bool bad = false;
-  if (A.by_score) {
+  {
+    float v[EPL];
+    {
+      if (!A.sigmoid && (by_score || !A.renorm)) {
+        // the largest logit (0 if there is none) and the exponentials' sum relative to it
+        top = row_max<LPR>(local_max(z));
+        if (top == (T)-INFINITY) top = 0;
+        sum = 0;
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) {
-      const int e = e0 + i;
-      if (v[i] == (V)-INFINITY) continue;
-      V s;
-      if (A.sigmoid) s = (V)1 / ((V)1 + exp_of(-v[i]));
-      else s = exp_of(v[i] - top) / sum;
-      v[i] = s + (A.bias ? (V)A.bias[e] : (V)0);
+        for (int i = 0; i < EPL; ++i) sum += quick_exp(z[i] - top);
+        sum = row_sum<LPR>(sum);
+      }
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) {
+        // (a float64 logit below float32's range is one all the same)
+        const float f = (float)z[i];
+        v[i] = sizeof(T) == 8 && f == -INFINITY && z[i] != (T)-INFINITY ? -3.402823466e38f : f;
+      }
+      if (by_score) {
+        // float32 scores: a sigmoid s is off by at most s (1 - s) (|z| + 2) 2^-24 for the exponential (below
+        // 3/4 2^-24) and 3 2^-24 for sum and reciprocal, so two of them by less than 2^-21; a softmax, whose
+        // largest is 1 / sum, by 2^-18 of that (the mean distance from the top that the sum weighs is below ln 1024)
+        if (A.sigmoid) {
+#pragma unroll
+          for (int i = 0; i < EPL; ++i)
+            v[i] = v[i] == -INFINITY ? v[i] : __builtin_amdgcn_rcpf(1.0f + quick_exp(-v[i]));
+        } else {
+          const float share = 1.0f / (float)sum;
+#pragma unroll
+          for (int i = 0; i < EPL; ++i) v[i] = v[i] == -INFINITY ? v[i] : quick_exp((float)(z[i] - top)) * share;
+        }
+        if (A.bias) {
+#pragma unroll
+          for (int i = 0; i < EPL; ++i)
+            if (e0 + i < A.E) v[i] += A.bias[e0 + i];
+        }
+      }
     }
+    float any = 0;  // NaN where a value is (or infinities of either sign are)
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) any += v[i];
+    if (row_ballot<LPR>(any != any, lane) != 0) {
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) {
+        bad |= v[i] != v[i];
+        v[i] = v[i] != v[i] ? -INFINITY : v[i];
+      }
+      bad = row_ballot<LPR>(bad, lane) != 0;
+    }
+    float margin = sizeof(T) == 8 ? 0x1p-100f : 0.f;  // (float64 logits are rounded, too)
+    if (by_score) margin = A.sigmoid ? 0x1p-21f : 0x1p-17f / (float)sum + 0x1p-22f;
+    if (A.groups > 1) keep_groups<L, V, LPR>(v, A, at, row, 2.f * margin, X);
+    if (!select_keys<L, LPR, EPL, sizeof(V) == 4>(v, A, lane, row, margin, X)) select_values<L, V, LPR, EPL>(A, lane, row, X);
   }
-#pragma unroll
-  for (int i = 0; i < EPL; ++i)
-    if (v[i] != v[i]) {
-      bad = true;
-      v[i] = (V)-INFINITY;
-    }
-  bad = row_ballot<LPR>(bad, lane) != 0;
-  if (A.groups > 1) keep_groups<LPR, EPL>(v, A, lane, all);
-  select_top<LPR, EPL>(v, A.k, lane, sel);
-  wave_sync();
 
-  // the weights, a selection or two a lane
-  constexpr int JPL = kMostK / LPR > 0 ? kMostK / LPR : 1;
-  T z[JPL], w[JPL];
-  int e[JPL];
-  T most = (T)-INFINITY;
-#pragma unroll
-  for (int q = 0; q < JPL; ++q) {
-    const int j = q * LPR + at;
-    e[q] = -1;
-    z[q] = (T)-INFINITY;
-    if (q * LPR >= A.k) continue;
-    e[q] = j < A.k ? sel[j] : -1;
-    if (e[q] >= 0) z[q] = (T)widen(row[e[q]]);
-    most = z[q] > most ? z[q] : most;
+  // the weights, a selection a lane
+  T* part = reinterpret_cast<T*>(X.area);
+  T most = (T)-INFINITY, total = 0;
+  for (int j = at; j < A.k; j += LPR) {
+    const int e = X.e[j];
+    const T x = e >= 0 ? (T)widen(row[e]) : (T)-INFINITY;
+    part[j] = x;
+    most = x > most ? x : most;
   }
   if (A.renorm) most = row_max<LPR>(most);
-  T total = 0;
-#pragma unroll
-  for (int q = 0; q < JPL; ++q) {
-    w[q] = 0;
-    if (e[q] < 0) continue;
+  for (int j = at; j < A.k; j += LPR) {
+    const T x = part[j];
+    T w;
     if (!A.sigmoid) {
-      w[q] = A.renorm ? exp_of(z[q] - most) : exp_of(z[q] - (T)top) / (T)sum;
-    } else if (A.renorm && most < 0) {
-      // all of them below 1/2: relative to exp(most), so that none is lost
-      w[q] = exp_of(z[q] - most) / ((T)1 + exp_of(z[q]));
+      w = exp_of(x - (A.renorm ? most : top));
     } else {
-      w[q] = (T)1 / ((T)1 + exp_of(-z[q]));
+      // all of them below 1/2: relative to exp(most), so that none is lost
+      const bool low = A.renorm && most < 0;
+      w = (low ? exp_of(x - most) : (T)1) / ((T)1 + exp_of(low ? x : -x));
     }
-    total += w[q];
+    w = x == (T)-INFINITY ? (T)0 : w;
+    part[j] = w;
+    total += w;
   }
   if (A.renorm) total = row_sum<LPR>(total);
-#pragma unroll
-  for (int q = 0; q < JPL; ++q) {
-    const int j = q * LPR + at;
-    if (j >= A.k) continue;
-    T r = A.renorm && e[q] >= 0 ? w[q] / total : w[q];
-    r *= (T)A.scale;
-    A.idx[(int64_t)n * A.k + j] = e[q];
-    A.weight[(int64_t)n * A.k + j] = bad ? NAN : (float)r;
+  else total = A.sigmoid ? (T)1 : sum;
+  const T share = (T)A.scale / total;
+  for (int j = at; j < A.k; j += LPR) {
+    const int e = X.e[j];
+    A.idx[(int64_t)n * A.k + j] = e;
+    A.weight[(int64_t)n * A.k + j] = bad ? NAN : e < 0 ? 0.f : (float)(part[j] * share);
   }
 }
 
@@ -396,22 +671,36 @@ template <class L, class V, int LPR, int EPL, int NT, bool ONE>
 __global__ __launch_bounds__(NT) void k_route_rows(const RouteArgs A) {
   constexpr int ROWS = NT / LPR;  // rows at a time
   extern __shared__ __align__(16) unsigned char lds[];
-  V* all = reinterpret_cast<V*>(lds);                                      // [ROWS][E] with groups
-  int* sel = reinterpret_cast<int*>(all + (A.groups > 1 ? ROWS * A.E : 0));  // [ROWS][k], all rows if ONE
-  int* count = sel + (ONE ? std::max(A.N, ROWS) : ROWS) * A.k;             // [E + 1], ONE: then [NT / 64][E]
+  int* sel = reinterpret_cast<int*>(lds + ROWS * A.row_lds);  // ONE: [N][k]
+  int* count = sel + (ONE ? A.N * A.k : 0);                   // [E + 1], ONE: then [NT / 64][E]
   const int tid = threadIdx.x, lane = tid & 63, r = tid / LPR;
+  unsigned char* own = lds + r * A.row_lds;
+  const RowLds X(own, A);
   if (!ONE && A.place) {
     for (int i = tid; i < A.E; i += NT) count[i] = 0;
     __syncthreads();
   }
   const int first = ONE ? 0 : blockIdx.x * A.block_rows;
   const int last = ONE ? A.N : (int)std::min<int64_t>(A.N, (int64_t)first + A.block_rows);
+  // a row's logits are on their way while the one before is worked on
+  typedef typename Wide<L>::type T;
+  const auto load = [&](int n, T (&z)[EPL]) {
+    if (n < last) load_row<EPL>(static_cast<const L*>(A.logits) + (int64_t)n * A.ld, (lane & (LPR - 1)) * EPL, A.E, A.wide, z);
+  };
+  T next[EPL];
+  load(first + r, next);
   for (int n = first + r; n < last; n += ROWS) {
-    int* mine = sel + (ONE ? n : r) * A.k;
-    route_row<L, V, LPR, EPL>(A, n, lane, mine, all + (A.groups > 1 ? r * A.E : 0));
-    if (!ONE && A.place)
-      for (int j = lane & (LPR - 1); j < A.k; j += LPR)
-        if (mine[j] >= 0) atomicAdd(&count[mine[j]], 1);
+    T z[EPL];
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) z[i] = next[i];
+    load(n + ROWS, next);
+    route_row<L, V, LPR, EPL>(A, n, lane, X, z);
+    if (ONE || A.place)
+      for (int j = lane & (LPR - 1); j < A.k; j += LPR) {
+        const int e = X.e[j];
+        if (ONE) sel[n * A.k + j] = e;
+        else if (e >= 0) atomicAdd(&count[e], 1);
+      }
     wave_sync();
   }
   if (!A.place) return;
@@ -473,6 +762,9 @@ __global__ __launch_bounds__(1024) void k_route_scan(const RouteArgs A) {
   }
 }
 
+// Places of a block's slots. SUM: few blocks, whose counts every workgroup sums
+// by itself; else k_route_scan has.
+template <bool SUM>
 __global__ __launch_bounds__(256) void k_route_place(const RouteArgs A) {
   constexpr int NT = 256;
   extern __shared__ __align__(16) unsigned char lds[];
@@ -483,13 +775,34 @@ __global__ __launch_bounds__(256) void k_route_place(const RouteArgs A) {
   const int n = (int)std::min((int64_t)A.block_rows * A.k, (int64_t)A.N * A.k - first);
   const int32_t* idx = A.idx + first;
   const auto slot = [&](int i) { return idx[i]; };
-  for (int e = tid; e < A.E; e += NT) count[e] = A.count[(int64_t)A.blocks * A.E + e];
+  int before[1024 / NT];
+#pragma unroll
+  for (int q = 0; q < 1024 / NT; ++q) {
+    const int e = q * NT + tid;
+    if (e >= A.E) break;
+    if constexpr (SUM) {
+      int total = 0, sum = 0;
+#pragma unroll 8
+      for (int c = 0; c < A.blocks; ++c) {
+        const int v = A.count[c * A.E + e];
+        total += v;
+        sum += c < b ? v : 0;
+      }
+      count[e] = total;
+      before[q] = sum;
+    } else {
+      count[e] = A.count[(int64_t)A.blocks * A.E + e];
+      before[q] = A.count[(int64_t)b * A.E + e];
+    }
+  }
   count_slots<NT>(n, A.E, next, slot);
   scan_experts<NT>(count, A.E, part);
   if (b == 0)
     for (int e = tid; e <= A.E; e += NT) A.offsets[e] = count[e];
   __syncthreads();
-  for (int e = tid; e < A.E; e += NT) count[e] += A.count[(int64_t)b * A.E + e];
+#pragma unroll
+  for (int q = 0; q < 1024 / NT; ++q)
+    if (q * NT + tid < A.E) count[q * NT + tid] += before[q];
   __syncthreads();
   start_slots<NT>(A.E, next, count);
   place_slots<NT>(n, A.E, next, slot, A.place + first);
@@ -592,30 +905,41 @@ __global__ __launch_bounds__(256) void k_route_backward(const RouteArgs A) {
 }
 
 template <class L, class V, int LPR, int EPL>
-hipError_t run_rows(const RouteArgs& A, hipStream_t s) {
+hipError_t run_rows(const RouteArgs& given, hipStream_t s) {
+  RouteArgs A = given;
+  A.slots = (A.k + kSpare + 1) / 2 * 2;
+  A.row_lds = row_bytes<V, LPR, EPL>(A);
+  A.by_each = Divisor(A.each);
+  A.group_lanes = -1;
+  for (int lg = 0; 1 << lg <= 16; ++lg)
+    if (A.each == EPL << lg) A.group_lanes = lg;
   if (A.N <= kRouteSmall) {
-    constexpr int NT = 512, ROWS = NT / LPR;
-    const size_t lds = (A.groups > 1 ? (size_t)ROWS * A.E * sizeof(V) : 0) + 4 * ((size_t)std::max(A.N, ROWS) * A.k +
-                       A.E + 1 + NT / 64 * A.E + NT / 64);
+    constexpr int NT = EPL <= 8 && LPR == 16 ? 512 : 256, ROWS = NT / LPR;  // (their LDS is below 160 KiB)
+    const size_t lds = (size_t)ROWS * A.row_lds + 4 * ((size_t)A.N * A.k + A.E + 1 + NT / 64 * A.E + NT / 64);
     k_route_rows<L, V, LPR, EPL, NT, true><<<dim3(1), dim3(NT), lds, s>>>(A);
     return hipGetLastError();
   }
   constexpr int NT = 256, ROWS = NT / LPR;
-  const size_t lds = (A.groups > 1 ? (size_t)ROWS * A.E * sizeof(V) : 0) + 4 * ((size_t)ROWS * A.k + A.E + 1);
+  const size_t lds = (size_t)ROWS * A.row_lds + 4 * ((size_t)A.E + 1);
   k_route_rows<L, V, LPR, EPL, NT, false><<<dim3((unsigned)A.blocks), dim3(NT), lds, s>>>(A);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !A.place) return e;
+  const size_t lds2 = 4 * ((size_t)A.E + 1 + 4 * A.E + 4);
+  if (A.blocks <= kSumBlocks) {
+    k_route_place<true><<<dim3((unsigned)A.blocks), dim3(256), lds2, s>>>(A);
+    return hipGetLastError();
+  }
   k_route_scan<<<dim3((unsigned)((A.E + 15) / 16)), dim3(1024), 0, s>>>(A);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  const size_t lds2 = 4 * ((size_t)A.E + 1 + 4 * A.E + 4);
-  k_route_place<<<dim3((unsigned)A.blocks), dim3(256), lds2, s>>>(A);
+  k_route_place<false><<<dim3((unsigned)A.blocks), dim3(256), lds2, s>>>(A);
   return hipGetLastError();
 }
 
 template <class L, class V>
 hipError_t run_width(const RouteArgs& A, hipStream_t s) {
-  if (A.E <= 64) return run_rows<L, V, 16, 4>(A, s);
-  if (A.E <= 128) return run_rows<L, V, 16, 8>(A, s);
+  const bool one = A.N <= kRouteSmall;
+  if (A.E <= 64) return one ? run_rows<L, V, 16, 4>(A, s) : run_rows<L, V, 8, 8>(A, s);
+  if (A.E <= 128) return one ? run_rows<L, V, 16, 8>(A, s) : run_rows<L, V, 8, 16>(A, s);
   if (A.E <= 256) return run_rows<L, V, 16, 16>(A, s);
   if (A.E <= 512) return run_rows<L, V, 64, 8>(A, s);
   return run_rows<L, V, 64, 16>(A, s);
@@ -644,7 +968,7 @@ hipError_t back_width(const RouteArgs& A, hipStream_t s) {
 // Lanes of a row: its experts stay in at most 16 registers a lane. Rows of a
 // block: a whole number of passes of its 256 threads.
 void plan_route(RouteArgs* A) {
-  const int rows = A->E <= 256 ? 16 : 4;  // of 256 threads at a time
+  const int rows = A->E <= 128 ? 32 : A->E <= 256 ? 16 : 4;  // of 256 threads at a time
   const int64_t per = ((int64_t)A->N + kRouteBlocks - 1) / kRouteBlocks;
   A->block_rows = (int32_t)std::max<int64_t>(rows, (per + rows - 1) / rows * rows);
   A->blocks = (int32_t)(((int64_t)A->N + A->block_rows - 1) / A->block_rows);

@@ -8,6 +8,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "cardan_ffn_plan.h"
+
 
 namespace cardan {
 
@@ -37,6 +39,8 @@ struct RouteArgs {
   int32_t* offsets;                        // [E + 1] with place
   int32_t* count;                          // [blocks][E] (workspace), then totals [E]
   int32_t block_rows, blocks;
+  Divisor by_each;                         // division by `each`
+  int32_t group_lanes, row_lds, slots;
   const float* dweight;                    // [N][k]
   void* dlogits;                           // [N][dld]
 };

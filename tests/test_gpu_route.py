@@ -388,3 +388,51 @@ def test_other_streams_and_shared_workspaces_in_turn(C):
         got = [C.route_rows(v, 8, ws=ws) for v in z]
     torch.cuda.current_stream().wait_stream(s)
     assert all(torch.equal(a, b) for x, y in zip(got, want) for a, b in zip(x, y))
+
+
+@pytest.mark.parametrize("E", [16, 64, 128, 256, 512, 1024])
+def test_logits_a_step_apart(C, E):
+    """Values that differ in their last bits alone, in every order of the experts."""
+    g = torch.Generator().manual_seed(E)
+    for base in (1.0, -3.0, 1e-30, 1e30):
+        bits = torch.tensor(base).view(torch.int32) + torch.randint(0, 3, (80, E), generator=g, dtype=torch.int32)
+        z = bits.view(F32).cuda()
+        for k in (1, 8, min(E, 17), min(E, 32)):
+            _check(C, z, None, _opts(k, "softmax"))
+            _check(C, z, None, _opts(k, "sigmoid", True, 1.0, 4, 3, 1) if E // 4 * 3 >= k else _opts(k))
+
+
+@pytest.mark.parametrize("E", [16, 64, 256, 512])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_scores_that_float32_does_not_tell_apart(C, E, score):
+    """Biases that undo the scores up to 2^-30 or so: the order is float64's. Differences are
+    above 2^-40, so that two float64 exponentials agree on it."""
+    g = torch.Generator().manual_seed(E + 1)
+    z = torch.randn((90, E), generator=g, dtype=F64).float()
+    z[1:] = z[:1] + torch.randint(-4, 5, (89, E), generator=g).float() * 2.0 ** -23
+    s = torch.sigmoid(z.double()) if score == "sigmoid" else torch.softmax(z.double(), 1)
+    bias = (0.5 - s[0]).float()
+    v = (s + bias.double()).sort(1).values
+    keep = (v.diff(dim=1) > 2.0 ** -44).all(1)
+    assert keep.sum() >= 20
+    z = z[keep].cuda()
+    for o in (_opts(5, score), _opts(5, score, False, 1.0, 4, 2, 2), _opts(5, score, True, 1.0, 4, 2, 1)):
+        _check(C, z, bias.cuda(), o)
+
+
+def test_large_biases(C):
+    for size in (1e3, 1e6, 1e-6):
+        for o in (_opts(6, "sigmoid"), _opts(6, "softmax", True, 1.0, 4, 2, 2)):
+            _check(C, _logits(100, 64, F32, 3), _bias(64) * size, o)
+
+
+@pytest.mark.parametrize("groups", [1, 4])
+def test_float64_logits_that_float32_does_not_tell_apart(C, groups):
+    g = torch.Generator().manual_seed(groups)
+    for scale in (1.0, 1e200, 1e-200):
+        z = (1.0 + torch.randint(-9, 10, (80, 64), generator=g).double() * 2.0 ** -40) * scale
+        z[:, ::5] *= -1
+        for o in (_opts(6, "softmax", True, 1.0, groups, max(1, groups // 2), 1),):
+            idx, w, place, offsets = C.route_rows(z.cuda(), **o)
+            want, _, _ = _oracle(z, None, o)
+            assert np.array_equal(idx.cpu().numpy(), want)
