@@ -481,7 +481,7 @@ typedef struct {
   float* m_scale;     /* 8-bit moments alone                                  */
   float* v_scale;
   cardan_bf16* copy;  /* receives float32 weights rounded to bf16, or NULL    */
-  int64_t n;          /* values, 0 allowed                                    */
+  int64_t n;          /* values, 0 to 2^34                                    */
 } cardan_adamw_tensor;
 
 typedef struct {

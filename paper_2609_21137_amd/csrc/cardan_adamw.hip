@@ -23,8 +23,8 @@ namespace {
 
 constexpr int kThreads = 256, kEach = 8;           // values of a lane at once: half a wave holds a block
 constexpr int kPass = 64 * kEach;                  // values of a wave at once
-constexpr int kPasses = 2;
-constexpr int kWork = kThreads / 64 * kPass * kPasses;  // values of a workgroup
+constexpr int kWork = kThreads / 64 * kPass;        // values of a workgroup: one pass (two 4 % slower, four 6 %)
+static_assert(kWork == kAdamwWork, "the host counts workgroups");
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -156,154 +156,151 @@ __global__ __launch_bounds__(kThreads) void k_adamw(const AdamwArgs A) {
   }
   const float gs = A.grad_scale ? A.grad_scale[0] : 1.0f;
 
-#pragma unroll 1
-  for (int pass = 0; pass < kPasses; ++pass) {
-    const int64_t at = start + (pass * (kThreads / 64) + wave) * kPass + lane * kEach;
-    const int64_t left = n - at;
-    const int have = left >= kEach ? kEach : left > 0 ? (int)left : 0;
-    const bool full = have == kEach;
-    Floats p, g, m, v;
+  const int64_t at = start + wave * kPass + lane * kEach;
+  const int64_t left = n - at;
+  const int have = left >= kEach ? kEach : left > 0 ? (int)left : 0;
+  const bool full = have == kEach;
+  Floats p, g, m, v;
 #pragma unroll
-    for (int q = 0; q < kEach; ++q) p.v[q] = g.v[q] = m.v[q] = v.v[q] = 0.f;
-    float ms = 0.f, vs = 0.f;
-    uint8_t* m8 = static_cast<uint8_t*>(T.m);
-    uint8_t* v8 = static_cast<uint8_t*>(T.v);
-    const int64_t block = at / kAdamwBlock;
-    if (full) {
-      p = PBF ? load_bf16(static_cast<const uint16_t*>(T.p) + at) : load_f32(static_cast<const float*>(T.p) + at);
-      g = GBF ? load_bf16(static_cast<const uint16_t*>(T.g) + at) : load_f32(static_cast<const float*>(T.g) + at);
-      if constexpr (!S8) {
-        m = load_f32(static_cast<const float*>(T.m) + at);
-        v = load_f32(static_cast<const float*>(T.v) + at);
-      }
-    } else {
-#pragma unroll
-      for (int q = 0; q < kEach; ++q) {
-        if (q >= have) break;
-        p.v[q] = PBF ? __uint_as_float((uint32_t) static_cast<const uint16_t*>(T.p)[at + q] << 16)
-                     : static_cast<const float*>(T.p)[at + q];
-        g.v[q] = GBF ? __uint_as_float((uint32_t) static_cast<const uint16_t*>(T.g)[at + q] << 16)
-                     : static_cast<const float*>(T.g)[at + q];
-        if constexpr (!S8) {
-          m.v[q] = static_cast<const float*>(T.m)[at + q];
-          v.v[q] = static_cast<const float*>(T.v)[at + q];
-        }
-      }
+  for (int q = 0; q < kEach; ++q) p.v[q] = g.v[q] = m.v[q] = v.v[q] = 0.f;
+  float ms = 0.f, vs = 0.f;
+  uint8_t* m8 = static_cast<uint8_t*>(T.m);
+  uint8_t* v8 = static_cast<uint8_t*>(T.v);
+  const int64_t block = at / kAdamwBlock;
+  if (full) {
+    p = PBF ? load_bf16(static_cast<const uint16_t*>(T.p) + at) : load_f32(static_cast<const float*>(T.p) + at);
+    g = GBF ? load_bf16(static_cast<const uint16_t*>(T.g) + at) : load_f32(static_cast<const float*>(T.g) + at);
+    if constexpr (!S8) {
+      m = load_f32(static_cast<const float*>(T.m) + at);
+      v = load_f32(static_cast<const float*>(T.v) + at);
     }
-    if constexpr (S8) {
-      u32x2 mc = {0, 0}, vc = {0, 0};
-      if (full) {
-        mc = *reinterpret_cast<const u32x2_at1*>(m8 + at);
-        vc = *reinterpret_cast<const u32x2_at1*>(v8 + at);
-      } else {
-#pragma unroll
-        for (int q = 0; q < kEach; ++q) {
-          if (q >= have) break;
-          mc[q >> 2] |= (uint32_t)m8[at + q] << 8 * (q & 3);
-          vc[q >> 2] |= (uint32_t)v8[at + q] << 8 * (q & 3);
-        }
-      }
-      if (have > 0) {
-        ms = T.ms[block];
-        vs = T.vs[block];
-      }
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const f32x2 a = q & 1 ? __builtin_amdgcn_cvt_pk_f32_fp8(mc[q >> 1], true) : __builtin_amdgcn_cvt_pk_f32_fp8(mc[q >> 1], false);
-        const f32x2 b = q & 1 ? __builtin_amdgcn_cvt_pk_f32_bf8(vc[q >> 1], true) : __builtin_amdgcn_cvt_pk_f32_bf8(vc[q >> 1], false);
-        m.v[2 * q] = a[0] * ms;
-        m.v[2 * q + 1] = a[1] * ms;
-        v.v[2 * q] = b[0] * vs;
-        v.v[2 * q + 1] = b[1] * vs;
-      }
-    }
-    uint32_t mtop = 0, vtop = 0;
+  } else {
 #pragma unroll
     for (int q = 0; q < kEach; ++q) {
-      const float x = g.v[q] * gs;
-      m.v[q] = m.v[q] * A.b1 + x * A.a1;
-      v.v[q] = v.v[q] * A.b2 + x * x * A.a2;
-      p.v[q] = p.v[q] - p.v[q] * lr_decay - (m.v[q] * lr_c1) / (sqrtf(v.v[q] * inv_c2) + A.eps);
-      if constexpr (S8) {
-        if (q < have) {
-          const uint32_t a = __float_as_uint(m.v[q]) & 0x7fffffffu, b = __float_as_uint(v.v[q]) & 0x7fffffffu;
-          mtop = a > mtop ? a : mtop;
-          vtop = b > vtop ? b : vtop;
-        }
+      if (q >= have) break;
+      p.v[q] = PBF ? __uint_as_float((uint32_t) static_cast<const uint16_t*>(T.p)[at + q] << 16)
+                   : static_cast<const float*>(T.p)[at + q];
+      g.v[q] = GBF ? __uint_as_float((uint32_t) static_cast<const uint16_t*>(T.g)[at + q] << 16)
+                   : static_cast<const float*>(T.g)[at + q];
+      if constexpr (!S8) {
+        m.v[q] = static_cast<const float*>(T.m)[at + q];
+        v.v[q] = static_cast<const float*>(T.v)[at + q];
       }
     }
-    uint32_t h[kEach];
-    if constexpr (S8 || PBF) {
-#pragma unroll
-      for (int q = 0; q < kEach; ++q) h[q] = mixed(at + q, t);
-    }
-    if constexpr (S8) {
-      const float new_ms = scale_of(block_max(mtop), 1.0f / 448.0f), new_vs = scale_of(block_max(vtop), 1.0f / 57344.0f);
-      const float mi = new_ms > 0.f ? 1.0f / new_ms : new_ms, vi = new_vs > 0.f ? 1.0f / new_vs : new_vs;
-      u32x2 mc = {0, 0}, vc = {0, 0};
-#pragma unroll
-      for (int q = 0; q < kEach; ++q) {
-        const uint32_t sign = __float_as_uint(m.v[q]) >> 24 & 0x80u;
-        mc[q >> 2] |= (code_of<3, -120, 0x7e>(fabsf(m.v[q]) * mi, h[q] & 0xffffu) | sign) << 8 * (q & 3);
-        vc[q >> 2] |= code_of<2, -112, 0x7b>(v.v[q] * vi, h[q] >> 16) << 8 * (q & 3);
-      }
-      if (full) {
-        *reinterpret_cast<u32x2_at1*>(m8 + at) = mc;
-        *reinterpret_cast<u32x2_at1*>(v8 + at) = vc;
-      } else {
-#pragma unroll
-        for (int q = 0; q < kEach; ++q) {
-          if (q >= have) break;
-          m8[at + q] = (uint8_t)(mc[q >> 2] >> 8 * (q & 3));
-          v8[at + q] = (uint8_t)(vc[q >> 2] >> 8 * (q & 3));
-        }
-      }
-      if (have > 0 && at % kAdamwBlock == 0) {
-        T.ms[block] = new_ms;
-        T.vs[block] = new_vs;
-      }
-    } else if (full) {
-      store_f32(static_cast<float*>(T.m) + at, m);
-      store_f32(static_cast<float*>(T.v) + at, v);
+  }
+  if constexpr (S8) {
+    u32x2 mc = {0, 0}, vc = {0, 0};
+    if (full) {
+      mc = *reinterpret_cast<const u32x2_at1*>(m8 + at);
+      vc = *reinterpret_cast<const u32x2_at1*>(v8 + at);
     } else {
 #pragma unroll
       for (int q = 0; q < kEach; ++q) {
         if (q >= have) break;
-        static_cast<float*>(T.m)[at + q] = m.v[q];
-        static_cast<float*>(T.v)[at + q] = v.v[q];
+        mc[q >> 2] |= (uint32_t)m8[at + q] << 8 * (q & 3);
+        vc[q >> 2] |= (uint32_t)v8[at + q] << 8 * (q & 3);
       }
     }
-    if constexpr (PBF) {
-      uint32_t b[kEach];
+    if (have > 0) {
+      ms = T.ms[block];
+      vs = T.vs[block];
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const f32x2 a = q & 1 ? __builtin_amdgcn_cvt_pk_f32_fp8(mc[q >> 1], true) : __builtin_amdgcn_cvt_pk_f32_fp8(mc[q >> 1], false);
+      const f32x2 b = q & 1 ? __builtin_amdgcn_cvt_pk_f32_bf8(vc[q >> 1], true) : __builtin_amdgcn_cvt_pk_f32_bf8(vc[q >> 1], false);
+      m.v[2 * q] = a[0] * ms;
+      m.v[2 * q + 1] = a[1] * ms;
+      v.v[2 * q] = b[0] * vs;
+      v.v[2 * q + 1] = b[1] * vs;
+    }
+  }
+  uint32_t mtop = 0, vtop = 0;
+#pragma unroll
+  for (int q = 0; q < kEach; ++q) {
+    const float x = g.v[q] * gs;
+    m.v[q] = m.v[q] * A.b1 + x * A.a1;
+    v.v[q] = v.v[q] * A.b2 + x * x * A.a2;
+    p.v[q] = p.v[q] - p.v[q] * lr_decay - (m.v[q] * lr_c1) / (sqrtf(v.v[q] * inv_c2) + A.eps);
+    if constexpr (S8) {
+      if (q < have) {
+        const uint32_t a = __float_as_uint(m.v[q]) & 0x7fffffffu, b = __float_as_uint(v.v[q]) & 0x7fffffffu;
+        mtop = a > mtop ? a : mtop;
+        vtop = b > vtop ? b : vtop;
+      }
+    }
+  }
+  uint32_t h[kEach];
+  if constexpr (S8 || PBF) {
+#pragma unroll
+    for (int q = 0; q < kEach; ++q) h[q] = mixed(at + q, t);
+  }
+  if constexpr (S8) {
+    const float new_ms = scale_of(block_max(mtop), 1.0f / 448.0f), new_vs = scale_of(block_max(vtop), 1.0f / 57344.0f);
+    const float mi = new_ms > 0.f ? 1.0f / new_ms : new_ms, vi = new_vs > 0.f ? 1.0f / new_vs : new_vs;
+    u32x2 mc = {0, 0}, vc = {0, 0};
+#pragma unroll
+    for (int q = 0; q < kEach; ++q) {
+      const uint32_t sign = __float_as_uint(m.v[q]) >> 24 & 0x80u;
+      mc[q >> 2] |= (code_of<3, -120, 0x7e>(fabsf(m.v[q]) * mi, h[q] & 0xffffu) | sign) << 8 * (q & 3);
+      vc[q >> 2] |= code_of<2, -112, 0x7b>(v.v[q] * vi, h[q] >> 16) << 8 * (q & 3);
+    }
+    if (full) {
+      *reinterpret_cast<u32x2_at1*>(m8 + at) = mc;
+      *reinterpret_cast<u32x2_at1*>(v8 + at) = vc;
+    } else {
 #pragma unroll
       for (int q = 0; q < kEach; ++q) {
-        uint32_t u = h[q] * 0x9E3779B9u;
-        u = (u ^ u >> 16) & 0xffffu;
-        const uint32_t bits = __float_as_uint(p.v[q]);
-        // (a sum past the largest value is infinity; infinity and NaN stay what they are)
-        b[q] = (bits & 0x7f800000u) == 0x7f800000u ? nearest_bf16(p.v[q]) : (bits + u) >> 16;
+        if (q >= have) break;
+        m8[at + q] = (uint8_t)(mc[q >> 2] >> 8 * (q & 3));
+        v8[at + q] = (uint8_t)(vc[q >> 2] >> 8 * (q & 3));
       }
-      if (full) store_bf16(static_cast<uint16_t*>(T.p) + at, b);
+    }
+    if (have > 0 && at % kAdamwBlock == 0) {
+      T.ms[block] = new_ms;
+      T.vs[block] = new_vs;
+    }
+  } else if (full) {
+    store_f32(static_cast<float*>(T.m) + at, m);
+    store_f32(static_cast<float*>(T.v) + at, v);
+  } else {
+#pragma unroll
+    for (int q = 0; q < kEach; ++q) {
+      if (q >= have) break;
+      static_cast<float*>(T.m)[at + q] = m.v[q];
+      static_cast<float*>(T.v)[at + q] = v.v[q];
+    }
+  }
+  if constexpr (PBF) {
+    uint32_t b[kEach];
+#pragma unroll
+    for (int q = 0; q < kEach; ++q) {
+      uint32_t u = h[q] * 0x9E3779B9u;
+      u = (u ^ u >> 16) & 0xffffu;
+      const uint32_t bits = __float_as_uint(p.v[q]);
+      // (a sum past the largest value is infinity; infinity and NaN stay what they are)
+      b[q] = (bits & 0x7f800000u) == 0x7f800000u ? nearest_bf16(p.v[q]) : (bits + u) >> 16;
+    }
+    if (full) store_bf16(static_cast<uint16_t*>(T.p) + at, b);
+    else
+#pragma unroll
+      for (int q = 0; q < kEach; ++q)
+        if (q < have) static_cast<uint16_t*>(T.p)[at + q] = (uint16_t)b[q];
+  } else {
+    if (full) store_f32(static_cast<float*>(T.p) + at, p);
+    else
+#pragma unroll
+      for (int q = 0; q < kEach; ++q)
+        if (q < have) static_cast<float*>(T.p)[at + q] = p.v[q];
+    if (T.copy) {
+      uint32_t b[kEach];
+#pragma unroll
+      for (int q = 0; q < kEach; ++q) b[q] = nearest_bf16(p.v[q]);
+      if (full) store_bf16(T.copy + at, b);
       else
 #pragma unroll
         for (int q = 0; q < kEach; ++q)
-          if (q < have) static_cast<uint16_t*>(T.p)[at + q] = (uint16_t)b[q];
-    } else {
-      if (full) store_f32(static_cast<float*>(T.p) + at, p);
-      else
-#pragma unroll
-        for (int q = 0; q < kEach; ++q)
-          if (q < have) static_cast<float*>(T.p)[at + q] = p.v[q];
-      if (T.copy) {
-        uint32_t b[kEach];
-#pragma unroll
-        for (int q = 0; q < kEach; ++q) b[q] = nearest_bf16(p.v[q]);
-        if (full) store_bf16(T.copy + at, b);
-        else
-#pragma unroll
-          for (int q = 0; q < kEach; ++q)
-            if (q < have) T.copy[at + q] = (uint16_t)b[q];
-      }
+          if (q < have) T.copy[at + q] = (uint16_t)b[q];
     }
   }
 }
@@ -316,8 +313,7 @@ void run(const AdamwArgs& A, bool s8, dim3 grid, hipStream_t s) {
 
 }  // namespace
 
-// Tensors of one launch; first[] is filled in here. A tensor of more values
-// than a launch's 2^31 threads reach does not fit in memory.
+// Tensors of one launch; first[] is filled in here.
 hipError_t launch_adamw(const AdamwArgs& given, bool pbf, bool gbf, bool s8, hipStream_t s) {
   AdamwArgs A = given;
   int64_t blocks = 0;

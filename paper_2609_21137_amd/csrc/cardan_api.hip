@@ -1147,7 +1147,7 @@ int cardan_adamw_step(const cardan_adamw* config, int32_t count, const cardan_ad
   const uintptr_t ss = s8 ? 1 : 4;
   for (int32_t i = 0; i < count; ++i) {
     const cardan_adamw_tensor& T = tensors[i];
-    if (T.n < 0 || T.n > (int64_t)1 << 36) return fail(CARDAN_ERR_BAD_SHAPE, "tensor %d has %lld values", i, (long long)T.n);
+    if (T.n < 0 || T.n > kAdamwMost) return fail(CARDAN_ERR_BAD_SHAPE, "tensor %d has %lld values", i, (long long)T.n);
     if (T.n == 0) continue;
     START(T.param, "param", pbf ? 2 : 4);
     START(T.grad, "grad", gbf ? 2 : 4);
@@ -1181,8 +1181,10 @@ int cardan_adamw_step(const cardan_adamw* config, int32_t count, const cardan_ad
   A.step_device = c.step_device;
   A.grad_scale = c.grad_scale;
   for (int32_t i = 0; i < count;) {
+    int64_t values = 0;
     for (A.count = 0; i < count && A.count < kAdamwTensors; ++i) {
       const cardan_adamw_tensor& T = tensors[i];
+      if ((values += T.n + kAdamwWork) > kAdamwMost + kAdamwWork && A.count) break;
       if (T.n > 0) A.t[A.count++] = AdamwTensor{T.param, T.grad, T.m, T.v, T.m_scale, T.v_scale, T.copy, T.n};
     }
     const hipError_t e = A.count ? launch_adamw(A, pbf, gbf, s8, stream) : hipSuccess;

@@ -60,6 +60,8 @@ struct RowsArgs {
 };
 
 constexpr int kAdamwBlock = 256;  // values that share a scale
+constexpr int kAdamwWork = 2048;  // values of a workgroup
+constexpr int64_t kAdamwMost = (int64_t)1 << 34;  // values of a launch: its threads are counted in 32 bits
 constexpr int kAdamwTensors = 40; // tensors of one launch (their table is a kernel argument)
 
 struct AdamwTensor {

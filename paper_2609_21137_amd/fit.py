@@ -399,9 +399,17 @@ class TrainedLayer:
     codes and router stay fixed. ``forward`` runs rows of any number and keeps
     what ``backward`` needs; ``backward`` returns the gradient of every factor.
     One basis shared by gate and up (``U_up is U_gate``) is one factor,
-    ``U_up``."""
+    ``U_up``.
 
-    def __init__(self, layer: dict, k: int, d: int, act: str = "silu_glu", device="cuda"):
+    ``routing`` (a dict of ``cardan.route_rows``'s arguments: score, bias,
+    groups, ...) routes by it instead of by the softmax over the kept logits,
+    and the rows go to their experts and back by ``cardan.dispatch_rows`` and
+    ``cardan.combine_rows``. ``train_router`` makes the router a factor, too
+    (``router_w`` and, where the layer has one, ``router_bias``); its gradient
+    is that of the experts' weights."""
+
+    def __init__(self, layer: dict, k: int, d: int, act: str = "silu_glu", device="cuda", routing: dict | None = None,
+                 train_router: bool = False):
         import torch
 
         from . import cardan
@@ -417,6 +425,12 @@ class TrainedLayer:
         self.router_w = cardan.bf16_tensor(layer["router_w"], self.device)
         bias = layer.get("router_bias")
         self.router_bias = None if bias is None else torch.as_tensor(bias, device=self.device)
+        self.routing = {} if train_router and routing is None else routing
+        self.train_router = train_router
+        if train_router:
+            self.factors["router_w"] = self.router_w.float()
+            if bias is not None:
+                self.factors["router_bias"] = self.router_bias.float()
         self.codes, self._word_sums = {}, {}
         for p in self._projections() + ["down"]:
             J = torch.as_tensor(np.ascontiguousarray(layer["codes_" + p])).to(self.device).long()
@@ -445,13 +459,25 @@ class TrainedLayer:
             W = W + torch.matmul(self.factors[left], self.factors[right])
         return W.to(torch.bfloat16)
 
+    def _logits(self, x):
+        """Float64 logits of the router as it is stored (bf16 weights, float32 bias)."""
+        import torch
+        w = self.factors["router_w"].to(torch.bfloat16) if self.train_router else self.router_w
+        bias = self.factors.get("router_bias", self.router_bias)
+        logits = x.double() @ w.double()
+        return logits if bias is None else logits + bias.double()
+
     def route(self, x):
         """Top-k experts (descending logit, ties to the lower index) and their
-        softmax affinities, from float64 logits."""
+        softmax affinities, from float64 logits; with ``routing`` the experts and
+        weights that it says."""
         import torch
-        logits = x.double() @ self.router_w.double()
-        if self.router_bias is not None:
-            logits = logits + self.router_bias.double()
+
+        from . import cardan
+        logits = self._logits(x)
+        if self.routing is not None:
+            idx, a, _, _ = cardan.route_rows(logits, self.k, places=False, **self.routing)
+            return idx.long(), a
         val, idx = torch.sort(logits, dim=1, descending=True, stable=True)
         return idx[:, :self.k], torch.softmax(val[:, :self.k], 1).float()
 
@@ -462,6 +488,8 @@ class TrainedLayer:
         from . import cardan
         N, H = x.shape
         E = self.codes["up"].shape[0]
+        if self.routing is not None:
+            return self._forward_routed(x)
         idx, a = self.route(x)
         order = torch.argsort(idx.reshape(-1), stable=True)      # rows of an expert together
         rows, a = order // self.k, a.reshape(-1)[order]
@@ -477,6 +505,34 @@ class TrainedLayer:
         self._kept = (xe, rows, a, offsets, W, saved)
         return part.sum(1)
 
+    def _forward_routed(self, x):
+        import torch
+
+        from . import cardan
+        logits = self._logits(x)
+        idx, a, place, offsets = cardan.route_rows(logits, self.k, **self.routing)
+        W = {p: self.dense(p) for p in self._projections() + ["down"]}
+        xe = cardan.dispatch_rows(x.contiguous(), place)
+        ye, saved = cardan.ffn_forward(xe, W.get("gate"), W["up"], W["down"], offsets=offsets, act=self.act, save=True)
+        self._kept = (xe, (x, logits, idx, place, ye), a, offsets, W, saved)
+        return cardan.combine_rows(ye, place, a, dtype=torch.float32)
+
+    def _backward_routed(self, dy):
+        """The experts' gradient rows, and the router's gradients."""
+        import torch
+
+        from . import cardan
+        _, (x, logits, idx, place, ye), a, _, _, _ = self._kept
+        dye, da = cardan.combine_rows_backward(dy.float().contiguous(), ye, place, a, need_dweight=self.train_router)
+        if not self.train_router:
+            return dye, {}
+        how = {n: v for n, v in self.routing.items() if n != "bias"}
+        dz = cardan.route_rows_backward(logits, idx, da, **how)
+        grads = {"router_w": torch.mm(x.double().t(), dz).float()}
+        if "router_bias" in self.factors:
+            grads["router_bias"] = dz.sum(0).float()
+        return dye, grads
+
     def backward(self, dy):
         """Gradients of the factors for the gradient dy [N, H] of the last
         ``forward``'s output."""
@@ -486,10 +542,13 @@ class TrainedLayer:
         if self._kept is None:
             raise RuntimeError("backward needs a forward pass")
         xe, rows, a, offsets, W, saved = self._kept
-        dye = (dy.float()[rows] * a[:, None]).to(torch.bfloat16)  # (what the block takes)
+        grads = {}
+        if self.routing is not None:
+            dye, grads = self._backward_routed(dy)
+        else:
+            dye = (dy.float()[rows] * a[:, None]).to(torch.bfloat16)  # (what the block takes)
         _, dg, du, dd = cardan.ffn_backward(dye, xe, W.get("gate"), W["up"], W["down"], saved, offsets=offsets,
                                             act=self.act, need_dx=False)
-        grads = {}
         for p, dW in (("gate", dg), ("up", du), ("down", dd)):
             if dW is None:
                 continue
@@ -513,7 +572,8 @@ class TrainedLayer:
         """The layer dict ``like`` with these factors, in storage formats."""
         out = dict(like)
         for name, t in self.factors.items():
-            out[name] = to_bf16_bits(t.detach().cpu().numpy())
+            host = t.detach().cpu().numpy()
+            out[name] = host if name == "router_bias" else to_bf16_bits(host)
         if self.shared:
             out["U_gate"] = out["U_up"]
         return out
@@ -542,23 +602,40 @@ def distill_step(student: TrainedLayer, x, head, teacher, ids, labels=None, temp
 
 def distill_layer(layer: dict, X, head, teacher, ids, k: int, d: int, act: str = "silu_glu", labels=None,
                   temperature: float = 1.0, ce_weight: float = 0.0, steps: int = 100, rows: int = 4096,
-                  lr: float = 1e-4, seed: int = 0, device="cuda"):
+                  lr: float = 1e-4, seed: int = 0, device="cuda", optimizer: str = "adam", weight_decay: float = 0.0,
+                  routing: dict | None = None, train_router: bool = False):
     """Distillation of a fitted layer (Sec. 3.3, Eq. (3)): ``steps`` Adam steps
     on its code books, bases and coefficients over random batches of ``rows`` of
-    the rows ``X`` [N, H] (bf16) with a teacher's kept logits. Returns ``(layer
-    dict in storage formats, mean loss [steps, 2])``."""
+    the rows ``X`` [N, H] (bf16) with a teacher's kept logits. ``optimizer`` is
+    ``"adam"`` (torch's), ``"adamw"`` or ``"adamw8"`` (``cardan.adamw_step`` with
+    float32 or 8-bit moments, and ``weight_decay``); ``routing`` and
+    ``train_router`` as of ``TrainedLayer``. Returns ``(layer dict in storage
+    formats, mean loss [steps, 2])``."""
     import torch
-    student = TrainedLayer(layer, k, d, act, device)
+
+    from . import cardan
+    if optimizer not in ("adam", "adamw", "adamw8"):
+        raise ValueError(f"unknown optimizer {optimizer!r}")
+    if optimizer == "adam" and weight_decay:
+        raise ValueError("weight_decay needs adamw or adamw8")
+    student = TrainedLayer(layer, k, d, act, device, routing, train_router)
     params = list(student.factors.values())
-    opt = torch.optim.Adam(params, lr=lr)
+    if optimizer == "adam":
+        opt = torch.optim.Adam(params, lr=lr)
+    else:
+        moments = [cardan.adamw_state(p, 8 if optimizer == "adamw8" else 32) for p in params]
     gen = torch.Generator().manual_seed(seed)
     N, history = X.shape[0], []
-    for _ in range(steps):
+    for step in range(steps):
         at = torch.randperm(N, generator=gen)[:rows].to(X.device)
         loss, grads = distill_step(student, X[at].contiguous(), head, teacher[at].contiguous(), ids[at].contiguous(),
                                    None if labels is None else labels[at].contiguous(), temperature, ce_weight)
-        for name, t in student.factors.items():
-            t.grad = grads[name]
-        opt.step()
+        if optimizer == "adam":
+            for name, t in student.factors.items():
+                t.grad = grads[name]
+            opt.step()
+        else:
+            cardan.adamw_step(params, [grads[name].contiguous() for name in student.factors], moments, step + 1, lr,
+                              weight_decay=weight_decay)
         history.append(loss.mean(0))
     return student.layer(layer), torch.stack(history).cpu().numpy() if history else np.zeros((0, 2))
