@@ -999,9 +999,10 @@ int cardan_route_rows_workspace_bytes(const cardan_routing* routing, int32_t N, 
   int rc = check_routing(routing, N);
   if (rc) return rc;
   if (!out) return fail(CARDAN_ERR_NULL_PTR, "out is NULL");
-  // counts of every block of rows, and their totals
-  const int64_t blocks = std::min<int64_t>(kRouteBlocks, ((int64_t)N + 3) / 4);
-  *out = N <= kRouteSmall ? 0 : align256((size_t)(blocks + 1) * routing->E * 4);
+  // counts of every block of rows (of four at least)
+  const int64_t few = std::min<int64_t>(kRouteBlocks, ((int64_t)N + 3) / 4);
+  const int64_t blocks = std::max<int64_t>(few, ((int64_t)N + kBlockRows - 1) / kBlockRows);
+  *out = N <= kRouteSmall ? 0 : align256((size_t)blocks * count_row(routing->E) * 2);
   return CARDAN_OK;
 }
 
@@ -1028,7 +1029,7 @@ int cardan_route_rows(const cardan_routing* routing, int32_t N, int32_t logits_t
   A.weight = weight;
   A.place = place;
   A.offsets = offsets;
-  A.count = static_cast<int32_t*>(ws);
+  A.count = static_cast<uint16_t*>(ws);
   const hipError_t e = launch_route(A, stream);
   return e == hipSuccess ? CARDAN_OK : hip_fail(e, "routing launch");
 }

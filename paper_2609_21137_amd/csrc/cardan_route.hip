@@ -22,7 +22,6 @@ namespace cardan {
 namespace {
 
 constexpr int kMostK = 32;
-constexpr int kSumBlocks = 64;  // blocks whose counts are summed without a launch of their own
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ float widen(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
@@ -615,9 +614,12 @@ __device__ __forceinline__ void place_slots(int n, int E, int* next, F slot, int
   constexpr int NW = NT / 64;
   const int chunks = (n + 63) / 64, per = (chunks + NW - 1) / NW;
   int* mine = next + wave * E;
-  for (int c = wave * per; c < std::min(chunks, (wave + 1) * per); ++c) {
+  const int end = std::min(chunks, (wave + 1) * per);
+  int ahead = wave * per < end && wave * per * 64 + lane < n ? slot(wave * per * 64 + lane) : -1;
+  for (int c = wave * per; c < end; ++c) {
     const int i = c * 64 + lane;
-    const int e = i < n ? slot(i) : -1;
+    const int e = ahead;
+    ahead = c + 1 < end && i + 64 < n ? slot(i + 64) : -1;
     // the lanes with the same expert
     uint64_t same = __ballot(e >= 0);
     for (int bit = 0; (E - 1) >> bit; ++bit) {
@@ -645,6 +647,7 @@ __device__ __forceinline__ void count_slots(int n, int E, int* next, F slot) {
   for (int i = threadIdx.x; i < NW * E; i += NT) next[i] = 0;
   __syncthreads();
   const int chunks = (n + 63) / 64, per = (chunks + NW - 1) / NW;
+#pragma unroll 4
   for (int c = wave * per; c < std::min(chunks, (wave + 1) * per); ++c) {
     const int i = c * 64 + lane;
     const int e = i < n ? slot(i) : -1;
@@ -654,12 +657,15 @@ __device__ __forceinline__ void count_slots(int n, int E, int* next, F slot) {
 }
 template <int NT>
 __device__ __forceinline__ void start_slots(int E, int* next, const int* base) {
+  constexpr int NW = NT / 64;
   for (int e = threadIdx.x; e < E; e += NT) {
-    int at = base[e];
-    for (int w = 0; w < NT / 64; ++w) {
-      const int c = next[w * E + e];
+    int at = base[e], c[NW];
+#pragma unroll
+    for (int w = 0; w < NW; ++w) c[w] = next[w * E + e];
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
       next[w * E + e] = at;
-      at += c;
+      at += c[w];
     }
   }
   __syncthreads();
@@ -721,88 +727,55 @@ __global__ __launch_bounds__(NT) void k_route_rows(const RouteArgs A) {
     start_slots<NT>(A.E, next, count);
     place_slots<NT>(n, A.E, next, slot, A.place);
   } else {
-    for (int i = tid; i < A.E; i += NT) A.count[(int64_t)blockIdx.x * A.E + i] = count[i];
+    for (int i = tid; i < A.E; i += NT) A.count[(int64_t)blockIdx.x * count_row(A.E) + i] = (uint16_t)count[i];
   }
 }
 
-// Counts of the blocks -> sums over the blocks before, and totals behind them:
-// a workgroup 16 experts, a thread up to 16 blocks of one, in registers. (With
-// a lane an expert and a wave 64 blocks, read twice, 24 us at 1024 blocks.)
-__global__ __launch_bounds__(1024) void k_route_scan(const RouteArgs A) {
-  constexpr int PER = kRouteBlocks / 64;
-  __shared__ int part[16][65];
-  const int tid = threadIdx.x, col = tid & 15, slice = tid >> 4, e = blockIdx.x * 16 + col;
-  const int per = (A.blocks + 63) / 64, lo = slice * per;
-  int c[PER], sum = 0;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) c[i] = i < per && lo + i < A.blocks && e < A.E ? A.count[(int64_t)(lo + i) * A.E + e] : 0;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) sum += c[i];
-  part[col][slice] = sum;
-  __syncthreads();
-  {
-    const int lane = tid & 63, wave = tid >> 6;  // a wave an expert, a lane a slice
-    const int own = part[wave][lane];
-    int up = own;
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) {
-      const int o = __shfl_up(up, s);
-      if (lane >= s) up += o;
-    }
-    part[wave][lane] = up - own;
-    if (lane == 63 && blockIdx.x * 16 + wave < (unsigned)A.E)
-      A.count[(int64_t)A.blocks * A.E + blockIdx.x * 16 + wave] = up;
-  }
-  __syncthreads();
-  int at = part[col][slice];
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    if (i < per && lo + i < A.blocks && e < A.E) A.count[(int64_t)(lo + i) * A.E + e] = at;
-    at += c[i];
-  }
-}
+constexpr int kPlaceThreads = 1024;
 
-// Places of a block's slots. SUM: few blocks, whose counts every workgroup sums
-// by itself; else k_route_scan has.
-template <bool SUM>
-__global__ __launch_bounds__(256) void k_route_place(const RouteArgs A) {
-  constexpr int NT = 256;
+// Places of a block's slots: after the slots of the experts before, of the same
+// expert in the blocks before, and of the waves before. Every workgroup sums
+// the blocks' counts by itself; a launch of its own for that took 5 us, this
+// takes one or two with the 256 blocks of large calls.
+__global__ __launch_bounds__(kPlaceThreads) void k_route_place(const RouteArgs A) {
+  constexpr int NT = kPlaceThreads;
   extern __shared__ __align__(16) unsigned char lds[];
-  int* count = reinterpret_cast<int*>(lds);  // [E + 1]
-  int *next = count + A.E + 1, *part = next + NT / 64 * A.E;
+  int* count = reinterpret_cast<int*>(lds);  // [E + 1], then those of the blocks before [E]
+  int *before = count + A.E + 1, *next = before + A.E, *part = next + NT / 64 * A.E;
   const int tid = threadIdx.x, b = blockIdx.x;
   const int64_t first = (int64_t)b * A.block_rows * A.k;
   const int n = (int)std::min((int64_t)A.block_rows * A.k, (int64_t)A.N * A.k - first);
   const int32_t* idx = A.idx + first;
   const auto slot = [&](int i) { return idx[i]; };
-  int before[1024 / NT];
-#pragma unroll
-  for (int q = 0; q < 1024 / NT; ++q) {
-    const int e = q * NT + tid;
-    if (e >= A.E) break;
-    if constexpr (SUM) {
-      int total = 0, sum = 0;
+  for (int e = tid; e < 2 * A.E + 1; e += NT) count[e] = 0;
+  __syncthreads();
+  // a thread eight experts and a slice of the blocks
+  const int cols = (A.E + 7) / 8, width = cols > 64 ? 128 : cols > 32 ? 64 : cols > 16 ? 32 : cols > 8 ? 16 : 8;
+  if (const int col = tid % width; col < cols) {
+    uint32_t total[8] = {}, sum[8] = {};
 #pragma unroll 8
-      for (int c = 0; c < A.blocks; ++c) {
-        const int v = A.count[c * A.E + e];
-        total += v;
-        sum += c < b ? v : 0;
+    for (int c = tid / width; c < A.blocks; c += NT / width) {
+      const u32x4 v = *reinterpret_cast<const u32x4*>(A.count + (int64_t)c * count_row(A.E) + col * 8);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const uint32_t x = v[q >> 1] >> 16 * (q & 1) & 0xffffu;
+        total[q] += x;
+        sum[q] += c < b ? x : 0u;
       }
-      count[e] = total;
-      before[q] = sum;
-    } else {
-      count[e] = A.count[(int64_t)A.blocks * A.E + e];
-      before[q] = A.count[(int64_t)b * A.E + e];
     }
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      if (col * 8 + q < A.E) {
+        atomicAdd(&count[col * 8 + q], (int)total[q]);
+        atomicAdd(&before[col * 8 + q], (int)sum[q]);
+      }
   }
   count_slots<NT>(n, A.E, next, slot);
   scan_experts<NT>(count, A.E, part);
   if (b == 0)
     for (int e = tid; e <= A.E; e += NT) A.offsets[e] = count[e];
   __syncthreads();
-#pragma unroll
-  for (int q = 0; q < 1024 / NT; ++q)
-    if (q * NT + tid < A.E) count[q * NT + tid] += before[q];
+  for (int e = tid; e < A.E; e += NT) count[e] += before[e];
   __syncthreads();
   start_slots<NT>(A.E, next, count);
   place_slots<NT>(n, A.E, next, slot, A.place + first);
@@ -904,6 +877,25 @@ __global__ __launch_bounds__(256) void k_route_backward(const RouteArgs A) {
   }
 }
 
+// Threads of a workgroup: 256 while the blocks of so many rows are no more than
+// kRouteBlocks, else as many as its registers and LDS allow, so that large
+// calls fill the chip with few blocks.
+template <class L, class V, int LPR, int EPL, int NT>
+hipError_t run_blocks(RouteArgs& A, hipStream_t s) {
+  constexpr int ROWS = NT / LPR;
+  const int64_t per = ((int64_t)A.N + kRouteBlocks - 1) / kRouteBlocks;
+  A.block_rows = (int32_t)std::min<int64_t>(kBlockRows, std::max<int64_t>(ROWS, (per + ROWS - 1) / ROWS * ROWS));
+  A.blocks = (int32_t)(((int64_t)A.N + A.block_rows - 1) / A.block_rows);
+  const size_t lds = (size_t)ROWS * A.row_lds + 4 * ((size_t)A.E + 1);
+  k_route_rows<L, V, LPR, EPL, NT, false><<<dim3((unsigned)A.blocks), dim3(NT), lds, s>>>(A);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !A.place) return e;
+  constexpr int kWaves = kPlaceThreads / 64;
+  const size_t lds2 = 4 * ((size_t)A.E + 1 + A.E + kWaves * A.E + kWaves);
+  k_route_place<<<dim3((unsigned)A.blocks), dim3(kPlaceThreads), lds2, s>>>(A);
+  return hipGetLastError();
+}
+
 template <class L, class V, int LPR, int EPL>
 hipError_t run_rows(const RouteArgs& given, hipStream_t s) {
   RouteArgs A = given;
@@ -919,20 +911,8 @@ hipError_t run_rows(const RouteArgs& given, hipStream_t s) {
     k_route_rows<L, V, LPR, EPL, NT, true><<<dim3(1), dim3(NT), lds, s>>>(A);
     return hipGetLastError();
   }
-  constexpr int NT = 256, ROWS = NT / LPR;
-  const size_t lds = (size_t)ROWS * A.row_lds + 4 * ((size_t)A.E + 1);
-  k_route_rows<L, V, LPR, EPL, NT, false><<<dim3((unsigned)A.blocks), dim3(NT), lds, s>>>(A);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !A.place) return e;
-  const size_t lds2 = 4 * ((size_t)A.E + 1 + 4 * A.E + 4);
-  if (A.blocks <= kSumBlocks) {
-    k_route_place<true><<<dim3((unsigned)A.blocks), dim3(256), lds2, s>>>(A);
-    return hipGetLastError();
-  }
-  k_route_scan<<<dim3((unsigned)((A.E + 15) / 16)), dim3(1024), 0, s>>>(A);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  k_route_place<false><<<dim3((unsigned)A.blocks), dim3(256), lds2, s>>>(A);
-  return hipGetLastError();
+  if (A.N <= kRouteBlocks * (256 / LPR)) return run_blocks<L, V, LPR, EPL, 256>(A, s);
+  return run_blocks<L, V, LPR, EPL, LPR == 8 && sizeof(V) == 4 ? 1024 : 512>(A, s);
 }
 
 template <class L, class V>
@@ -965,25 +945,14 @@ hipError_t back_width(const RouteArgs& A, hipStream_t s) {
 
 }  // namespace
 
-// Lanes of a row: its experts stay in at most 16 registers a lane. Rows of a
-// block: a whole number of passes of its 256 threads.
-void plan_route(RouteArgs* A) {
-  const int rows = A->E <= 128 ? 32 : A->E <= 256 ? 16 : 4;  // of 256 threads at a time
-  const int64_t per = ((int64_t)A->N + kRouteBlocks - 1) / kRouteBlocks;
-  A->block_rows = (int32_t)std::max<int64_t>(rows, (per + rows - 1) / rows * rows);
-  A->blocks = (int32_t)(((int64_t)A->N + A->block_rows - 1) / A->block_rows);
-}
-
 hipError_t launch_route(const RouteArgs& A, hipStream_t s) {
   if (A.N == 0) {
     if (A.offsets) k_route_none<<<dim3(1), dim3(256), 0, s>>>(A.offsets, A.E);
     return hipGetLastError();
   }
-  RouteArgs B = A;
-  plan_route(&B);
-  if (A.type == LOGIT_F64) return run_width<double, double>(B, s);
-  if (A.type == LOGIT_F32) return A.by_score ? run_width<float, double>(B, s) : run_width<float, float>(B, s);
-  return A.by_score ? run_width<uint16_t, double>(B, s) : run_width<uint16_t, float>(B, s);
+  if (A.type == LOGIT_F64) return run_width<double, double>(A, s);
+  if (A.type == LOGIT_F32) return A.by_score ? run_width<float, double>(A, s) : run_width<float, float>(A, s);
+  return A.by_score ? run_width<uint16_t, double>(A, s) : run_width<uint16_t, float>(A, s);
 }
 
 hipError_t launch_route_backward(const RouteArgs& A, hipStream_t s) {

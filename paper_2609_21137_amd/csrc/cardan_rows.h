@@ -16,8 +16,10 @@ namespace cardan {
 enum LogitType { LOGIT_BF16 = 0, LOGIT_F32 = 1, LOGIT_F64 = 2 };
 
 // The blocks of rows that count their experts' selections before the rows'
-// places are known: at most this many, so that their prefix sums stay short.
-constexpr int kRouteBlocks = 1024;
+// places are known: this many at most, so that their sums stay short, unless a
+// block had more rows than 16 bits count (a row chooses an expert once).
+constexpr int kRouteBlocks = 256, kBlockRows = 1 << 15;
+__host__ __device__ inline int count_row(int E) { return (E + 7) / 8 * 8; }
 // Rows of one call that a single workgroup routes and places by itself.
 constexpr int kRouteSmall = 64;
 
@@ -37,7 +39,7 @@ struct RouteArgs {
   float* weight;                           // [N][k]
   int32_t* place;                          // [N][k] or nullptr, -1: none
   int32_t* offsets;                        // [E + 1] with place
-  int32_t* count;                          // [blocks][E] (workspace), then totals [E]
+  uint16_t* count;                         // [blocks][count_row(E)] (workspace)
   int32_t block_rows, blocks;
   Divisor by_each;                         // division by `each`
   int32_t group_lanes, row_lds, slots;

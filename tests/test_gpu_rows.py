@@ -152,6 +152,16 @@ def test_arrays_past_31_bits(C):
     assert ((dw.double() - ref[:, None]).abs() <= (H / 64 + 8) * EPS * ref[:, None]).all()
 
 
+@pytest.mark.parametrize("H", [4096, 4097])
+def test_arrays_that_the_caches_do_not_keep(C, H):
+    N, k = 6500, 4
+    x, ye, place, w = _inputs(N, k, H, N * k, True, 8)
+    assert ye.numel() * 2 > 192 << 20
+    dy = torch.randn((N, H), device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).bfloat16()
+    _check(C, x, ye, place, w, dy)
+    torch.cuda.empty_cache()
+
+
 def test_many_rows(C):
     """More rows than one launch has in its second dimension."""
     N, k, H = 70000, 2, 8

@@ -58,11 +58,12 @@ def test_route_workspace(C):
         assert lib.cardan_route_rows_workspace_bytes(ctypes.byref(r), N, ctypes.byref(n)) == code
     sizes = [C.route_rows_workspace_bytes(N, 64, 4) for N in (0, 1, 64, 65, 1000, 4096, 100000, (1 << 29) - 1)]
     assert sizes == sorted(sizes) and sizes[0] == 0
-    # blocks of 16 rows (4 above 256 experts), at most 1024 of them, and the totals
-    for E, rows in ((64, 16), (300, 4)):
-        for N in (65, 66, 1000, 5000, 1 << 20):
-            blocks = min(1024, -(-N // rows))
-            assert C.route_rows_workspace_bytes(N, E, 4) >= (blocks + 1) * E * 4
+    # counts of 16 bits for blocks of 32 rows (16 above 128 experts, 4 above 256), of at most 256
+    # blocks, or more where a block would have more than 2^15 rows
+    for E, rows in ((64, 32), (200, 16), (301, 4)):
+        for N in (65, 66, 1000, 5000, 1 << 20, 1 << 24, (1 << 29) - 1):
+            blocks = max(min(256, -(-N // rows)), -(-N >> 15))
+            assert C.route_rows_workspace_bytes(N, E, 4) >= blocks * E * 2
 
 
 def _route(C, N=100, kind=1, logits=FAKE, ld=64, bias=None, idx=FAKE, w=FAKE, place=FAKE, off=FAKE, ws=FAKE, nbytes=None, **kw):
