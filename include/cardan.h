@@ -505,7 +505,8 @@ typedef struct {
  * of a value's place in its tensor and t (right in the mean; the same arguments
  * give the same result). Copies are rounded to nearest. A gradient that is not
  * finite goes on into its weight and moments; with 8-bit moments into those of
- * its 256 values. With step_device and lr_device a captured call follows both.
+ * its 256 values. eps = 0 gives NaN where a gradient has always been 0. With
+ * step_device and lr_device a captured call follows both.
  * Tensors must not overlap one another. */
 int cardan_adamw_step(const cardan_adamw* config, int32_t count, const cardan_adamw_tensor* tensors,
                       hipStream_t stream);

@@ -931,6 +931,9 @@ def adamw_step(params, grads, states, step, lr, betas=(0.9, 0.999), eps: float =
             rows += (0, 0)
         rows += (0 if c is None else _arg(c, kept, "copies", shape, dev), n)
     table = (ctypes.c_int64 * len(rows))(*rows)
+    starts = [a for a, n in zip(rows[::8], rows[7::8]) if n]
+    if len(set(starts)) != len(starts):
+        raise ValueError("a tensor is given twice")
     conf = Adamw(_TYPES[pt], _TYPES[gt], 32 if kinds == 2 else 8, 0, 0.0, betas[0], betas[1], eps, weight_decay)
     if isinstance(step, torch.Tensor):
         conf.step_device = _scalar(step, torch.int32, "step", dev)

@@ -573,8 +573,7 @@ __device__ __forceinline__ void route_row(const RouteArgs& A, int n, int lane, c
   }
 }
 
-// Exclusive sums of count[E] in place (LDS), all NT threads; returns nothing,
-// total behind the last (count[E]).
+// Exclusive sums of count[E] in place (LDS) by all NT threads, the total in count[E].
 template <int NT>
 __device__ __forceinline__ void scan_experts(int* count, int E, int* part) {
   constexpr int EPT = (1024 + NT - 1) / NT, NW = NT / 64;
@@ -896,7 +895,7 @@ hipError_t run_blocks(RouteArgs& A, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <class L, class V, int LPR, int EPL>
+template <class L, class V, int LPR, int EPL, bool ONE>
 hipError_t run_rows(const RouteArgs& given, hipStream_t s) {
   RouteArgs A = given;
   A.slots = (A.k + kSpare + 1) / 2 * 2;
@@ -905,24 +904,38 @@ hipError_t run_rows(const RouteArgs& given, hipStream_t s) {
   A.group_lanes = -1;
   for (int lg = 0; 1 << lg <= 16; ++lg)
     if (A.each == EPL << lg) A.group_lanes = lg;
-  if (A.N <= kRouteSmall) {
+  if constexpr (ONE) {
     constexpr int NT = EPL <= 8 && LPR == 16 ? 512 : 256, ROWS = NT / LPR;  // (their LDS is below 160 KiB)
     const size_t lds = (size_t)ROWS * A.row_lds + 4 * ((size_t)A.N * A.k + A.E + 1 + NT / 64 * A.E + NT / 64);
     k_route_rows<L, V, LPR, EPL, NT, true><<<dim3(1), dim3(NT), lds, s>>>(A);
     return hipGetLastError();
+  } else {
+    if (A.N <= kRouteBlocks * (256 / LPR)) return run_blocks<L, V, LPR, EPL, 256>(A, s);
+    if constexpr (LPR == 8 && sizeof(V) == 4) {
+      if (A.groups == 1) return run_blocks<L, V, LPR, EPL, 1024>(A, s);  // (with groups' values: up to 210 KiB of LDS)
+    }
+    return run_blocks<L, V, LPR, EPL, 512>(A, s);
   }
-  if (A.N <= kRouteBlocks * (256 / LPR)) return run_blocks<L, V, LPR, EPL, 256>(A, s);
-  return run_blocks<L, V, LPR, EPL, LPR == 8 && sizeof(V) == 4 ? 1024 : 512>(A, s);
 }
 
+// Lanes of a row: 8 or 16 of up to 16 experts each, so that a reduction takes
+// three or four steps and serves 8 or 4 rows of a wave (128 experts with 16
+// lanes of 8: 20.3 us for 65536 rows, with 8 of 16: 16.2); a few rows, whose
+// latency counts, have more lanes.
 template <class L, class V>
 hipError_t run_width(const RouteArgs& A, hipStream_t s) {
-  const bool one = A.N <= kRouteSmall;
-  if (A.E <= 64) return one ? run_rows<L, V, 16, 4>(A, s) : run_rows<L, V, 8, 8>(A, s);
-  if (A.E <= 128) return one ? run_rows<L, V, 16, 8>(A, s) : run_rows<L, V, 8, 16>(A, s);
-  if (A.E <= 256) return run_rows<L, V, 16, 16>(A, s);
-  if (A.E <= 512) return run_rows<L, V, 64, 8>(A, s);
-  return run_rows<L, V, 64, 16>(A, s);
+  if (A.N <= kRouteSmall) {
+    if (A.E <= 64) return run_rows<L, V, 16, 4, true>(A, s);
+    if (A.E <= 128) return run_rows<L, V, 16, 8, true>(A, s);
+    if (A.E <= 256) return run_rows<L, V, 16, 16, true>(A, s);
+    if (A.E <= 512) return run_rows<L, V, 64, 8, true>(A, s);
+    return run_rows<L, V, 64, 16, true>(A, s);
+  }
+  if (A.E <= 64) return run_rows<L, V, 8, 8, false>(A, s);
+  if (A.E <= 128) return run_rows<L, V, 8, 16, false>(A, s);
+  if (A.E <= 256) return run_rows<L, V, 16, 16, false>(A, s);
+  if (A.E <= 512) return run_rows<L, V, 64, 8, false>(A, s);
+  return run_rows<L, V, 64, 16, false>(A, s);
 }
 
 template <class L, int LPR, int EPL>

@@ -165,6 +165,13 @@ def test_shapes_and_gradients_that_are_missing(C):
     C.adamw_step(params, [None] * 3, states, 2, 1e-2)
 
 
+def test_the_same_tensor_twice_is_refused(C):
+    p, g = torch.ones(10, device="cuda"), torch.ones(10, device="cuda")
+    with pytest.raises(ValueError):
+        C.adamw_step([p, p], [g, g], [C.adamw_state(p), C.adamw_state(p)], 1, 1e-3)
+    assert (p == 1).all()
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_many_tensors(C, bits):
     """More tensors than a launch's table holds, each as if it were alone."""

@@ -147,6 +147,23 @@ def test_forms(C, E, o, biased, dtype):
         _check(C, _logits(N, E, dtype, N), _bias(E) if biased else None, o)
 
 
+@pytest.mark.parametrize("biased", [False, True])
+@pytest.mark.parametrize("E,o", FORMS + [(128, _opts(32, "softmax", True, 1.0, 4, 2, 1)), (64, _opts(32, "sigmoid", True, 1.0, 64, 40, 1))])
+def test_forms_of_many_rows(C, E, o, biased):
+    """More rows than blocks of 256 threads take; the rows are those of a call of 500, again and again."""
+    N = 8200
+    z, bias = _logits(500, E, F32, E), _bias(E) if biased else None
+    few = _check(C, z, bias, o)
+    for dtype in (F32, BF, F64):
+        if dtype is not F32:
+            z = _logits(500, E, dtype, E)
+            few = C.route_rows(z, bias=bias, **o)
+        at = torch.arange(N, device="cuda") % 500
+        idx, w, place, offsets = C.route_rows(z[at], bias=bias, **o)
+        assert torch.equal(idx, few[0][at]) and torch.equal(w, few[1][at])
+        _check_places(idx, place, offsets, E)
+
+
 @pytest.mark.parametrize("N", [1, 16, 63, 1024, 1025, 16385, 70001])
 def test_rows(C, N):
     """Rows of one workgroup, of a block, and of blocks of more rows than one pass."""
