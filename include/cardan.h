@@ -464,7 +464,8 @@ int cardan_combine_rows(int32_t N, int32_t k, int32_t H, int32_t M, const cardan
 /* Gradients of cardan_combine_rows for dy [N][H] (bf16 or float32):
  *   dye[place[n][j]] = weight[n][j] * dy[n]   (bf16; rows without a place stay)
  *   dweight[n][j] = <dy[n], ye[place[n][j]]>  (float32; 0 without a place)
- * dye or dweight may be NULL (not computed; ye is read for dweight alone). */
+ * dye or dweight may be NULL (not computed; ye is read for dweight alone). A
+ * row of dye named twice gets one of the two. */
 int cardan_combine_rows_backward(int32_t N, int32_t k, int32_t H, int32_t M, int32_t dy_type, const void* dy,
                                  const cardan_bf16* ye, const int32_t* place, const float* weight, cardan_bf16* dye,
                                  float* dweight, hipStream_t stream);

@@ -877,7 +877,7 @@ def _scalar(t, dtype, name, dev):
 
 def adamw_step(params, grads, states, step, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0,
                grad_scale=None, copies=None):
-    """One AdamW step over many tensors, in place: ``params`` (all float32 or
+    """One AdamW step over many tensors, in place and unseen by autograd: ``params`` (all float32 or
     all bf16), their ``grads`` (all float32 or all bf16; a parameter whose
     gradient is None is left out) and their ``states`` (``adamw_state``, all of one
     kind), at ``step`` (1 for the first).

@@ -453,3 +453,36 @@ def test_float64_logits_that_float32_does_not_tell_apart(C, groups):
             idx, w, place, offsets = C.route_rows(z.cuda(), **o)
             want, _, _ = _oracle(z, None, o)
             assert np.array_equal(idx.cpu().numpy(), want)
+
+
+def test_blocks_of_the_most_rows(C):
+    """More rows than 256 blocks of 2^15 hold: their counts are of 16 bits, and all rows choose few experts."""
+    N, E = (1 << 23) + 40000, 4
+    g = torch.Generator(device="cuda").manual_seed(1)
+    z = torch.randint(-3, 4, (N, E), generator=g, device="cuda").to(BF)
+    z[: N // 2, 1] = 9.0                                  # blocks whose rows all choose expert 1
+    idx, w, place, offsets = C.route_rows(z, 2, score="sigmoid")
+    val, want = torch.sort(z.float(), dim=1, descending=True, stable=True)
+    assert torch.equal(idx.long(), want[:, :2])
+    flat = idx.reshape(-1).long()
+    assert torch.equal(offsets[1:].long(), torch.bincount(flat, minlength=E).cumsum(0))
+    order = torch.argsort(flat, stable=True)
+    at = torch.empty_like(order)
+    at[order] = torch.arange(order.numel(), device="cuda")
+    assert torch.equal(place.reshape(-1).long(), at)
+    s = torch.sigmoid(val[:, :2].double())
+    ref = s / s.sum(1, keepdim=True)
+    assert ((w.double() - ref).abs() <= (2 * 18 + 32) * H * ref).all()
+    torch.cuda.empty_cache()
+
+
+def test_workspace_too_small_is_refused(C):
+    z = _logits(200, 64, F32, 1)
+    ws = torch.empty(C.route_rows_workspace_bytes(200, 64, 4) - 256, dtype=torch.uint8, device="cuda")
+    with pytest.raises(C.CardanError):
+        C.route_rows(z, 4, ws=ws)
+    with pytest.raises(ValueError):
+        C.route_rows(z[:, ::2], 4)
+    with pytest.raises(ValueError):
+        C.route_rows(z[:1].expand(200, 64), 4)
+    assert C.route_rows(z, 4, ws=torch.empty(1 << 20, dtype=torch.uint8, device="cuda"))[0].shape == (200, 4)
