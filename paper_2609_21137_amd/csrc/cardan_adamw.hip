@@ -12,6 +12,12 @@
 // so each is right in the mean and a call's result depends on its arguments
 // alone. bf16 weights are rounded the same way (an update is often below half
 // a step of them).
+//
+// Bound by memory: 38 M float32 weights with float32 moments in 202 us (5.3
+// TB/s), 403 M with bf16 gradients, bf16 copies and 8-bit moments in 1200 us (5.4;
+// a large copy reaches 4.8). A lane holds eight values, half a wave a block, so
+// that a scale is five steps over lanes and no LDS; the update has no fused
+// products, so that it is the same number wherever it is computed.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -2,7 +2,12 @@
 //   dispatch: xe[place[n][j]] = x[n]
 //   combine:  y[n] = sum_j w[n][j] ye[place[n][j]], in the order of j
 //   backward: dye[place[n][j]] = w[n][j] dy[n], dw[n][j] = <dy[n], ye[place[n][j]]>
-// (the gradient of dispatch is combine without weights).
+// (the gradient of dispatch is combine without weights). Bound by the rows' bytes:
+// 8192 x 8 rows of 2048 copied in 52 us (5.8 TB/s), combined in 60 (5.0), combine's
+// gradients in 114 (5.0); counters show the floor's bytes and no others. A
+// thread takes eight values of a row and goes through its k rows, so that a
+// token's row is read once and its sum stays in registers; the gradients take a
+// wave a row, whose inner products need no other one.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -19,8 +24,8 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 // A thread handles eight values at once. WIDE: every row starts on 16 bytes and
 // has a multiple of eight; else accesses of 16 bytes start on any value, and a
-// row's last values come one by one (3000 x 6 rows through all four calls: 113
-// us at 2001 values, 102 at 2000).
+// row's last values come one by one (3000 x 6 rows through all four calls: 105
+// us at 2001 values, 96 at 2000).
 constexpr int kVec = 8;
 typedef u32x4 u32x4_at2 __attribute__((aligned(2)));
 typedef f32x4 f32x4_at4 __attribute__((aligned(4)));
@@ -102,8 +107,8 @@ __device__ __forceinline__ void store_row(void* base, int64_t row, int H, int at
 constexpr int kThreads = 256;
 // A grouped array that the last-level cache (256 MB) does not keep is read and
 // written past the caches, which leaves them to the tokens' rows: 65536 x 2048
-// copied, combined and both gradients 295 us (347 through the caches; combine
-// 60 instead of 80). A smaller one, just written, is still there: 12282 x 2816
+// copied, combined and both gradients 286 us (about 50 more through the caches;
+// combine 60 instead of 80). A smaller one, just written, is still there: 12282 x 2816
 // combined in 15.5 us, past the caches 20.8.
 constexpr int64_t kPastBytes = (int64_t)192 << 20;
 
@@ -157,20 +162,26 @@ __global__ __launch_bounds__(NT) void k_combine(const RowsArgs A) {
 }
 
 // A wave a row: the products of the row of dy with its k rows are summed over
-// the wave's lanes, each in one order.
-template <bool WIDE, bool F32, bool PAST>
+// the wave's lanes, each in one order. A lane keeps up to KEEP runs of eight
+// values of dy's row (read again for every one of the k rows, they came from
+// memory: 509 MB instead of 302 for 65536 x 2048; 18000 x 2001 39 us, now 30).
+template <bool WIDE, bool F32, bool PAST, int KEEP>
 __global__ __launch_bounds__(kThreads) void k_combine_backward(const RowsArgs A) {
   const int lane = threadIdx.x & 63;
   const int64_t waves = (int64_t)gridDim.x * (kThreads / 64);
   for (int64_t n = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6); n < A.N; n += waves) {
+    float kept[KEEP][kVec];
+#pragma unroll
+    for (int c = 0; c < KEEP; ++c) {
+      const int at = (c * 64 + lane) * kVec;
+      if (at < A.H) load_row<WIDE, F32>(A.dy, n, A.H, at, kept[c]);
+    }
     for (int j = 0; j < A.k; ++j) {
       const int p = A.place[n * A.k + j];
       float dot = 0.f;
       if ((uint32_t)p < (uint32_t)A.M) {
         const float w = A.weight ? A.weight[n * A.k + j] : 1.0f;
-        for (int at = lane * kVec; at < A.H; at += 64 * kVec) {
-          float d[kVec];
-          load_row<WIDE, F32>(A.dy, n, A.H, at, d);
+        const auto both = [&](int at, const float (&d)[kVec]) {
           if (A.dweight) {
             float f[kVec];
             load_row<WIDE, false, PAST>(A.ye, p, A.H, at, f);
@@ -178,10 +189,21 @@ __global__ __launch_bounds__(kThreads) void k_combine_backward(const RowsArgs A)
             for (int q = 0; q < kVec; ++q) dot = fmaf(d[q], f[q], dot);
           }
           if (A.dye) {
+            float g[kVec];
 #pragma unroll
-            for (int q = 0; q < kVec; ++q) d[q] *= w;
-            store_row<WIDE, false, PAST>(A.dye, p, A.H, at, d);
+            for (int q = 0; q < kVec; ++q) g[q] = d[q] * w;
+            store_row<WIDE, false, PAST>(A.dye, p, A.H, at, g);
           }
+        };
+#pragma unroll
+        for (int c = 0; c < KEEP; ++c) {
+          const int at = (c * 64 + lane) * kVec;
+          if (at < A.H) both(at, kept[c]);
+        }
+        for (int at = (KEEP * 64 + lane) * kVec; at < A.H; at += 64 * kVec) {
+          float d[kVec];
+          load_row<WIDE, F32>(A.dy, n, A.H, at, d);
+          both(at, d);
         }
 #pragma unroll
         for (int s = 32; s; s >>= 1) dot += __shfl_xor(dot, s);
@@ -218,8 +240,13 @@ void combine(const RowsArgs& A, hipStream_t s) {
 
 template <bool WIDE, bool F32>
 void backward(const RowsArgs& A, dim3 grid, hipStream_t s) {
-  if (past(A)) k_combine_backward<WIDE, F32, true><<<grid, dim3(kThreads), 0, s>>>(A);
-  else k_combine_backward<WIDE, F32, false><<<grid, dim3(kThreads), 0, s>>>(A);
+  if (A.H <= 4 * 64 * kVec) {
+    if (past(A)) k_combine_backward<WIDE, F32, true, 4><<<grid, dim3(kThreads), 0, s>>>(A);
+    else k_combine_backward<WIDE, F32, false, 4><<<grid, dim3(kThreads), 0, s>>>(A);
+  } else {
+    if (past(A)) k_combine_backward<WIDE, F32, true, 8><<<grid, dim3(kThreads), 0, s>>>(A);
+    else k_combine_backward<WIDE, F32, false, 8><<<grid, dim3(kThreads), 0, s>>>(A);
+  }
 }
 
 // Threads of a workgroup: 128 where 256 would leave more of them without values
@@ -247,7 +274,11 @@ hipError_t launch_combine(const RowsArgs& A, hipStream_t s) {
 
 hipError_t launch_combine_backward(const RowsArgs& A, hipStream_t s) {
   if (A.N == 0) return hipSuccess;
-  const dim3 grid((unsigned)std::min<int64_t>(((int64_t)A.N + 3) / 4, 1 << 16));
+  // four workgroups a CU, each wave the same number of rows: 8192 rows of 2048 in
+  // 114 us, with a workgroup for every four rows 127, with 768 of them 124
+  const int64_t rounds = ((int64_t)A.N + 3) / 4, most = 1024;
+  const int64_t each = rounds < 2 * most ? 1 : (rounds + most - 1) / most;
+  const dim3 grid((unsigned)((rounds + each - 1) / each));
   if (A.wide) A.f32 ? backward<true, true>(A, grid, s) : backward<true, false>(A, grid, s);
   else A.f32 ? backward<false, true>(A, grid, s) : backward<false, false>(A, grid, s);
   return hipGetLastError();
