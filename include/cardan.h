@@ -387,7 +387,7 @@ int cardan_distill_loss(int32_t N, int32_t V, int32_t K, int32_t logits_type, co
  * cardan_ffn_forward's rows follow, with its gradient; the copies of the rows
  * and their weighted sums, with theirs; and the step that the gradients go
  * into. Conventions as for the training calls above, except that every pointer
- * need only start on a multiple of its own elements' size. */
+ * but the workspace's need only start on a multiple of its own elements' size. */
 
 enum { CARDAN_SCORE_SOFTMAX = 0, CARDAN_SCORE_SIGMOID = 1 };
 

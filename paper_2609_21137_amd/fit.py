@@ -430,7 +430,7 @@ class TrainedLayer:
         if train_router:
             self.factors["router_w"] = self.router_w.float()
             if bias is not None:
-                self.factors["router_bias"] = self.router_bias.float()
+                self.factors["router_bias"] = self.router_bias.float().clone()
         self.codes, self._word_sums = {}, {}
         for p in self._projections() + ["down"]:
             J = torch.as_tensor(np.ascontiguousarray(layer["codes_" + p])).to(self.device).long()

@@ -97,6 +97,12 @@ def test_array_of_other_rows(C, M):
     assert C.dispatch_rows(x, far, rows=M).shape == (M, H)
 
 
+def test_longest_rows(C):
+    x, ye, place, w = _inputs(3, 2, 1 << 20, 6, True, 3)
+    dy = torch.randn((3, 1 << 20), device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    _check(C, x, ye, place, w, dy.bfloat16())
+
+
 @pytest.mark.parametrize("H", [64, 72])
 def test_slices_that_start_on_any_row(C, H):
     N, k = 9, 3
