@@ -709,6 +709,10 @@ def _route_bytes(E, top_k, N):
 
 
 def _logit_rows(logits):
+    if isinstance(logits, torch.Tensor) and logits.dim() == 2 and logits.is_cuda and logits.is_contiguous():
+        kind = _TYPES.get(logits.dtype)
+        if kind is not None:
+            return logits.data_ptr(), logits.shape[1], kind
     if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or logits.dtype not in _TYPES:
         raise ValueError("logits must be a [N, E] tensor of bfloat16, float32 or float64")
     lp, ld = _rows_ptr(logits, logits.dtype, "logits", logits.shape, logits.device)
@@ -743,21 +747,24 @@ def route_rows(logits, top_k: int, bias=None, score: str = "softmax", renorm: bo
     r = _routing(E, top_k, score, renorm, scale, groups, top_groups, group_best)
     if out is not None:
         idx, weight, place, offsets = out
+        outs = (_arg(idx, i32, "idx", (N, top_k), dev), _arg(weight, f32, "weight", (N, top_k), dev),
+                _arg(place, i32, "place", (N, top_k), dev, offsets is None),
+                _arg(offsets, i32, "offsets", (E + 1,), dev, place is None))
     else:
         # (one allocation: each takes as long as a tenth of a small call)
         idx, place, weight = torch.empty((3, N, top_k), dtype=i32, device=dev).unbind()
         weight = weight.view(f32)
         place, offsets = (place, torch.empty((E + 1,), dtype=i32, device=dev)) if places else (None, None)
+        outs = (idx.data_ptr(), weight.data_ptr(), place.data_ptr() if places else None,
+                offsets.data_ptr() if places else None)
     need = _route_bytes(E, top_k, N) if offsets is not None else 0
     if ws is None:
         ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
     elif ws.dtype is not torch.uint8 or ws.device != dev or not ws.is_contiguous():
         raise ValueError(f"ws must be a contiguous uint8 tensor on {dev}")
-    args = (_arg(bias, f32, "bias", (E,), dev, True), _arg(idx, i32, "idx", (N, top_k), dev),
-            _arg(weight, f32, "weight", (N, top_k), dev), _arg(place, i32, "place", (N, top_k), dev, offsets is None),
-            _arg(offsets, i32, "offsets", (E + 1,), dev, place is None))
+    bias = None if bias is None else _arg(bias, f32, "bias", (E,), dev)
     with _Device(dev) as stream:
-        _check(_lib.cardan_route_rows(ctypes.byref(r), N, kind, lp, ld, *args, ws.data_ptr() if ws is not None else None,
+        _check(_lib.cardan_route_rows(ctypes.byref(r), N, kind, lp, ld, bias, *outs, ws.data_ptr() if ws is not None else None,
                                       ws.numel() if ws is not None else 0, stream))
     return idx, weight, place, offsets
 
@@ -776,8 +783,11 @@ def route_rows_backward(logits, idx, dweight, top_k: int | None = None, score: s
         raise ValueError("idx must be a [N, top_k] tensor")
     k = idx.shape[1]
     r = _routing(E, k, score, renorm, scale, groups, top_groups, group_best)
-    d = out if out is not None else torch.empty((N, E), dtype=logits.dtype, device=dev)
-    dp, dld = _rows_ptr(d, logits.dtype, "out", (N, E), dev)
+    if out is not None:
+        d, (dp, dld) = out, _rows_ptr(out, logits.dtype, "out", (N, E), dev)
+    else:
+        d = torch.empty((N, E), dtype=logits.dtype, device=dev)
+        dp, dld = d.data_ptr(), E
     args = (_arg(idx, torch.int32, "idx", (N, k), dev), _arg(dweight, torch.float32, "dweight", (N, k), dev))
     with _Device(dev) as stream:
         _check(_lib.cardan_route_rows_backward(ctypes.byref(r), N, kind, lp, ld, *args, dp, dld, stream))
@@ -799,9 +809,14 @@ def dispatch_rows(x, place, rows: int | None = None, out=None):
     N, H = _row_types(x, "x")
     k = _row_types(place, "place")[1]
     dev, bf = x.device, torch.bfloat16
-    xe = out if out is not None else torch.empty((N * k if rows is None else rows, H), dtype=bf, device=dev)
-    M = _row_types(xe, "out")[0]
-    args = (_arg(x, bf, "x", (N, H), dev), _arg(place, torch.int32, "place", (N, k), dev), _arg(xe, bf, "out", (M, H), dev))
+    if out is not None:
+        xe, M = out, _row_types(out, "out")[0]
+        to = _arg(xe, bf, "out", (M, H), dev)
+    else:
+        M = N * k if rows is None else rows
+        xe = torch.empty((M, H), dtype=bf, device=dev)
+        to = xe.data_ptr()
+    args = (_arg(x, bf, "x", (N, H), dev), _arg(place, torch.int32, "place", (N, k), dev), to)
     with _Device(dev) as stream:
         _check(_lib.cardan_dispatch_rows(N, k, H, M, *args, stream))
     return xe
@@ -816,11 +831,15 @@ def combine_rows(ye, place, weight=None, dtype=torch.bfloat16, out=None):
     M, H = _row_types(ye, "ye")
     N, k = _row_types(place, "place")
     dev = ye.device
-    y = out if out is not None else torch.empty((N, H), dtype=dtype, device=dev)
-    if not isinstance(y, torch.Tensor) or y.dtype not in (torch.bfloat16, torch.float32):
+    if out is not None:
+        y, dtype = out, getattr(out, "dtype", None)
+    if dtype not in (torch.bfloat16, torch.float32):
         raise ValueError("y is bfloat16 or float32")
+    if out is None:
+        y = torch.empty((N, H), dtype=dtype, device=dev)
     args = (_arg(ye, torch.bfloat16, "ye", (M, H), dev), _arg(place, torch.int32, "place", (N, k), dev),
-            _arg(weight, torch.float32, "weight", (N, k), dev, True), _TYPES[y.dtype], _arg(y, y.dtype, "out", (N, H), dev))
+            _arg(weight, torch.float32, "weight", (N, k), dev, True), _TYPES[dtype],
+            y.data_ptr() if out is None else _arg(y, dtype, "out", (N, H), dev))
     with _Device(dev) as stream:
         _check(_lib.cardan_combine_rows(N, k, H, M, *args, stream))
     return y
