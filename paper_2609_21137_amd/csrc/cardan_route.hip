@@ -610,20 +610,42 @@ __device__ __forceinline__ void scan_experts(int* count, int E, int* part) {
   __syncthreads();
 }
 
-// Places of n slots whose experts `slot(i)` gives, in their order: next[wave][E]
-// (LDS) holds where a wave's first slot of every expert goes.
+// A wave's run of a block's n slots, 64 at a time; the experts of the first few
+// are read ahead of everything else.
+template <int NT>
+struct Slots {
+  static constexpr int NW = NT / 64, AHEAD = 4;
+  int n, lane, begin, end;  // chunks of 64
+  int ahead[AHEAD];
+  template <class F>
+  __device__ __forceinline__ Slots(int count, F slot) : n(count) {
+    lane = threadIdx.x & 63;
+    const int wave = threadIdx.x >> 6, chunks = (n + 63) / 64, per = (chunks + NW - 1) / NW;
+    begin = wave * per;
+    end = std::min(chunks, begin + per);
+#pragma unroll
+    for (int q = 0; q < AHEAD; ++q) ahead[q] = begin + q < end && (begin + q) * 64 + lane < n ? slot((begin + q) * 64 + lane) : -1;
+  }
+  // f(i, e): slot i (may be past the last) has expert e, -1 where there is none
+  template <class F, class G>
+  __device__ __forceinline__ void each(F slot, G f) const {
+#pragma unroll
+    for (int q = 0; q < AHEAD; ++q)
+      if (begin + q < end) f((begin + q) * 64 + lane, ahead[q]);
+    for (int c = begin + AHEAD; c < end; ++c) {
+      const int i = c * 64 + lane;
+      f(i, i < n ? slot(i) : -1);
+    }
+  }
+};
+
+// Places of a wave's slots in their order: next[wave][E] (LDS) holds where its
+// first slot of every expert goes.
 template <int NT, class F>
-__device__ __forceinline__ void place_slots(int n, int E, int* next, F slot, int32_t* place) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  constexpr int NW = NT / 64;
-  const int chunks = (n + 63) / 64, per = (chunks + NW - 1) / NW;
-  int* mine = next + wave * E;
-  const int end = std::min(chunks, (wave + 1) * per);
-  int ahead = wave * per < end && wave * per * 64 + lane < n ? slot(wave * per * 64 + lane) : -1;
-  for (int c = wave * per; c < end; ++c) {
-    const int i = c * 64 + lane;
-    const int e = ahead;
-    ahead = c + 1 < end && i + 64 < n ? slot(i + 64) : -1;
+__device__ __forceinline__ void place_slots(const Slots<NT>& S, int E, int* next, F slot, int32_t* place) {
+  const int lane = S.lane;
+  int* mine = next + (threadIdx.x >> 6) * E;
+  S.each(slot, [&](int i, int e) {
     // the lanes with the same expert
     uint64_t same = __ballot(e >= 0);
     for (int bit = 0; (E - 1) >> bit; ++bit) {
@@ -638,27 +660,21 @@ __device__ __forceinline__ void place_slots(int n, int E, int* next, F slot, int
       if (lane == first) start = atomicAdd(&mine[e], __popcll(same));
       at = __shfl(start, first) + before;
     }
-    if (i < n) place[i] = at;
-  }
+    if (i < S.n) place[i] = at;
+  });
 }
 
-// next[wave][E] from where the block's slots of every expert start (base[E])
-// and the slots of the waves before.
+// next[wave][E]: how many of a wave's slots every expert has. next is zero.
 template <int NT, class F>
-__device__ __forceinline__ void count_slots(int n, int E, int* next, F slot) {
-  constexpr int NW = NT / 64;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int i = threadIdx.x; i < NW * E; i += NT) next[i] = 0;
-  __syncthreads();
-  const int chunks = (n + 63) / 64, per = (chunks + NW - 1) / NW;
-#pragma unroll 4
-  for (int c = wave * per; c < std::min(chunks, (wave + 1) * per); ++c) {
-    const int i = c * 64 + lane;
-    const int e = i < n ? slot(i) : -1;
-    if (e >= 0) atomicAdd(&next[wave * E + e], 1);
-  }
+__device__ __forceinline__ void count_slots(const Slots<NT>& S, int E, int* next, F slot) {
+  int* mine = next + (threadIdx.x >> 6) * E;
+  S.each(slot, [&](int, int e) {
+    if (e >= 0) atomicAdd(&mine[e], 1);
+  });
   __syncthreads();
 }
+// ... and from that where a wave's first slot of every expert goes: behind those
+// of the block's earlier waves, the first of which goes to base[e].
 template <int NT>
 __device__ __forceinline__ void start_slots(int E, int* next, const int* base) {
   constexpr int NW = NT / 64;
@@ -719,7 +735,10 @@ __global__ __launch_bounds__(NT) void k_route_rows(const RouteArgs A) {
     int *next = count + A.E + 1, *part = next + NT / 64 * A.E;
     const int n = A.N * A.k;
     const auto slot = [&](int i) { return sel[i]; };
-    count_slots<NT>(n, A.E, next, slot);
+    const Slots<NT> S(n, slot);
+    for (int i = tid; i < NT / 64 * A.E; i += NT) next[i] = 0;
+    __syncthreads();
+    count_slots<NT>(S, A.E, next, slot);
     for (int e = tid; e < A.E; e += NT) {
       int c = 0;
       for (int w = 0; w < NT / 64; ++w) c += next[w * A.E + e];
@@ -729,7 +748,7 @@ __global__ __launch_bounds__(NT) void k_route_rows(const RouteArgs A) {
     scan_experts<NT>(count, A.E, part);
     for (int e = tid; e <= A.E; e += NT) A.offsets[e] = count[e];
     start_slots<NT>(A.E, next, count);
-    place_slots<NT>(n, A.E, next, slot, A.place);
+    place_slots<NT>(S, A.E, next, slot, A.place);
   } else {
     for (int i = tid; i < A.E; i += NT) A.count[(int64_t)blockIdx.x * count_row(A.E) + i] = (uint16_t)count[i];
   }
@@ -751,7 +770,8 @@ __global__ __launch_bounds__(kPlaceThreads) void k_route_place(const RouteArgs A
   const int n = (int)std::min((int64_t)A.block_rows * A.k, (int64_t)A.N * A.k - first);
   const int32_t* idx = A.idx + first;
   const auto slot = [&](int i) { return idx[i]; };
-  for (int e = tid; e < 2 * A.E + 1; e += NT) count[e] = 0;
+  const Slots<NT> S(n, slot);
+  for (int e = tid; e < (2 + NT / 64) * A.E + 1; e += NT) count[e] = 0;  // (before and next behind it)
   __syncthreads();
   // a thread eight experts and a slice of the blocks
   const int cols = (A.E + 7) / 8, width = cols > 64 ? 128 : cols > 32 ? 64 : cols > 16 ? 32 : cols > 8 ? 16 : 8;
@@ -774,7 +794,7 @@ __global__ __launch_bounds__(kPlaceThreads) void k_route_place(const RouteArgs A
         atomicAdd(&before[col * 8 + q], (int)sum[q]);
       }
   }
-  count_slots<NT>(n, A.E, next, slot);
+  count_slots<NT>(S, A.E, next, slot);
   scan_experts<NT>(count, A.E, part);
   if (b == 0)
     for (int e = tid; e <= A.E; e += NT) A.offsets[e] = count[e];
@@ -782,7 +802,7 @@ __global__ __launch_bounds__(kPlaceThreads) void k_route_place(const RouteArgs A
   for (int e = tid; e < A.E; e += NT) count[e] += before[e];
   __syncthreads();
   start_slots<NT>(A.E, next, count);
-  place_slots<NT>(n, A.E, next, slot, A.place + first);
+  place_slots<NT>(S, A.E, next, slot, A.place + first);
 }
 
 // Without rows: no expert has any.
