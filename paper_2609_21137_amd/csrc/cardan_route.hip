@@ -14,7 +14,7 @@
 // so that the lowest lane with the largest value holds the lowest index. Bound
 // by vector instructions and latency, not by memory: 65536 rows of 128 float32
 // logits take 16 us, of which 8 are the read of 34 MB and the launch (4.2 TB/s);
-// a wave's pass over 8 rows is about 690 vector instructions. With a bias and
+// a wave's pass over 8 rows is about 660 vector instructions. With a bias and
 // groups (8191 x 256) 19 us, 5 of them for the few rows whose groups float32
 // does not tell apart: their wave's float64 scores end the kernel. The places
 // are a second launch of 6 to 9 us, most of it the length of its barriers.
@@ -339,9 +339,9 @@ __device__ __forceinline__ void keep_groups(float (&v)[EPL], const RouteArgs& A,
 // the selection's last, so that others may be, too. (A lane's keys come out of
 // LDS one by one: shifted in registers they took a third of the kernel's
 // instructions.)
-template <class L, int LPR, int EPL, bool LOGITS>
+template <class L, int LPR, int EPL, bool LOGITS, class F>
 __device__ __forceinline__ bool select_keys(const float (&v)[EPL], const RouteArgs& A, int lane, const L* row, float margin,
-                                            const RowLds& X) {
+                                            const RowLds& X, F ahead) {
   constexpr uint32_t kMask = (LOGITS ? LPR * EPL : EPL) - 1;
   const int at = lane & (LPR - 1);
   uint32_t key[EPL], low = 0;
@@ -350,6 +350,7 @@ __device__ __forceinline__ bool select_keys(const float (&v)[EPL], const RouteAr
     if constexpr (LOGITS) low |= __float_as_uint(v[i]);
     key[i] = (ordered(v[i]) & ~kMask) | (kMask - (LOGITS ? at * EPL + i : i));
   }
+  ahead();
   // logits whose low bits are all zero (bf16 ones) lose nothing in the keys
   bool whole = LOGITS && sizeof(L) == 2;
   if constexpr (LOGITS && sizeof(L) == 4) whole = row_ballot<LPR>((low & kMask) != 0, lane) == 0;
@@ -478,10 +479,11 @@ __device__ __forceinline__ void select_values(const RouteArgs& A, int lane, cons
   wave_sync();
 }
 
-// The selection and the weights of row n, whose logits are z; X.e receives the experts.
-template <class L, class V, int LPR, int EPL>
+// The selection and the weights of row n, whose logits are z; X.e receives the
+// experts. ahead() is called once z is used up: it fetches the next row's.
+template <class L, class V, int LPR, int EPL, class F>
 __device__ __forceinline__ void route_row(const RouteArgs& A, int n, int lane, const RowLds& X,
-                                          const typename Wide<L>::type (&z)[EPL]) {
+                                          const typename Wide<L>::type (&z)[EPL], F ahead) {
   typedef typename Wide<L>::type T;
   const int at = lane & (LPR - 1), e0 = at * EPL;
   const L* row = static_cast<const L*>(A.logits) + (int64_t)n * A.ld;
@@ -541,7 +543,8 @@ __device__ __forceinline__ void route_row(const RouteArgs& A, int n, int lane, c
     float margin = sizeof(T) == 8 ? 0x1p-100f : 0.f;  // (float64 logits are rounded, too)
     if (by_score) margin = A.sigmoid ? 0x1p-21f : 0x1p-17f / (float)sum + 0x1p-22f;
     if (A.groups > 1) keep_groups<L, V, LPR>(v, A, at, row, 2.f * margin, X);
-    if (!select_keys<L, LPR, EPL, sizeof(V) == 4>(v, A, lane, row, margin, X)) select_values<L, V, LPR, EPL>(A, lane, row, X);
+    if (!select_keys<L, LPR, EPL, sizeof(V) == 4>(v, A, lane, row, margin, X, ahead))
+      select_values<L, V, LPR, EPL>(A, lane, row, X);
   }
 
   // the weights, a selection a lane
@@ -713,14 +716,10 @@ __global__ __launch_bounds__(NT) void k_route_rows(const RouteArgs A) {
   const auto load = [&](int n, T (&z)[EPL]) {
     if (n < last) load_row<EPL>(static_cast<const L*>(A.logits) + (int64_t)n * A.ld, (lane & (LPR - 1)) * EPL, A.E, A.wide, z);
   };
-  T next[EPL];
-  load(first + r, next);
+  T z[EPL];
+  load(first + r, z);
   for (int n = first + r; n < last; n += ROWS) {
-    T z[EPL];
-#pragma unroll
-    for (int i = 0; i < EPL; ++i) z[i] = next[i];
-    load(n + ROWS, next);
-    route_row<L, V, LPR, EPL>(A, n, lane, X, z);
+    route_row<L, V, LPR, EPL>(A, n, lane, X, z, [&] { load(n + ROWS, z); });
     if (ONE || A.place)
       for (int j = lane & (LPR - 1); j < A.k; j += LPR) {
         const int e = X.e[j];

@@ -486,3 +486,24 @@ def test_workspace_too_small_is_refused(C):
     with pytest.raises(ValueError):
         C.route_rows(z[:1].expand(200, 64), 4)
     assert C.route_rows(z, 4, ws=torch.empty(1 << 20, dtype=torch.uint8, device="cuda"))[0].shape == (200, 4)
+
+
+def test_rows_past_31_bits(C):
+    """Logits and gradients whose last rows lie behind 2^31 elements."""
+    N, E, ld = (1 << 21) + 70, 64, 1024
+    full = torch.zeros((N, ld), dtype=BF, device="cuda")
+    grad = torch.zeros((N, ld), dtype=BF, device="cuda")
+    z = full[:, :E]
+    last = _logits(70, E, BF, 3)
+    z[-70:] = last
+    o = _opts(4, "softmax", False)
+    idx, w, place, offsets = C.route_rows(z, **o)
+    want = C.route_rows(last, **o)
+    assert torch.equal(idx[-70:], want[0]) and torch.equal(w[-70:], want[1])
+    assert torch.equal(idx[:5], torch.arange(4, device="cuda").int().expand(5, 4))
+    d = torch.ones(w.shape, device="cuda")
+    C.route_rows_backward(z, idx, d, out=grad[:, :E], **o)
+    assert torch.equal(grad[-70:, :E], C.route_rows_backward(last, want[0], d[-70:].contiguous(), **o))
+    assert not grad[:, E:].any()
+    del full, grad
+    torch.cuda.empty_cache()
