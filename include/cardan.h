@@ -411,9 +411,9 @@ int cardan_route_rows_workspace_bytes(const cardan_routing* routing, int32_t N, 
 
 /* Routing of N rows of logits z (row n at logits + n * ld; bf16, float32 or
  * float64). Scores s_e = softmax(z)_e over all E or sigmoid(z_e). The selection
- * goes by v_e = s_e + bias_e in float64 (bias: [E] float32, or NULL) where there
- * is a bias or group_best is 2 with groups; else by z_e, in the scores' order. A
- * group counts by its best v or the sum of its best two; of the top_groups best
+ * goes by v_e = s_e + bias_e in float64 (bias: [E] float32) where there is a bias,
+ * without one (NULL) by z_e, in the scores' order. A group counts by its best v
+ * or the sum of its best two (of scores, with or without bias); of the top_groups best
  * groups (ties to the lower index) the top_k largest v are kept, descending,
  * exact ties to the lower index. weight_j = scale * s_j, divided by the sum of
  * the kept s with renorm; the bias is in no weight. With softmax, renorm, no

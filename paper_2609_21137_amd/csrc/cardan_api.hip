@@ -1002,7 +1002,7 @@ int cardan_route_rows_workspace_bytes(const cardan_routing* routing, int32_t N, 
   // counts of every block of rows (of four at least)
   const int64_t few = std::min<int64_t>(kRouteBlocks, ((int64_t)N + 3) / 4);
   const int64_t blocks = std::max<int64_t>(few, ((int64_t)N + kBlockRows - 1) / kBlockRows);
-  *out = N <= kRouteSmall ? 0 : align256((size_t)blocks * count_row(routing->E) * 2);
+  *out = N <= route_small(routing->E) ? 0 : align256((size_t)blocks * count_row(routing->E) * 2);
   return CARDAN_OK;
 }
 
@@ -1023,6 +1023,7 @@ int cardan_route_rows(const cardan_routing* routing, int32_t N, int32_t logits_t
   size_t need = 0;
   if ((rc = cardan_route_rows_workspace_bytes(routing, N, &need))) return rc;
   if (offsets && need > 0 && (rc = check_ws(need, ws, ws_bytes))) return rc;
+  if (A.top_groups == A.groups) A.groups = A.top_groups = 1, A.each = A.E;  // (all of them are kept)
   A.by_score = bias != nullptr || (A.groups > 1 && A.best == 2);
   A.bias = bias;
   A.idx = idx;

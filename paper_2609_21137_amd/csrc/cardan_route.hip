@@ -3,11 +3,10 @@
 // the logits.
 //
 // Per row with logits z: score s_e = softmax(z)_e or sigmoid(z_e); the
-// selection goes by v_e = s_e + bias_e in float64 where there is a bias or a
-// group counts by its best two, else by z_e, whose order is the scores'.
-// Groups of E / G consecutive experts count by their best v, or by the sum of
-// their best two; the top_k largest v of the kept groups, descending, ties to
-// the lower index. weight_j = scale s_j, over the sum of the kept s if
+// selection goes by v_e = s_e + bias_e in float64 where there is a bias, else by
+// z_e, whose order is the scores'. Groups of E / G consecutive experts count by
+// their best v, or by the sum of their best two (of scores); the top_k largest v
+// of the kept groups, descending, ties to the lower index. weight_j = scale s_j, over the sum of the kept s if
 // renormalised.
 //
 // A row is spread over LPR lanes of one wave, EPL consecutive experts a lane,
@@ -66,10 +65,8 @@ __device__ __forceinline__ V over_row(V v, F f) {
   v = f(v, lane_move<0x4E>(v));   // lane ^ 2
   v = f(v, lane_move<0x141>(v));  // the other half of 8
   if constexpr (LPR >= 16) v = f(v, lane_move<0x140>(v));  // the other half of 16
-  if constexpr (LPR == 64) {
-    v = f(v, __shfl_xor(v, 16));
-    v = f(v, __shfl_xor(v, 32));
-  }
+  if constexpr (LPR >= 32) v = f(v, __shfl_xor(v, 16));
+  if constexpr (LPR == 64) v = f(v, __shfl_xor(v, 32));
   return v;
 }
 template <int LPR, class V>
@@ -135,6 +132,13 @@ __device__ __forceinline__ void store_row(L* row, int e0, int E, bool wide, cons
 template <class T> __device__ __forceinline__ T exp_of(T v);
 template <> __device__ __forceinline__ float exp_of(float v) { return expf(v); }
 template <> __device__ __forceinline__ double exp_of(double v) { return exp(v); }
+
+// A logit as float32; a float64 one below float32's range is one all the same.
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(double v) {
+  const float f = (float)v;
+  return f == -INFINITY && v != -INFINITY ? -3.402823466e38f : f;
+}
 
 template <int EPL, class V>
 __device__ __forceinline__ V local_max(const V (&v)[EPL]) {
@@ -221,30 +225,44 @@ __device__ __forceinline__ void rank_groups(const RouteArgs& A, int at, const V*
     else most = x > most ? x : most;
   }
 }
-// Values of this lane's groups from all[E] (LDS).
+// Values of the groups from all[E] (LDS): 2^group_split lanes a group. (One lane
+// a group took 69 us for 237 rows of 180 experts in two groups, several take 30.)
 template <int LPR, class V>
 __device__ __forceinline__ void value_groups(const RouteArgs& A, int at, const V* all, V* value) {
-  for (int grp = at; grp < A.groups; grp += LPR) {
+  const int lg = A.group_split, sub = at & ((1 << lg) - 1);
+  for (int first = 0; first < A.groups; first += LPR >> lg) {
+    const int grp = first + (at >> lg);
     V b1 = (V)-INFINITY, b2 = (V)-INFINITY;
+    if (grp < A.groups) {
 #pragma unroll 4
-    for (int i = 0; i < A.each; ++i) {
-      const V x = all[grp * A.each + i], lo = x < b1 ? x : b1;
-      b1 = x > b1 ? x : b1;
-      b2 = lo > b2 ? lo : b2;
+      for (int i = sub; i < A.each; i += 1 << lg) {
+        const V x = all[grp * A.each + i], lo = x < b1 ? x : b1;
+        b1 = x > b1 ? x : b1;
+        b2 = lo > b2 ? lo : b2;
+      }
     }
-    value[grp] = A.best == 2 && b2 != (V)-INFINITY ? b1 + b2 : b1;
+    const auto join = [&](V o1, V o2) {
+      const V lo = o1 < b1 ? o1 : b1, hi = o2 > b2 ? o2 : b2;
+      b1 = o1 > b1 ? o1 : b1;
+      b2 = lo > hi ? lo : hi;
+    };
+    if (lg > 0) join(lane_move<0xB1>(b1), lane_move<0xB1>(b2));
+    if (lg > 1) join(lane_move<0x4E>(b1), lane_move<0x4E>(b2));
+    if (lg > 2) join(lane_move<0x141>(b1), lane_move<0x141>(b2));
+    if (lg > 3) join(lane_move<0x140>(b1), lane_move<0x140>(b2));
+    if (sub == 0 && grp < A.groups) value[grp] = A.best == 2 && b2 != (V)-INFINITY ? b1 + b2 : b1;
   }
 }
 
 // The values that define the selection, logits or float64 scores with their
 // bias, -infinity for NaN and what is not there, into all[E] (X.area).
 template <class L, class V, int LPR, int EPL>
-__device__ __forceinline__ void exact_values(const RouteArgs& A, int at, const L* row, const RowLds& X) {
+__device__ __forceinline__ void exact_values(const RouteArgs& A, bool scores, int at, const L* row, const RowLds& X) {
   const int lo = at * EPL;
   V* all = reinterpret_cast<V*>(X.area);
   V x[EPL], top = (V)-INFINITY, sum = 0;
   load_row<EPL>(row, lo, A.E, A.wide, x);
-  if (sizeof(V) == 8 && (sizeof(L) < 8 || A.by_score)) {
+  if (sizeof(V) == 8 && scores) {
     if (!A.sigmoid) {
       top = row_max<LPR>(local_max(x));
       if (top == (V)-INFINITY) top = 0;
@@ -312,7 +330,7 @@ __device__ __forceinline__ void keep_groups(float (&v)[EPL], const RouteArgs& A,
     most = row_max<LPR>(most);
     if (!(most == -INFINITY || least - most > margin + 0x1p-23f * (fabsf(least) + fabsf(most)))) {
       V a = 0, b = 0, *exact = reinterpret_cast<V*>(X.group);
-      exact_values<L, V, LPR, EPL>(A, at, row, X);
+      exact_values<L, V, LPR, EPL>(A, A.by_score, at, row, X);
       value_groups<LPR>(A, at, reinterpret_cast<V*>(X.area), exact);
       wave_sync();
       rank_groups<LPR>(A, at, exact, keep, a, b);
@@ -410,19 +428,23 @@ __device__ __forceinline__ bool select_keys(const float (&v)[EPL], const RouteAr
     }
   } else {
     double *value = reinterpret_cast<double*>(X.area), top = 0, sum = 1;
-    const bool by_score = sizeof(L) < 8 || A.by_score;
-    if (by_score && !A.sigmoid) {
+    const bool scores = sizeof(L) < 8 || A.bias != nullptr;  // (float64 logits are rounded in v, too)
+    if (scores && !A.sigmoid) {
       double z[EPL];
       load_row<EPL>(row, at * EPL, A.E, A.wide, z);
       top = row_max<LPR>(local_max(z));
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) value[at * EPL + i] = z[i] - top;
       sum = 0;
-      for (int e = at * EPL; e < at * EPL + EPL && e < A.E; ++e) sum += exp_of((double)widen(row[e]) - top);
+#pragma unroll 4
+      for (int i = 0; i < EPL; ++i) sum += exp_of(value[at * EPL + i]);
       sum = row_sum<LPR>(sum);
+      wave_sync();
     }
     for (int j = at; j < total; j += LPR) {
       const int e = X.e[j];
       double x = e >= 0 ? (double)widen(row[e]) : -INFINITY;
-      if (by_score && e >= 0) {
+      if (scores && e >= 0) {
         const double y = exp_of(A.sigmoid ? -x : x - top);
         x = (A.sigmoid ? 1.0 / (1.0 + y) : y / sum) + (A.bias ? (double)A.bias[e] : 0.0);
       }
@@ -451,7 +473,7 @@ template <class L, class V, int LPR, int EPL>
 __device__ __forceinline__ void select_values(const RouteArgs& A, int lane, const L* row, const RowLds& X) {
   const int at = lane & (LPR - 1), lo = at * EPL, hi = lo + EPL < A.E ? lo + EPL : A.E;
   V* all = reinterpret_cast<V*>(X.area);
-  exact_values<L, V, LPR, EPL>(A, at, row, X);
+  exact_values<L, V, LPR, EPL>(A, A.bias != nullptr, at, row, X);
   if (A.groups > 1) {
     const int* keep = reinterpret_cast<const int*>(X.group + 64 * 8);
     for (int e = lo; e < hi; ++e)
@@ -504,11 +526,7 @@ __device__ __forceinline__ void route_row(const RouteArgs& A, int n, int lane, c
         sum = row_sum<LPR>(sum);
       }
 #pragma unroll
-      for (int i = 0; i < EPL; ++i) {
-        // (a float64 logit below float32's range is one all the same)
-        const float f = (float)z[i];
-        v[i] = sizeof(T) == 8 && f == -INFINITY && z[i] != (T)-INFINITY ? -3.402823466e38f : f;
-      }
+      for (int i = 0; i < EPL; ++i) v[i] = to_float(z[i]);
       if (by_score) {
         // float32 scores: a sigmoid s is off by at most s (1 - s) (|z| + 2) 2^-24 for the exponential (below
         // 3/4 2^-24) and 3 2^-24 for sum and reciprocal, so two of them by less than 2^-21; a softmax, whose
@@ -540,11 +558,17 @@ __device__ __forceinline__ void route_row(const RouteArgs& A, int n, int lane, c
       }
       bad = row_ballot<LPR>(bad, lane) != 0;
     }
-    float margin = sizeof(T) == 8 ? 0x1p-100f : 0.f;  // (float64 logits are rounded, too)
-    if (by_score) margin = A.sigmoid ? 0x1p-21f : 0x1p-17f / (float)sum + 0x1p-22f;
+    const float least = sizeof(T) == 8 ? 0x1p-100f : 0.f;  // (float64 logits are rounded, too)
+    const float margin = !by_score ? least : A.sigmoid ? 0x1p-21f : 0x1p-17f / (float)sum + 0x1p-22f;
     if (A.groups > 1) keep_groups<L, V, LPR>(v, A, at, row, 2.f * margin, X);
-    if (!select_keys<L, LPR, EPL, sizeof(V) == 4>(v, A, lane, row, margin, X, ahead))
-      select_values<L, V, LPR, EPL>(A, lane, row, X);
+    bool decided;
+    if (by_score && !A.bias) {  // scores were for the groups alone
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) v[i] = v[i] == -INFINITY ? v[i] : to_float(z[i]);
+    }
+    if (sizeof(V) == 4 || (sizeof(L) < 8 && !A.bias)) decided = select_keys<L, LPR, EPL, sizeof(L) < 8>(v, A, lane, row, least, X, ahead);
+    else decided = select_keys<L, LPR, EPL, false>(v, A, lane, row, A.bias ? margin : least, X, ahead);
+    if (!decided) select_values<L, V, LPR, EPL>(A, lane, row, X);
   }
 
   // the weights, a selection a lane
@@ -931,6 +955,8 @@ hipError_t run_rows(const RouteArgs& given, hipStream_t s) {
   A.group_lanes = -1;
   for (int lg = 0; 1 << lg <= 16; ++lg)
     if (A.each == EPL << lg) A.group_lanes = lg;
+  A.group_split = 0;
+  while (A.group_split < 4 && A.groups << (A.group_split + 1) <= LPR) ++A.group_split;
   if constexpr (ONE) {
     constexpr int NT = EPL <= 8 && LPR == 16 ? 512 : 256, ROWS = NT / LPR;  // (their LDS is below 160 KiB)
     const size_t lds = (size_t)ROWS * A.row_lds + 4 * ((size_t)A.N * A.k + A.E + 1 + NT / 64 * A.E + NT / 64);
@@ -951,7 +977,7 @@ hipError_t run_rows(const RouteArgs& given, hipStream_t s) {
 // latency counts, have more lanes.
 template <class L, class V>
 hipError_t run_width(const RouteArgs& A, hipStream_t s) {
-  if (A.N <= kRouteSmall) {
+  if (A.N <= route_small(A.E)) {
     if (A.E <= 64) return run_rows<L, V, 16, 4, true>(A, s);
     if (A.E <= 128) return run_rows<L, V, 16, 8, true>(A, s);
     if (A.E <= 256) return run_rows<L, V, 16, 16, true>(A, s);
@@ -961,7 +987,7 @@ hipError_t run_width(const RouteArgs& A, hipStream_t s) {
   if (A.E <= 64) return run_rows<L, V, 8, 8, false>(A, s);
   if (A.E <= 128) return run_rows<L, V, 8, 16, false>(A, s);
   if (A.E <= 256) return run_rows<L, V, 16, 16, false>(A, s);
-  if (A.E <= 512) return run_rows<L, V, 64, 8, false>(A, s);
+  if (A.E <= 512) return run_rows<L, V, 32, 16, false>(A, s);
   return run_rows<L, V, 64, 16, false>(A, s);
 }
 

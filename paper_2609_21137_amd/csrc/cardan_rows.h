@@ -20,15 +20,16 @@ enum LogitType { LOGIT_BF16 = 0, LOGIT_F32 = 1, LOGIT_F64 = 2 };
 // block had more rows than 16 bits count (a row chooses an expert once).
 constexpr int kRouteBlocks = 256, kBlockRows = 1 << 15;
 __host__ __device__ inline int count_row(int E) { return (E + 7) / 8 * 8; }
-// Rows of one call that a single workgroup routes and places by itself.
-constexpr int kRouteSmall = 64;
+// Rows of one call that a single workgroup routes and places by itself: two
+// passes of its threads (2.5 us each; a second launch takes 6).
+inline int route_small(int E) { return E <= 128 ? 64 : E <= 256 ? 32 : 8; }
 
 // One call of the routing of N rows (the backward pass reads idx and dweight).
 struct RouteArgs {
   int32_t N, E, k;
   int32_t sigmoid, renorm;
   int32_t groups, top_groups, best, each;  // each = E / groups experts a group
-  int32_t by_score;                        // selection by float64 scores (plus bias), else by logits
+  int32_t by_score;                        // float64 scores are needed: a bias, or groups by their best two
   int32_t type;                            // LogitType
   int32_t wide;                            // rows and strides allow 16-byte accesses
   float scale;
@@ -42,7 +43,7 @@ struct RouteArgs {
   uint16_t* count;                         // [blocks][count_row(E)] (workspace)
   int32_t block_rows, blocks;
   Divisor by_each;                         // division by `each`
-  int32_t group_lanes, row_lds, slots;
+  int32_t group_lanes, group_split, row_lds, slots;
   const float* dweight;                    // [N][k]
   void* dlogits;                           // [N][dld]
 };

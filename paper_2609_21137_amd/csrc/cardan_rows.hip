@@ -112,13 +112,28 @@ constexpr int kThreads = 256;
 // combined in 15.5 us, past the caches 20.8.
 constexpr int64_t kPastBytes = (int64_t)192 << 20;
 
-// blockIdx.x: a run of a row's values, blockIdx.y: rows, strided.
+// The rows of a workgroup's threads. NT > 0: blockIdx.x is a run of a row's
+// values, blockIdx.y rows, strided. NT == 0: rows of less than half a workgroup's
+// values one behind the other (15138 rows of 92 copied twice, combined and both
+// gradients 65 us with a workgroup a row, now 29). f(n, position).
+template <int NT, class F>
+__device__ __forceinline__ void each_row(const RowsArgs& A, F f) {
+  if constexpr (NT > 0) {
+    const int at = (blockIdx.x * NT + threadIdx.x) * kVec;
+    if (at >= A.H) return;
+    for (int64_t n = blockIdx.y; n < A.N; n += gridDim.y) f(n, at);
+  } else {
+    const int vecs = (A.H + kVec - 1) / kVec, rows = kThreads / vecs;
+    const int r = threadIdx.x / vecs, at = (threadIdx.x - r * vecs) * kVec;
+    if (r >= rows) return;
+    for (int64_t n = (int64_t)blockIdx.x * rows + r; n < A.N; n += (int64_t)gridDim.x * rows) f(n, at);
+  }
+}
+
 template <bool WIDE, bool PAST, int NT>
-__global__ __launch_bounds__(NT) void k_dispatch(const RowsArgs A) {
+__global__ __launch_bounds__(NT ? NT : kThreads) void k_dispatch(const RowsArgs A) {
   typedef typename At<WIDE>::bf16 V;
-  const int at = (blockIdx.x * NT + threadIdx.x) * kVec;
-  if (at >= A.H) return;
-  for (int64_t n = blockIdx.y; n < A.N; n += gridDim.y) {
+  each_row<NT>(A, [&](int64_t n, int at) {
     const uint16_t* from = A.x + n * A.H + at;
     if (WIDE || at + kVec <= A.H) {
       const u32x4 v = *reinterpret_cast<const V*>(from);
@@ -136,14 +151,12 @@ __global__ __launch_bounds__(NT) void k_dispatch(const RowsArgs A) {
         for (int q = 0; at + q < A.H; ++q) A.xe[(int64_t)p * A.H + at + q] = from[q];
       }
     }
-  }
+  });
 }
 
 template <bool WIDE, bool F32, bool PAST, int NT>
-__global__ __launch_bounds__(NT) void k_combine(const RowsArgs A) {
-  const int at = (blockIdx.x * NT + threadIdx.x) * kVec;
-  if (at >= A.H) return;
-  for (int64_t n = blockIdx.y; n < A.N; n += gridDim.y) {
+__global__ __launch_bounds__(NT ? NT : kThreads) void k_combine(const RowsArgs A) {
+  each_row<NT>(A, [&](int64_t n, int at) {
     float sum[kVec];
 #pragma unroll
     for (int q = 0; q < kVec; ++q) sum[q] = 0.f;
@@ -158,25 +171,29 @@ __global__ __launch_bounds__(NT) void k_combine(const RowsArgs A) {
       for (int q = 0; q < kVec; ++q) sum[q] = fmaf(w, f[q], sum[q]);
     }
     store_row<WIDE, F32>(A.y, n, A.H, at, sum);
-  }
+  });
 }
 
 // A wave a row: the products of the row of dy with its k rows are summed over
 // the wave's lanes, each in one order. A lane keeps up to KEEP runs of eight
 // values of dy's row (read again for every one of the k rows, they came from
 // memory: 509 MB instead of 302 for 65536 x 2048; 18000 x 2001 39 us, now 30).
+// KEEP == 0: a wave a row and place, for few rows (2 x 7 rows of 6215 took 35 us).
 template <bool WIDE, bool F32, bool PAST, int KEEP>
 __global__ __launch_bounds__(kThreads) void k_combine_backward(const RowsArgs A) {
   const int lane = threadIdx.x & 63;
   const int64_t waves = (int64_t)gridDim.x * (kThreads / 64);
-  for (int64_t n = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6); n < A.N; n += waves) {
-    float kept[KEEP][kVec];
+  const int64_t items = KEEP ? A.N : (int64_t)A.N * A.k;
+  for (int64_t item = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6); item < items; item += waves) {
+    const int64_t n = KEEP ? item : item / A.k;
+    const int j0 = KEEP ? 0 : (int)(item - n * A.k), j1 = KEEP ? A.k : j0 + 1;
+    float kept[KEEP ? KEEP : 1][kVec];
 #pragma unroll
     for (int c = 0; c < KEEP; ++c) {
       const int at = (c * 64 + lane) * kVec;
       if (at < A.H) load_row<WIDE, F32>(A.dy, n, A.H, at, kept[c]);
     }
-    for (int j = 0; j < A.k; ++j) {
+    for (int j = j0; j < j1; ++j) {
       const int p = A.place[n * A.k + j];
       float dot = 0.f;
       if ((uint32_t)p < (uint32_t)A.M) {
@@ -200,6 +217,7 @@ __global__ __launch_bounds__(kThreads) void k_combine_backward(const RowsArgs A)
           const int at = (c * 64 + lane) * kVec;
           if (at < A.H) both(at, kept[c]);
         }
+#pragma unroll 4
         for (int at = (KEEP * 64 + lane) * kVec; at < A.H; at += 64 * kVec) {
           float d[kVec];
           load_row<WIDE, F32>(A.dy, n, A.H, at, d);
@@ -217,70 +235,83 @@ bool past(const RowsArgs& A) { return (int64_t)A.M * A.H * 2 > kPastBytes; }
 
 template <int NT>
 dim3 row_grid(const RowsArgs& A) {
-  return dim3((unsigned)(((int64_t)A.H + kVec * NT - 1) / (kVec * NT)), (unsigned)std::min(A.N, 65535));
+  const int vecs = (A.H + kVec - 1) / kVec;
+  if constexpr (NT == 0) {
+    const int64_t rows = kThreads / vecs;
+    return dim3((unsigned)std::min<int64_t>(((int64_t)A.N + rows - 1) / rows, 1 << 20));
+  } else {
+    return dim3((unsigned)((vecs + NT - 1) / NT), (unsigned)std::min(A.N, 65535));
+  }
 }
 
 template <bool WIDE, int NT>
 void dispatch(const RowsArgs& A, hipStream_t s) {
-  const dim3 grid = row_grid<NT>(A);
-  if (past(A)) k_dispatch<WIDE, true, NT><<<grid, dim3(NT), 0, s>>>(A);
-  else k_dispatch<WIDE, false, NT><<<grid, dim3(NT), 0, s>>>(A);
+  const dim3 grid = row_grid<NT>(A), threads(NT ? NT : kThreads);
+  if (past(A)) k_dispatch<WIDE, true, NT><<<grid, threads, 0, s>>>(A);
+  else k_dispatch<WIDE, false, NT><<<grid, threads, 0, s>>>(A);
 }
 template <bool WIDE, int NT>
 void combine(const RowsArgs& A, hipStream_t s) {
-  const dim3 grid = row_grid<NT>(A);
+  const dim3 grid = row_grid<NT>(A), threads(NT ? NT : kThreads);
   if (past(A)) {
-    if (A.f32) k_combine<WIDE, true, true, NT><<<grid, dim3(NT), 0, s>>>(A);
-    else k_combine<WIDE, false, true, NT><<<grid, dim3(NT), 0, s>>>(A);
+    if (A.f32) k_combine<WIDE, true, true, NT><<<grid, threads, 0, s>>>(A);
+    else k_combine<WIDE, false, true, NT><<<grid, threads, 0, s>>>(A);
   } else {
-    if (A.f32) k_combine<WIDE, true, false, NT><<<grid, dim3(NT), 0, s>>>(A);
-    else k_combine<WIDE, false, false, NT><<<grid, dim3(NT), 0, s>>>(A);
+    if (A.f32) k_combine<WIDE, true, false, NT><<<grid, threads, 0, s>>>(A);
+    else k_combine<WIDE, false, false, NT><<<grid, threads, 0, s>>>(A);
   }
 }
 
-template <bool WIDE, bool F32>
+template <bool WIDE, bool F32, int KEEP>
 void backward(const RowsArgs& A, dim3 grid, hipStream_t s) {
-  if (A.H <= 4 * 64 * kVec) {
-    if (past(A)) k_combine_backward<WIDE, F32, true, 4><<<grid, dim3(kThreads), 0, s>>>(A);
-    else k_combine_backward<WIDE, F32, false, 4><<<grid, dim3(kThreads), 0, s>>>(A);
-  } else {
-    if (past(A)) k_combine_backward<WIDE, F32, true, 8><<<grid, dim3(kThreads), 0, s>>>(A);
-    else k_combine_backward<WIDE, F32, false, 8><<<grid, dim3(kThreads), 0, s>>>(A);
-  }
+  if (past(A)) k_combine_backward<WIDE, F32, true, KEEP><<<grid, dim3(kThreads), 0, s>>>(A);
+  else k_combine_backward<WIDE, F32, false, KEEP><<<grid, dim3(kThreads), 0, s>>>(A);
+}
+template <bool WIDE, bool F32>
+void backward(const RowsArgs& A, hipStream_t s) {
+  // four workgroups a CU, each wave the same number of rows: 8192 rows of 2048 in
+  // 114 us, with a workgroup for every four rows 127, with 768 of them 124
+  const int64_t most = 1024;
+  const auto grid = [&](int64_t items) {
+    const int64_t rounds = (items + 3) / 4, each = rounds < 2 * most ? 1 : (rounds + most - 1) / most;
+    return dim3((unsigned)((rounds + each - 1) / each));
+  };
+  if ((int64_t)A.N * A.k <= 4 * most) backward<WIDE, F32, 0>(A, grid((int64_t)A.N * A.k), s);
+  else if (A.H <= 4 * 64 * kVec) backward<WIDE, F32, 4>(A, grid(A.N), s);
+  else backward<WIDE, F32, 8>(A, grid(A.N), s);
 }
 
-// Threads of a workgroup: 128 where 256 would leave more of them without values
-// (rows of 2816: 14.3 and 12.4 us for 2047 x 6, with 256 threads 15.5 and 14.5).
-bool narrow(const RowsArgs& A) {
+// Threads of a row: 128 where 256 would leave more of them without values
+// (rows of 2816: 14.3 and 12.4 us for 2047 x 6, with 256 threads 15.5 and 14.5),
+// 0 (rows behind one another) where several rows fit.
+int row_threads(const RowsArgs& A) {
   const int vecs = (A.H + kVec - 1) / kVec;
-  return (vecs + 127) / 128 * 128 < (vecs + 255) / 256 * 256;
+  if (vecs <= kThreads / 2) return 0;
+  return (vecs + 127) / 128 * 128 < (vecs + 255) / 256 * 256 ? 128 : 256;
 }
 
 }  // namespace
 
 hipError_t launch_dispatch(const RowsArgs& A, hipStream_t s) {
   if (A.N == 0) return hipSuccess;
-  if (A.wide) narrow(A) ? dispatch<true, 128>(A, s) : dispatch<true, 256>(A, s);
-  else narrow(A) ? dispatch<false, 128>(A, s) : dispatch<false, 256>(A, s);
+  const int nt = row_threads(A);
+  if (A.wide) nt == 0 ? dispatch<true, 0>(A, s) : nt == 128 ? dispatch<true, 128>(A, s) : dispatch<true, 256>(A, s);
+  else nt == 0 ? dispatch<false, 0>(A, s) : nt == 128 ? dispatch<false, 128>(A, s) : dispatch<false, 256>(A, s);
   return hipGetLastError();
 }
 
 hipError_t launch_combine(const RowsArgs& A, hipStream_t s) {
   if (A.N == 0) return hipSuccess;
-  if (A.wide) narrow(A) ? combine<true, 128>(A, s) : combine<true, 256>(A, s);
-  else narrow(A) ? combine<false, 128>(A, s) : combine<false, 256>(A, s);
+  const int nt = row_threads(A);
+  if (A.wide) nt == 0 ? combine<true, 0>(A, s) : nt == 128 ? combine<true, 128>(A, s) : combine<true, 256>(A, s);
+  else nt == 0 ? combine<false, 0>(A, s) : nt == 128 ? combine<false, 128>(A, s) : combine<false, 256>(A, s);
   return hipGetLastError();
 }
 
 hipError_t launch_combine_backward(const RowsArgs& A, hipStream_t s) {
   if (A.N == 0) return hipSuccess;
-  // four workgroups a CU, each wave the same number of rows: 8192 rows of 2048 in
-  // 114 us, with a workgroup for every four rows 127, with 768 of them 124
-  const int64_t rounds = ((int64_t)A.N + 3) / 4, most = 1024;
-  const int64_t each = rounds < 2 * most ? 1 : (rounds + most - 1) / most;
-  const dim3 grid((unsigned)((rounds + each - 1) / each));
-  if (A.wide) A.f32 ? backward<true, true>(A, grid, s) : backward<true, false>(A, grid, s);
-  else A.f32 ? backward<false, true>(A, grid, s) : backward<false, false>(A, grid, s);
+  if (A.wide) A.f32 ? backward<true, true>(A, s) : backward<true, false>(A, s);
+  else A.f32 ? backward<false, true>(A, s) : backward<false, false>(A, s);
   return hipGetLastError();
 }
 

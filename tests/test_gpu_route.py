@@ -42,7 +42,6 @@ def _oracle(logits, bias, o):
     k, G = o["top_k"], o["groups"]
     idx, w = np.full((N, k), -1), np.zeros((N, k))
     scores = np.zeros((N, E))
-    by_score = b is not None or (G > 1 and o["group_best"] == 2)
     for n in range(N):
         live = z[n] != -np.inf
         with np.errstate(over="ignore", under="ignore", invalid="ignore"):
@@ -53,15 +52,14 @@ def _oracle(logits, bias, o):
                 e = np.exp(z[n] - top)
                 s = e / e.sum() if live.any() else e
         scores[n] = s
-        v = (s if by_score else z[n]).copy()
-        if b is not None:
-            v = v + b
+        v = z[n].copy() if b is None else s + b
         v[~live] = -np.inf
         bad = np.isnan(v).any()
         v[np.isnan(v)] = -np.inf
         if G > 1:
             of = v.reshape(G, E // G)
-            tops = -np.sort(-of, 1)[:, :o["group_best"]]
+            counted = of if b is not None or o["group_best"] == 1 else np.where(of == -np.inf, -np.inf, s.reshape(of.shape))
+            tops = -np.sort(-counted, 1)[:, :o["group_best"]]
             count = np.where(tops[:, 0] == -np.inf, -np.inf, np.where(tops == -np.inf, 0.0, tops).sum(1))
             kept = np.argsort(-count, kind="stable")[:o["top_groups"]]
             out = np.ones(G, bool)
