@@ -899,7 +899,7 @@ def adamw_step(params, grads, states, step, lr, betas=(0.9, 0.999), eps: float =
     """One AdamW step over many tensors, in place and unseen by autograd: ``params`` (all float32 or
     all bf16), their ``grads`` (all float32 or all bf16; a parameter whose
     gradient is None is left out) and their ``states`` (``adamw_state``, all of one
-    kind), at ``step`` (1 for the first).
+    kind, each of one parameter alone), at ``step`` (1 for the first).
 
     ``m = b1 m + (1 - b1) g``, ``v = b2 v + (1 - b2) g^2``, ``p -= lr
     (weight_decay p + m / (1 - b1^t) / (sqrt(v / (1 - b2^t)) + eps))`` in float32.
@@ -952,8 +952,8 @@ def adamw_step(params, grads, states, step, lr, betas=(0.9, 0.999), eps: float =
             rows += (0, 0)
         rows += (0 if c is None else _arg(c, kept, "copies", shape, dev), n)
     table = (ctypes.c_int64 * len(rows))(*rows)
-    starts = [a for a, n in zip(rows[::8], rows[7::8]) if n]
-    if len(set(starts)) != len(starts):
+    written = [a for i in (0, 2, 3, 4, 5, 6) for a in rows[i::8] if a]
+    if len(set(written)) != len(written):
         raise ValueError("a tensor is given twice")
     conf = Adamw(_TYPES[pt], _TYPES[gt], 32 if kinds == 2 else 8, 0, 0.0, betas[0], betas[1], eps, weight_decay)
     if isinstance(step, torch.Tensor):

@@ -173,6 +173,27 @@ def test_the_same_tensor_twice_is_refused(C):
 
 
 @pytest.mark.parametrize("bits", [32, 8])
+def test_the_same_state_twice_is_refused(C, bits):
+    """Whatever the step writes: moments, their scales, copies."""
+    g = torch.ones(10, device="cuda")
+    params = [torch.ones(10, device="cuda") for _ in range(2)]
+    a, b = C.adamw_state(g, bits), C.adamw_state(g, bits)
+    copy = torch.zeros(10, dtype=torch.bfloat16, device="cuda")
+    given = [([a, a], None), ([a, b[:1] + a[1:2] + b[2:]], None), ([a, b], [copy, copy])]
+    if bits == 8:
+        given.append(([a, b[:2] + a[2:3] + b[3:]], None))
+    else:
+        given.append(([a, (b[0], b[0])], None))
+    for states, copies in given:
+        with pytest.raises(ValueError, match="twice"):
+            C.adamw_step(params, [g, g], states, 1, 1e-3, copies=copies)
+    torch.cuda.synchronize()
+    assert all((p == 1).all() for p in params) and not any(s.float().any() for s in a + b) and not copy.any()
+    empty = [torch.zeros(0, device="cuda") for _ in range(2)]
+    C.adamw_step(empty, empty, [C.adamw_state(e, bits) for e in empty], 1, 1e-3)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
 def test_many_tensors(C, bits):
     """More tensors than a launch's table holds, each as if it were alone."""
     sizes = [(i * 37) % 700 for i in range(95)]
