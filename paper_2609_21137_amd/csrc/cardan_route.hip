@@ -208,10 +208,10 @@ int row_bytes(const RouteArgs& A) {
   return A.slots * 8 + (A.groups > 1 ? kGroupBytes : 0) + std::max(std::max(list, values), more);
 }
 
-// value[g], g < groups (LDS): which are kept, and the least of these and the
-// largest of the others over this lane's groups.
-template <int LPR, class V>
-__device__ __forceinline__ void rank_groups(const RouteArgs& A, int at, const V* value, int* keep, V& least, V& most) {
+// value[g], g < groups (LDS): which are kept. near(kept, x, g) for this lane's
+// groups that are there.
+template <int LPR, class V, class F>
+__device__ __forceinline__ void rank_groups(const RouteArgs& A, int at, const V* value, int* keep, F near) {
   for (int grp = at; grp < A.groups; grp += LPR) {
     const V x = value[grp];
     int before = 0;
@@ -219,17 +219,16 @@ __device__ __forceinline__ void rank_groups(const RouteArgs& A, int at, const V*
       const V o = value[h];
       before += o > x || (o == x && h < grp);
     }
-    const bool in = before < A.top_groups && x != (V)-INFINITY;
+    const bool there = x != (V)-INFINITY, in = there && before < A.top_groups;
     keep[grp] = in;
-    if (in) least = x < least ? x : least;
-    else most = x > most ? x : most;
+    if (there) near(in, x, grp);
   }
 }
-// Values of the groups from all[E] (LDS): 2^group_split lanes a group (237 rows
-// of 180 experts in two groups: 11.5 us, with one lane a group 17.8; 56 of 504 in
-// four: 14.2 and 23.0).
-template <int LPR, class V>
-__device__ __forceinline__ void value_groups(const RouteArgs& A, int at, const V* all, V* value) {
+// What a group counts by from all[E] (LDS), as put(g, best, second best or 0):
+// 2^group_split lanes a group (237 rows of 180 experts in two groups: 11.5 us,
+// with one lane a group 17.8; 56 of 504 in four: 14.2 and 23.0).
+template <int LPR, class V, class F>
+__device__ __forceinline__ void value_groups(const RouteArgs& A, int at, const V* all, F put) {
   const int lg = A.group_split, sub = at & ((1 << lg) - 1);
   for (int first = 0; first < A.groups; first += LPR >> lg) {
     const int grp = first + (at >> lg);
@@ -251,7 +250,7 @@ __device__ __forceinline__ void value_groups(const RouteArgs& A, int at, const V
     if (lg > 1) join(lane_move<0x4E>(b1), lane_move<0x4E>(b2));
     if (lg > 2) join(lane_move<0x141>(b1), lane_move<0x141>(b2));
     if (lg > 3) join(lane_move<0x140>(b1), lane_move<0x140>(b2));
-    if (sub == 0 && grp < A.groups) value[grp] = A.best == 2 && b2 != (V)-INFINITY ? b1 + b2 : b1;
+    if (sub == 0 && grp < A.groups) put(grp, b1, A.best == 2 && b2 != (V)-INFINITY ? b2 : (V)0);
   }
 }
 
@@ -291,13 +290,21 @@ __device__ __forceinline__ void exact_values(const RouteArgs& A, bool scores, in
 }
 
 // Experts outside the kept groups leave the selection, by float32 values v
-// that are at most `margin` / 4 off; by the exact ones where that does not
-// decide.
+// whose scores are at most `margin` / 4 off; by the exact ones where that does
+// not decide. A group's value is off by margin / 2 for its scores, by 2^-24 |v|
+// for each of its best two (the bias was added to them) and 2^-24 of the sum;
+// the end of that interval is rounded once more. All of these are relative to
+// the sizes of the two, whose sum may be small where they cancel: 3 2^-24 of
+// |best| + |second| and a little, each group's own.
 template <class L, class V, int LPR, int EPL>
 __device__ __forceinline__ void keep_groups(float (&v)[EPL], const RouteArgs& A, int at, const L* row, float margin,
                                             const RowLds& X) {
-  float* value = reinterpret_cast<float*>(X.group);
+  float *value = reinterpret_cast<float*>(X.group), *off = value + 64;  // (exact values take the place of both)
   int* keep = reinterpret_cast<int*>(X.group + 64 * 8);
+  const auto put = [&](int grp, float best, float second) {
+    value[grp] = best + second;
+    off[grp] = 0.5f * margin + (fabsf(best) + fabsf(second)) * 0x1.9p-23f;
+  };
   const int lg = A.group_lanes;  // log2 of a group's lanes where it is made of whole ones, else -1
   if (lg >= 0) {
     float b1 = -INFINITY, b2 = -INFINITY;
@@ -314,27 +321,33 @@ __device__ __forceinline__ void keep_groups(float (&v)[EPL], const RouteArgs& A,
     if (lg > 1) join(lane_move<0x4E>(b1), lane_move<0x4E>(b2));
     if (lg > 2) join(lane_move<0x141>(b1), lane_move<0x141>(b2));
     if (lg > 3) join(lane_move<0x140>(b1), lane_move<0x140>(b2));
-    if ((at & ((1 << lg) - 1)) == 0 && at >> lg < A.groups) value[at >> lg] = A.best == 2 && b2 != -INFINITY ? b1 + b2 : b1;
+    if ((at & ((1 << lg) - 1)) == 0 && at >> lg < A.groups) put(at >> lg, b1, A.best == 2 && b2 != -INFINITY ? b2 : 0.f);
   } else {
     float* all = reinterpret_cast<float*>(X.area);
 #pragma unroll
     for (int i = 0; i < EPL; ++i) all[at * EPL + i] = v[i];
     wave_sync();
-    value_groups<LPR>(A, at, all, value);
+    value_groups<LPR>(A, at, all, put);
   }
   wave_sync();
+  // the least that a kept group may be, the most that another one may be
   float least = INFINITY, most = -INFINITY;
-  rank_groups<LPR>(A, at, value, keep, least, most);
+  rank_groups<LPR>(A, at, value, keep, [&](bool in, float x, int grp) {
+    const float o = off[grp];
+    const float end = o < INFINITY ? (in ? x - o : x + o) : in ? -INFINITY : INFINITY;
+    if (in) least = fminf(least, end);
+    else most = fmaxf(most, end);
+  });
   wave_sync();
   if (margin != 0.f) {
     least = -row_max<LPR>(-least);
     most = row_max<LPR>(most);
-    if (!(most == -INFINITY || least - most > margin + 0x1p-23f * (fabsf(least) + fabsf(most)))) {
-      V a = 0, b = 0, *exact = reinterpret_cast<V*>(X.group);
+    if (!(most == -INFINITY || least > most)) {
+      V* exact = reinterpret_cast<V*>(X.group);
       exact_values<L, V, LPR, EPL>(A, A.by_score, at, row, X);
-      value_groups<LPR>(A, at, reinterpret_cast<V*>(X.area), exact);
+      value_groups<LPR>(A, at, reinterpret_cast<V*>(X.area), [&](int grp, V best, V second) { exact[grp] = best + second; });
       wave_sync();
-      rank_groups<LPR>(A, at, exact, keep, a, b);
+      rank_groups<LPR>(A, at, exact, keep, [](bool, V, int) {});
       wave_sync();
     }
   }

@@ -1,0 +1,71 @@
+"""Groups whose best two experts float32 does not add up: large biases of
+opposite sign leave a small sum of values whose roundings are large. The
+selection has to be float64's all the same, places and weights (bounds of
+tests/test_gpu_route.py) too.
+
+Logits are drawn so that the groups' sums lie a few roundings of the biased
+values apart; rows in which two sums, or two values, are closer than 2^-44 of
+the bias are left out, so that two float64 exponentials agree on the order.
+"""
+
+import pytest
+import torch
+from test_gpu_route import _check, _opts
+
+pytestmark = pytest.mark.gpu
+
+F32, F64, BF = torch.float32, torch.float64, torch.bfloat16
+
+
+@pytest.fixture(scope="module")
+def C():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2609_21137_amd import cardan
+    return cardan
+
+
+def _told_apart(z, bias, score, groups, gap):
+    s = torch.sigmoid(z.double()) if score == "sigmoid" else torch.softmax(z.double(), 1)
+    v = s + bias.double()
+    sums = v.view(z.shape[0], groups, -1).topk(2, 2).values.sum(2)
+    return (sums.sort(1).values.diff(dim=1) > gap).all(1) & (v.sort(1).values.diff(dim=1) > gap).all(1)
+
+
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("groups,each", [(4, 2), (8, 2), (4, 16), (8, 32), (6, 7), (64, 16)])
+@pytest.mark.parametrize("size", [32.0, 100.0, 1024.0, 1e4])
+def test_best_two_that_cancel(C, score, groups, each, size):
+    E, g = groups * each, torch.Generator().manual_seed(groups * each)
+    # the best of a group at +size, the second at -size, the others far below; no two alike
+    bias = torch.empty(groups, each, dtype=F64)
+    bias[:, 0], bias[:, 1] = size, -size
+    bias[:, 2:] = -4 * size - torch.arange(max(0, each - 2)) * size
+    bias = bias.view(E).float()
+    wide = min(0.5, size * 2.0 ** -22 * (1.0 if score == "sigmoid" else E))
+    z = ((torch.rand((2000, E), generator=g, dtype=F64) - 0.5) * wide * 8).float()
+    keep = _told_apart(z, bias, score, groups, size * 2.0 ** -44)
+    assert keep.sum() >= 300
+    z = z[keep]
+    for top in {1, groups // 2, groups - 1}:
+        o = _opts(min(8, top * each), score, True, 1.0, groups, top, 2)
+        for part in (z[:1], z[:60], z[:300]):
+            _check(C, part.cuda(), bias.cuda(), o)
+        _check(C, z[:300].double().cuda(), bias.cuda(), o)
+
+
+def test_two_groups_of_two(C):
+    """Float32 has 1 and 1.000061 for the two groups, float64 1.0000597 and 1.0000365."""
+    bias = torch.tensor([1024.0, -1024.0, 1024.0, -1024.0], device="cuda")
+    z = torch.tensor([[2.39e-4, 0.0, 0.0, 1.46e-4]], device="cuda")
+    idx = C.route_rows(z, 1, bias=bias, score="sigmoid", groups=2, top_groups=1, group_best=2)[0]
+    assert idx.tolist() == [[0]]
+    _check(C, z, bias, _opts(1, "sigmoid", True, 1.0, 2, 1, 2))
+
+
+def test_four_groups_of_two(C):
+    bias = torch.tensor([100.0, -100.0] * 4, device="cuda")
+    z = torch.tensor([[0.018112, -0.720061, 0.018211, -0.720161, 0.018055, -0.720078, 0.018151, -0.720109]], device="cuda")
+    idx = C.route_rows(z, 2, bias=bias, score="sigmoid", groups=4, top_groups=2, group_best=2)[0]
+    assert set((idx // 2).flatten().tolist()) == {0, 1}
+    _check(C, z, bias, _opts(2, "sigmoid", True, 1.0, 4, 2, 2))
