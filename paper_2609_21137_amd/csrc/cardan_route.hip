@@ -302,7 +302,8 @@ __device__ __forceinline__ void keep_groups(float (&v)[EPL], const RouteArgs& A,
   float *value = reinterpret_cast<float*>(X.group), *off = value + 64;  // (exact values take the place of both)
   int* keep = reinterpret_cast<int*>(X.group + 64 * 8);
   const auto put = [&](int grp, float best, float second) {
-    value[grp] = best + second;
+    // (a group that is there stays above -infinity, also where float32 has no such sum)
+    value[grp] = best == -INFINITY ? best : fmaxf(best + second, -3.402823466e38f);
     off[grp] = 0.5f * margin + (fabsf(best) + fabsf(second)) * 0x1.9p-23f;
   };
   const int lg = A.group_lanes;  // log2 of a group's lanes where it is made of whole ones, else -1

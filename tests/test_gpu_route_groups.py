@@ -69,3 +69,24 @@ def test_four_groups_of_two(C):
     idx = C.route_rows(z, 2, bias=bias, score="sigmoid", groups=4, top_groups=2, group_best=2)[0]
     assert set((idx // 2).flatten().tolist()) == {0, 1}
     _check(C, z, bias, _opts(2, "sigmoid", True, 1.0, 4, 2, 2))
+
+@pytest.mark.parametrize("N", [1, 40, 300])
+@pytest.mark.parametrize("groups,each", [(4, 2), (4, 16), (6, 7)])
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("low,high", [(torch.finfo(F32).min, 0.0), (-2e38, 0.0), (torch.finfo(F32).min, 2e38),
+                                      (-2e38, torch.finfo(F32).max)])
+def test_best_two_whose_sum_is_past_float32(C, N, groups, each, score, low, high):
+    """Biases of the type's lowest value keep an expert behind all others; it is there all the same, and
+    its group comes before none. (Such a bias swallows the score: equal values go to the lower index.)"""
+    E = groups * each
+    bias = torch.zeros(groups, each)
+    bias[1:] = low
+    bias[0] = high
+    bias = bias.view(E).cuda()
+    z = torch.randn((N, E), generator=torch.Generator().manual_seed(N)).cuda()
+    z[-1, : 2 * each] = -float("inf")
+    for top in (1, 2, groups - 1):
+        for dtype in (F32, BF, F64):
+            o = _opts(min(8, top * each), score, True, 1.0, groups, top, 2)
+            idx = _check(C, z.to(dtype), bias, o)[0]
+            assert (idx[:-1] >= 0).all()
