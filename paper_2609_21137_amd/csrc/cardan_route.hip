@@ -557,8 +557,10 @@ __device__ __forceinline__ void route_row(const RouteArgs& A, int n, int lane, c
         }
         if (A.bias) {
 #pragma unroll
-          for (int i = 0; i < EPL; ++i)
-            if (e0 + i < A.E) v[i] += A.bias[e0 + i];
+          for (int i = 0; i < EPL; ++i) {  // (no bias makes an expert be there)
+            const float b = e0 + i < A.E ? A.bias[e0 + i] : 0.f;
+            v[i] = v[i] == -INFINITY ? v[i] : v[i] + b;
+          }
         }
       }
     }
