@@ -751,10 +751,11 @@ def route_rows(logits, top_k: int, bias=None, score: str = "softmax", renorm: bo
                 _arg(place, i32, "place", (N, top_k), dev, offsets is None),
                 _arg(offsets, i32, "offsets", (E + 1,), dev, place is None))
     else:
-        # (one allocation: each takes as long as a tenth of a small call)
-        idx, place, weight = torch.empty((3, N, top_k), dtype=i32, device=dev).unbind()
-        weight = weight.view(f32)
-        place, offsets = (place, torch.empty((E + 1,), dtype=i32, device=dev)) if places else (None, None)
+        # (each an allocation of its own: parts of one would start anywhere, which calls that take the weights on
+        # 16 bytes refuse, and share a version, so that a change of idx spoils a graph that keeps the weights)
+        idx = torch.empty((N, top_k), dtype=i32, device=dev)
+        weight = torch.empty((N, top_k), dtype=f32, device=dev)
+        place, offsets = (torch.empty_like(idx), torch.empty((E + 1,), dtype=i32, device=dev)) if places else (None, None)
         outs = (idx.data_ptr(), weight.data_ptr(), place.data_ptr() if places else None,
                 offsets.data_ptr() if places else None)
     need = _route_bytes(E, top_k, N) if offsets is not None else 0
