@@ -221,12 +221,21 @@ def bf16_bits(t: torch.Tensor) -> np.ndarray:
 
 @dataclass
 class DeviceLayer:
-    """One layer's weights as device tensors (field names of ``cardan_layer``)."""
+    """One layer's weights as device tensors (field names of ``cardan_layer``).
+
+    ``routing``: the arguments of ``route_rows`` that the layer was trained to
+    route by (the key of that name of a layer dict, ``fit.distill_layer``). Such
+    a layer runs by ``route_rows(logits, top_k, **layer.routing)`` and
+    ``vq_lr_expert_ffn``; calls that route by themselves, by the softmax over the
+    kept logits, refuse it."""
     tensors: dict
+    routing: dict | None = None
 
     @classmethod
     def from_numpy(cls, L: dict, device="cuda") -> "DeviceLayer":
-        T = {}
+        T, routing = {}, L.get("routing")
+        if routing is not None and routing.get("bias") is not None:
+            routing = {**routing, "bias": torch.as_tensor(routing["bias"], dtype=torch.float32).to(device)}
         for key in LAYER_FIELDS:
             v = L.get(key)
             if v is None:
@@ -239,9 +248,12 @@ class DeviceLayer:
                 T[key] = torch.from_numpy(np.ascontiguousarray(v)).to(device)
             else:
                 T[key] = torch.from_numpy(np.ascontiguousarray(v, dtype=np.float32)).to(device)
-        return cls(T)
+        return cls(T, routing)
 
-    def struct(self) -> LayerStruct:
+    def struct(self, routed: bool = False) -> LayerStruct:
+        """``routed``: the call is given its routing."""
+        if self.routing and not routed:
+            raise ValueError("this layer has a routing of its own: run it by route_rows and vq_lr_expert_ffn")
         vals = []
         for key in LAYER_FIELDS:
             t = self.tensors.get(key)
@@ -303,7 +315,7 @@ def vq_lr_expert_ffn(shape: Shape, x, topk_idx, topk_w, z, layer: DeviceLayer, w
     y = out if out is not None else torch.empty((B, shape.H), dtype=torch.float32, device=dev)
     if ws is None:
         ws = new_workspace(shape, B, dev)
-    st = layer.struct()
+    st = layer.struct(routed=True)
     _check(_lib.cardan_vq_lr_expert_ffn(
         ctypes.byref(shape), B, _ptr(x, torch.bfloat16, "x", (B, shape.H)),
         _ptr(topk_idx, torch.int32, "topk_idx", (B, shape.top_k)),

@@ -14,7 +14,7 @@ bases and coefficients of such a layer on a GPU (``TrainedLayer``,
 ``distill_layer``): the experts run as dense bf16 matrices through the
 library's feed-forward block and its gradients, and the logits behind the
 layer are held against a teacher's kept top logits by its distillation loss.
-Index maps and routing stay as they are. Reading: the paper trains a whole
+Index maps stay as they are, and so does the router unless it is trained, too. Reading: the paper trains a whole
 model end to end; here the model behind the layer is one matrix to logits, or
 whatever produces the gradient of the layer's output.
 
@@ -391,6 +391,10 @@ class _WordSums:
         return torch.segment_reduce(parts.double(), "sum", lengths=self.pieces, axis=0, initial=0).float()
 
 
+# cardan.route_rows's arguments, with which it routes as a layer does
+ROUTING = dict(score="softmax", bias=None, renorm=True, scale=1.0, groups=1, top_groups=1, group_best=1)
+
+
 class TrainedLayer:
     """A compressed layer whose code books and low-rank factors are trained.
 
@@ -404,7 +408,10 @@ class TrainedLayer:
     ``routing`` (a dict of ``cardan.route_rows``'s arguments: score, bias,
     groups, ...) routes by it instead of by the softmax over the kept logits,
     and the rows go to their experts and back by ``cardan.dispatch_rows`` and
-    ``cardan.combine_rows``. ``train_router`` makes the router a factor, too
+    ``cardan.combine_rows``. The layer dict of such a layer keeps what it is
+    trained for under ``routing`` (its bias as float32 on the host), and a
+    layer dict that has it is routed by it unless ``routing`` says otherwise.
+    ``train_router`` makes the router a factor, too
     (``router_w`` and, where the layer has one, ``router_bias``); its gradient
     is that of the experts' weights."""
 
@@ -425,6 +432,10 @@ class TrainedLayer:
         self.router_w = cardan.bf16_tensor(layer["router_w"], self.device)
         bias = layer.get("router_bias")
         self.router_bias = None if bias is None else torch.as_tensor(bias, device=self.device)
+        if routing is None:
+            routing = layer.get("routing")
+        if routing is not None and isinstance(routing.get("bias"), np.ndarray):
+            routing = {**routing, "bias": torch.as_tensor(routing["bias"], device=self.device)}
         self.routing = {} if train_router and routing is None else routing
         self.train_router = train_router
         if train_router:
@@ -568,9 +579,22 @@ class TrainedLayer:
                 grads[name] = grads[name] + g if name in grads else g
         return grads
 
+    def _stored_routing(self) -> dict:
+        """What of the routing is not a layer's own."""
+        how = {**ROUTING, **(self.routing or {})}
+        if how["groups"] == how["top_groups"]:      # all groups are kept
+            how.update(groups=1, top_groups=1, group_best=1)
+        out = {n: how[n] for n in ROUTING if n != "bias" and how[n] != ROUTING[n]}
+        if how["bias"] is not None:
+            out["bias"] = how["bias"].detach().cpu().numpy()
+        return out
+
     def layer(self, like: dict) -> dict:
-        """The layer dict ``like`` with these factors, in storage formats."""
-        out = dict(like)
+        """The layer dict ``like`` with these factors, in storage formats, and
+        with the routing where it is not the softmax over the kept logits."""
+        out = {n: v for n, v in like.items() if n != "routing"}
+        if routing := self._stored_routing():
+            out["routing"] = routing
         for name, t in self.factors.items():
             host = t.detach().cpu().numpy()
             out[name] = host if name == "router_bias" else to_bf16_bits(host)
@@ -610,7 +634,9 @@ def distill_layer(layer: dict, X, head, teacher, ids, k: int, d: int, act: str =
     ``"adam"`` (torch's), ``"adamw"`` or ``"adamw8"`` (``cardan.adamw_step`` with
     float32 or 8-bit moments, and ``weight_decay``); ``routing`` and
     ``train_router`` as of ``TrainedLayer``. Returns ``(layer dict in storage
-    formats, mean loss [steps, 2])``."""
+    formats, mean loss [steps, 2])``. A layer distilled with another routing than
+    the softmax over the kept logits has it under ``routing`` and runs by
+    ``cardan.route_rows`` and ``cardan.vq_lr_expert_ffn`` (``cardan.DeviceLayer``)."""
     import torch
 
     from . import cardan
