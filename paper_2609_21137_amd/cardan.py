@@ -157,6 +157,13 @@ def _check(rc: int):
         raise CardanError(rc, _lib.cardan_last_error().decode())
 
 
+def _fits(*counts):
+    """Refuses what the library's 32-bit counts do not hold (ctypes keeps the low bits)."""
+    for n in counts:
+        if not -(1 << 31) <= n < 1 << 31:
+            raise ValueError(f"{n} does not fit 32 bits")
+
+
 def abi_version() -> int:
     return _lib.cardan_abi_version()
 
@@ -531,6 +538,7 @@ def ffn_shape(H, I, E=1, act="silu_glu") -> FfnShape:
 def ffn_workspace_bytes(shape: FfnShape, N: int) -> int:
     """Bytes of workspace of a forward or backward call over up to N rows (no
     zero fill needed; nothing is kept in it between calls)."""
+    _fits(N)
     out = ctypes.c_size_t(0)
     _check(_lib.cardan_ffn_workspace_bytes(ctypes.byref(shape), N, ctypes.byref(out)))
     return out.value
@@ -675,6 +683,7 @@ def distill_loss(logits, teacher, ids, labels=None, temperature: float = 1.0, ce
     if not isinstance(ids, torch.Tensor) or ids.dim() != 2:
         raise ValueError("ids must be a [N, K] tensor")
     K = ids.shape[1]
+    _fits(N, V, K)
     dt, f32, i32 = logits.dtype, torch.float32, torch.int32
     lp, ld = _rows_ptr(logits, dt, "logits", (N, V), dev)
     loss = out if out is not None else torch.empty((N, 2), dtype=f32, device=dev)
@@ -702,6 +711,7 @@ _TYPES = {torch.bfloat16: 0, torch.float32: 1, torch.float64: 2}
 def _routing(E, top_k, score, renorm, scale, groups, top_groups, group_best) -> Routing:
     if score not in SCORES:
         raise ValueError(f"unknown score {score!r}")
+    _fits(E, top_k, groups, top_groups, group_best)
     return Routing(E, top_k, SCORES[score], int(bool(renorm)), groups, top_groups, group_best, scale)
 
 
@@ -709,6 +719,7 @@ def route_rows_workspace_bytes(N: int, E: int, top_k: int, score: str = "softmax
                                scale: float = 1.0, groups: int = 1, top_groups: int = 1, group_best: int = 1) -> int:
     """Bytes of workspace of ``route_rows`` over up to N rows (no zero fill
     needed; nothing is kept in it between calls)."""
+    _fits(N)
     out = ctypes.c_size_t(0)
     r = _routing(E, top_k, score, renorm, scale, groups, top_groups, group_best)
     _check(_lib.cardan_route_rows_workspace_bytes(ctypes.byref(r), N, ctypes.byref(out)))
@@ -755,6 +766,8 @@ def route_rows(logits, top_k: int, bias=None, score: str = "softmax", renorm: bo
     ``route_rows_backward``."""
     lp, ld, kind = _logit_rows(logits)
     N, E = logits.shape
+    if N >> 31:
+        _fits(N)
     dev, i32, f32 = logits.device, torch.int32, torch.float32
     r = _routing(E, top_k, score, renorm, scale, groups, top_groups, group_best)
     if out is not None:
@@ -791,6 +804,8 @@ def route_rows_backward(logits, idx, dweight, top_k: int | None = None, score: s
     Where ``idx`` is -1 ``dweight`` is not looked at."""
     lp, ld, kind = _logit_rows(logits)
     N, E = logits.shape
+    if N >> 31:
+        _fits(N)
     dev = logits.device
     if not isinstance(idx, torch.Tensor) or idx.dim() != 2 or (top_k is not None and idx.shape[1] != top_k):
         raise ValueError("idx must be a [N, top_k] tensor")
@@ -822,11 +837,13 @@ def dispatch_rows(x, place, rows: int | None = None, out=None):
     N, H = _row_types(x, "x")
     k = _row_types(place, "place")[1]
     dev, bf = x.device, torch.bfloat16
+    M = _row_types(out, "out")[0] if out is not None else N * k if rows is None else rows
+    if (N | k | H | M) >> 31:
+        _fits(N, k, H, M)
     if out is not None:
-        xe, M = out, _row_types(out, "out")[0]
+        xe = out
         to = _arg(xe, bf, "out", (M, H), dev)
     else:
-        M = N * k if rows is None else rows
         xe = torch.empty((M, H), dtype=bf, device=dev)
         to = xe.data_ptr()
     args = (_arg(x, bf, "x", (N, H), dev), _arg(place, torch.int32, "place", (N, k), dev), to)
@@ -843,6 +860,8 @@ def combine_rows(ye, place, weight=None, dtype=torch.bfloat16, out=None):
     carries no autograd graph: ``combine_rows_backward``."""
     M, H = _row_types(ye, "ye")
     N, k = _row_types(place, "place")
+    if (N | k | H | M) >> 31:
+        _fits(N, k, H, M)
     dev = ye.device
     if out is not None:
         y, dtype = out, getattr(out, "dtype", None)
@@ -867,6 +886,8 @@ def combine_rows_backward(dy, ye, place, weight=None, need_dye: bool = True, nee
     asked for; ``dye`` and ``dweight`` give the tensors to write."""
     M, H = _row_types(ye, "ye")
     N, k = _row_types(place, "place")
+    if (N | k | H | M) >> 31:
+        _fits(N, k, H, M)
     dev = ye.device
     if not isinstance(dy, torch.Tensor) or dy.dtype not in (torch.bfloat16, torch.float32):
         raise ValueError("dy must be a [N, H] tensor of bfloat16 or float32")
@@ -929,6 +950,8 @@ def adamw_step(params, grads, states, step, lr, betas=(0.9, 0.999), eps: float =
     todo = [t for t in zip(params, grads, states, copies) if t[1] is not None]
     if not todo:
         return
+    if not isinstance(step, torch.Tensor):
+        _fits(step)
     p, g, s, _ = todo[0]
     if not isinstance(p, torch.Tensor) or not isinstance(g, torch.Tensor):
         raise TypeError("params and grads must be torch tensors")
