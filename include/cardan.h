@@ -448,9 +448,9 @@ int cardan_route_rows_backward(const cardan_routing* routing, int32_t N, int32_t
 
 /* xe[place[n][j]] = x[n] for the k places of every row: x [N][H] bf16, place
  * [N][k] int32, xe [M][H] bf16. Places outside [0, M) are none; rows of xe that
- * no place names are left as they were; a row named twice gets one of the two.
- * 1 <= k <= 32, 1 <= H <= 2^20. The gradient is cardan_combine_rows without
- * weights. */
+ * no place names are left as they were. A row named twice is unspecified: any
+ * mix of the two, not the same in every call. 1 <= k <= 32, 1 <= H <= 2^20. The
+ * gradient is cardan_combine_rows without weights. */
 int cardan_dispatch_rows(int32_t N, int32_t k, int32_t H, int32_t M, const cardan_bf16* x, const int32_t* place,
                          cardan_bf16* xe, hipStream_t stream);
 
@@ -465,7 +465,8 @@ int cardan_combine_rows(int32_t N, int32_t k, int32_t H, int32_t M, const cardan
  *   dye[place[n][j]] = weight[n][j] * dy[n]   (bf16; rows without a place stay)
  *   dweight[n][j] = <dy[n], ye[place[n][j]]>  (float32; 0 without a place)
  * dye or dweight may be NULL (not computed; ye is read for dweight alone). A
- * row of dye named twice gets one of the two. */
+ * row of dye named twice is unspecified: any mix of the two, not the same in
+ * every call (dweight is not concerned). */
 int cardan_combine_rows_backward(int32_t N, int32_t k, int32_t H, int32_t M, int32_t dy_type, const void* dy,
                                  const cardan_bf16* ye, const int32_t* place, const float* weight, cardan_bf16* dye,
                                  float* dweight, hipStream_t stream);

@@ -832,7 +832,8 @@ def dispatch_rows(x, place, rows: int | None = None, out=None):
     """Copies of the rows ``x [N, H]`` (bf16) at the places ``place [N, k]``
     (int32, as ``route_rows`` gives them): ``xe[place[n, j]] = x[n]`` in an
     array of ``rows`` rows (default N k). Places outside it are none; rows that
-    no place names are not written. The gradient of x is ``combine_rows`` of
+    no place names are not written, and a row named twice is unspecified (any mix of
+    the two). The gradient of x is ``combine_rows`` of
     xe's, without weights."""
     N, H = _row_types(x, "x")
     k = _row_types(place, "place")[1]
@@ -881,9 +882,9 @@ def combine_rows_backward(dy, ye, place, weight=None, need_dye: bool = True, nee
                           dweight=None):
     """Gradients of ``combine_rows`` for ``dy [N, H]`` (bf16 or float32):
     ``dye[place[n, j]] = weight[n, j] dy[n]`` (bf16, laid out as ye; rows that no
-    place names are not written) and ``dweight[n, j] = <dy[n], ye[place[n, j]]>``
-    (float32, 0 without a place). Returns ``(dye, dweight)``, None where not
-    asked for; ``dye`` and ``dweight`` give the tensors to write."""
+    place names are not written, a row named twice is unspecified) and ``dweight[n,
+    j] = <dy[n], ye[place[n, j]]>`` (float32, 0 without a place). Returns ``(dye,
+    dweight)``, None where not asked for; ``dye`` and ``dweight`` give the tensors to write."""
     M, H = _row_types(ye, "ye")
     N, k = _row_types(place, "place")
     if (N | k | H | M) >> 31:
@@ -941,7 +942,7 @@ def adamw_step(params, grads, states, step, lr, betas=(0.9, 0.999), eps: float =
     the mean, a function of step and place). ``step`` (int32) and ``lr`` (float32)
     may be one-element tensors on the device, which a captured call then follows;
     ``grad_scale`` (float32, one element on the device) multiplies every
-    gradient. ``copies``: bf16 tensors (or None) that receive float32 weights
+    gradient. What a step writes must not overlap. ``copies``: bf16 tensors (or None) that receive float32 weights
     rounded to bf16, as ``ffn_forward`` takes them."""
     params, grads, states = list(params), list(grads), list(states)
     copies = [None] * len(params) if copies is None else list(copies)
