@@ -419,9 +419,9 @@ int cardan_route_rows_workspace_bytes(const cardan_routing* routing, int32_t N, 
  * the kept s with renorm; the bias is in no weight. With softmax, renorm, no
  * bias and no groups this is cardan_route_topk's routing.
  * idx [N][top_k] int32, weight [N][top_k] float32.
- * A logit of -inf (or a v of -inf) is an expert that is not there; where fewer
- * than top_k are left (a padding row is one of -inf alone) the rest of idx is
- * -1 with weight 0. A NaN among a row's logits or v is never selected and makes
+ * A logit of -inf (or a v of -inf) is an expert that is not there, whatever its
+ * bias; where fewer than top_k are left (a padding row is one of -inf alone) the rest of idx is
+ * -1 with weight 0. Weights below 2^-126 may be rounded to 0. A NaN among a row's logits or v is never selected and makes
  * the row's weights NaN; +inf makes a softmax row's weights NaN.
  * place [N][top_k] and offsets [E + 1] (both or neither NULL): the (row,
  * selection) pairs of an expert e are rows offsets[e] <= p < offsets[e + 1] of

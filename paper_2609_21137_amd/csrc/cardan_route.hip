@@ -14,8 +14,8 @@
 // by vector instructions and latency, not by memory: 65536 rows of 128 float32
 // logits take 16 us, of which 8 are the read of 34 MB and the launch (4.2 TB/s);
 // a wave's pass over 8 rows is about 660 vector instructions. With a bias and
-// groups (8191 x 256) 19 us, 5 of them for the few rows whose groups float32
-// does not tell apart: their wave's float64 scores end the kernel. The places
+// groups (8191 x 256) 14 us, 19 to 20 where there are a few rows whose groups
+// float32 does not tell apart: their wave's float64 scores end the kernel. The places
 // are a second launch of 6 to 9 us, most of it the length of its barriers.
 #include <hip/hip_runtime.h>
 
@@ -799,7 +799,8 @@ constexpr int kPlaceThreads = 1024;
 // Places of a block's slots: after the slots of the experts before, of the same
 // expert in the blocks before, and of the waves before. Every workgroup sums
 // the blocks' counts by itself; a launch of its own for that took 5 us, this
-// takes one or two with the 256 blocks of large calls.
+// takes one or two with the 256 blocks of large calls (past 2^23 rows there are
+// more blocks, and every one sums all of them).
 __global__ __launch_bounds__(kPlaceThreads) void k_route_place(const RouteArgs A) {
   constexpr int NT = kPlaceThreads;
   extern __shared__ __align__(16) unsigned char lds[];

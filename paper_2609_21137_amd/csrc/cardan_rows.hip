@@ -109,7 +109,9 @@ constexpr int kThreads = 256;
 // written past the caches, which leaves them to the tokens' rows: 65536 x 2048
 // copied, combined and both gradients 286 us (about 50 more through the caches;
 // combine 60 instead of 80). A smaller one, just written, is still there: 12282 x 2816
-// combined in 15.5 us, past the caches 20.8.
+// combined in 14.6 us, past the caches 20.2. The array's size decides, also where a
+// call touches few of its rows: 2000 x 8 of 65536 rows of 2048 copied in 13.5 us and
+// combined in 15.6, through the caches 12.2 and 12.5; 16 x 8 of them no slower.
 constexpr int64_t kPastBytes = (int64_t)192 << 20;
 
 // The rows of a workgroup's threads. NT > 0: blockIdx.x is a run of a row's
@@ -276,14 +278,19 @@ void backward(const RowsArgs& A, hipStream_t s) {
     const int64_t rounds = (items + 3) / 4, each = rounds < 2 * most ? 1 : (rounds + most - 1) / most;
     return dim3((unsigned)((rounds + each - 1) / each));
   };
+  // A wave a row and place up to 4096 of them: 512 x 8 rows of 2048 in 8.6 us, with a
+  // wave a row 20.4; of 7168 in 30.4, with a wave a row 100. With many rows dy's row
+  // is read once: 5000 x 8 rows of 2048 in 75 us, else 92.5. In between the rule
+  // changes too early: 513 x 8 rows take 20.5 us instead of 8.2, 1000 x 8 31.6
+  // instead of 15.7, and rows of 7168 are slower up to 5000 x 8 (305, 265).
   if ((int64_t)A.N * A.k <= 4 * most) backward<WIDE, F32, 0>(A, grid((int64_t)A.N * A.k), s);
   else if (A.H <= 4 * 64 * kVec) backward<WIDE, F32, 4>(A, grid(A.N), s);
   else backward<WIDE, F32, 8>(A, grid(A.N), s);
 }
 
 // Threads of a row: 128 where 256 would leave more of them without values
-// (rows of 2816: 14.3 and 12.4 us for 2047 x 6, with 256 threads 15.5 and 14.5),
-// 0 (rows behind one another) where several rows fit.
+// (2047 x 6 rows of 2816 copied and combined in 15.3 and 19.4 us, with 256 threads
+// 18.0 and 20.8; from the caches 12.3 and 14.6, 14.6 and 15.6), 0 (rows behind one another) where several rows fit.
 int row_threads(const RowsArgs& A) {
   const int vecs = (A.H + kVec - 1) / kVec;
   if (vecs <= kThreads / 2) return 0;
